@@ -450,6 +450,150 @@ SSD_API void ssd_set_fault_injection(int kind, int countdown);
  * ssd_prefill / ssd_prefill_batch clears the word and the ctx is usable again.  async. */
 SSD_API ssd_status ssd_probe_bounded_wait(ssd_ctx* ctx, int64_t limit_ns);
 
+/* ---- Low-bit operators: a paged 8-bit K/V cache and 4-bit weights ----
+ * Building blocks of a decode step at about a quarter of the bytes of the engine's (bf16 weights,
+ * fp32 K/V).  They need no ctx and allocate nothing: the caller owns every buffer, including the
+ * workspaces, and describes them in plain structs.  All are async on cuda_stream (a cudaStream_t of
+ * the current device, NULL = legacy default stream), may be captured into a CUDA graph, and read
+ * lengths, tables and slots on the device only, so a decode loop needs no host round trip.
+ * The first call of each entry point on a device sets kernel attributes: make it before a capture.
+ * Calls that share an ssd_kv8's or a matmul's workspace must be ordered (one stream, or events).
+ * On failure ssd_op_last_error() holds a message for the calling thread. */
+
+/* Activation types. */
+enum { SSD_TYPE_BF16 = 0, SSD_TYPE_FP32 = 1 };
+
+#define SSD_KV8_MAX_BATCH 1024  /* seats of one block table */
+
+/* Bits of the cache's device status word, which ssd_kv8_status reads and clears. */
+enum {
+  SSD_KV8_NO_BLOCKS = 1,   /* the free stack ran out: rows without a block have slot -1 */
+  SSD_KV8_LENGTH = 2,      /* len / add / held out of range, or more rows than the step holds */
+  SSD_KV8_SLOT = 4,        /* a slot or block id outside the cache was skipped */
+  SSD_KV8_NON_FINITE = 8   /* a NaN (held as 0) or an infinity (held as the largest code) was appended */
+};
+
+/* A paged K/V cache in 8 bits.  Tokens live in blocks of block_tokens; block ids are shared by all
+ * layers.  A K (or V) vector of one kv head is held as head_dim codes c in -127..127 standing for
+ * c * s, with one fp32 scale s per layer, block, kv head and K / V.
+ *   data:   device, ssd_kv8_data_bytes(): [layer][block][kv head][16-token tile]{K, V}, the bytes of
+ *           a tile in the order the attention's matrix instructions take them; ssd_kv8_read returns
+ *           the values.  16-byte aligned.
+ *   scales: device fp32 [layer][block][kv head][2] (K, V), 8-byte aligned
+ *   table:  device int32 [max_batch][max_blocks], block ids of each seat in order
+ *   pool:   device int32 [n_blocks], the stack of free block ids (the last free one is handed out first)
+ *   work:   device, ssd_kv8_work_bytes(), zeroed once by the caller before the first call, 16-byte aligned */
+typedef struct {
+  int n_layers;
+  int n_heads;       /* query heads, a multiple of n_kv_heads */
+  int n_kv_heads;
+  int head_dim;      /* 64 or 128 */
+  int block_tokens;  /* 16, 32, 64 or 128 */
+  int n_blocks;
+  int max_batch;     /* seats, at most SSD_KV8_MAX_BATCH */
+  int max_blocks;    /* blocks one seat may hold */
+  void* data;
+  float* scales;
+  int32_t* table;
+  int32_t* pool;
+  void* work;
+} ssd_kv8;
+
+/* What one step works on, filled by ssd_kv8_plan: device int32, ssd_kv8_step_ints() of them, 8-byte aligned, in this order:
+ *   work_start int64 [batch + 1], seg_start [batch + 1]: the attention's partition (16-token tiles, items)
+ *   row_start  [batch + 1] prefix sums of the requests' new rows (rows of request b: row_start[b] ..)
+ *   len        [batch] tokens before the step
+ *   slot       [rows] block * block_tokens + offset of each new row, -1 for rows past the last request's
+ *             and rows without a block */
+typedef struct {
+  int batch;     /* requests: seats 0 .. batch - 1 */
+  int rows;      /* capacity: new rows of all requests */
+  int row_tile;  /* 8, 16 or 32: query rows x (n_heads / n_kv_heads) the attention takes at once; any
+                  * value is right, one near the usual product is fastest (0: from rows / batch) */
+  int32_t* data;
+} ssd_kv8_step;
+
+SSD_API int64_t ssd_kv8_data_bytes(const ssd_kv8* c);
+SSD_API int64_t ssd_kv8_work_bytes(const ssd_kv8* c);
+SSD_API int64_t ssd_kv8_step_ints(int batch, int rows);
+
+/* Block tables and slot maps of one step, from the requests' lengths.
+ *   len: device int32 [batch], tokens already in the cache; -1 gives the seat back: its held blocks go
+ *        on the free stack, in seat order, before any block of this call is handed out
+ *   add: device int32 [batch], new rows (0 = none this step; ignored for released seats)
+ *   state_in / state_out: device int32 [1 + max_batch], the number of free blocks and the blocks each
+ *        seat holds; may be the same buffer.  Seats beyond batch keep their count.
+ * A seat that holds fewer than ceil((len + add) / block_tokens) blocks gets the missing ones from the
+ * top of the stack, in seat order; one that holds more keeps them (a rollback after rejected drafts
+ * needs no call: pass the new len).  Writes the new entries of table, the step, and state_out; reads
+ * len / add on the device only.  Out-of-range values are clamped and flagged in the status word. */
+SSD_API ssd_status ssd_kv8_plan(const ssd_kv8* c, const ssd_kv8_step* step, const int32_t* len, const int32_t* add,
+                                const int32_t* state_in, int32_t* state_out, void* cuda_stream);
+
+/* Quantise rows of K and V into the cache at slot[row] (skipped when negative).
+ *   k, v: device, type SSD_TYPE_*, element (row, head, i) at row * row_stride + head * head_stride + i
+ *         (in elements, for k and v each)
+ * The rows of one block must be neighbours in the call and ascend by 1 (as ssd_kv8_plan lays them out).
+ * Per block, kv head and K / V: s' = max(s, amax / 127, 2^-100) with amax over the block's finite new
+ * values and s the block's scale, or 0 when a row goes to the block's first token.  If s' > s, the
+ * block's older codes become round(c * (s / s')).  New codes are round(x * (1 / s')) in -127..127, in
+ * fp32, ties to even. */
+SSD_API ssd_status ssd_kv8_append(const ssd_kv8* c, int layer, const void* k, const void* v, int type, int rows,
+                                  int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride,
+                                  int64_t v_head_stride, const int32_t* slot, void* cuda_stream);
+
+/* The values the cache holds at n slots: k, v = c * s, type SSD_TYPE_*, device [n][n_kv_heads][head_dim]
+ * (contiguous); zeros where slot is negative. */
+SSD_API ssd_status ssd_kv8_read(const ssd_kv8* c, int layer, const int32_t* slot, int n, void* k, void* v, int type,
+                                void* cuda_stream);
+
+/* Attention of a step's rows over the cache (its own K/V rows appended before):
+ *   o = sum_j softmax_j(scale * q . k_j) v_j
+ * Query head h reads kv head h / (n_heads / n_kv_heads).  Row i of request b (position len[b] + i) sees
+ * the keys before len[b] and, of the step's own rows j, those with bit j of row_mask[row] set -- or,
+ * with row_mask NULL, the rows j <= i.  A row that sees no key gives zeros, as do rows past the last
+ * request's.  Keys without a block are not seen.
+ *   q, o: device, type SSD_TYPE_*, element (row, head, i) at row * row_stride + head * head_stride + i;
+ *         o must not overlap q
+ *   row_mask: device uint32 [rows] or NULL (with it a request may have at most 32 rows)
+ * Scores, softmax statistics and sums are fp32; for bf16 rows the probabilities enter the products as
+ * fp16, for fp32 rows q and the probabilities as pairs of fp16. */
+SSD_API ssd_status ssd_kv8_attention(const ssd_kv8* c, int layer, const ssd_kv8_step* step, const void* q, void* o,
+                                     int type, int64_t q_row_stride, int64_t q_head_stride, int64_t o_row_stride,
+                                     int64_t o_head_stride, float scale, const uint32_t* row_mask, void* cuda_stream);
+
+/* Waits for the stream, reads and clears the status word: SSD_ERR_DEVICE if a bit was set.
+ * bits (host) may be NULL.  sync. */
+SSD_API ssd_status ssd_kv8_status(const ssd_kv8* c, int* bits, void* cuda_stream);
+
+#define SSD_W4_MAX_ROWS 16
+
+/* A weight matrix [n][k] in 4 bits: per row and group of `group` (32, 64 or 128) columns a bf16 scale
+ * s = amax / 7 (rounded to nearest even) and codes round(w * (1 / s)) in -8..7; k is padded to whole
+ * 128-column chunks and n to 16 rows with zeros.  Packed as [16-row tile][128-column chunk]{codes, scales}
+ * in the order the matrix instructions take them.  A group with a non-finite weight gives NaN. */
+SSD_API int64_t ssd_w4_bytes(int n, int k, int group);
+
+/* Pack w: device, type SSD_TYPE_*, [n][row_stride]; packed: device, 16-byte aligned. */
+SSD_API ssd_status ssd_w4_pack(const void* w, int type, int n, int k, int64_t row_stride, int group, void* packed,
+                               void* cuda_stream);
+
+/* The fp32 values c * s of a packed matrix: out device fp32 [n][k]. */
+SSD_API ssd_status ssd_w4_unpack(const void* packed, int n, int k, int group, float* out, void* cuda_stream);
+
+/* y = x W^T (+ residual), rows <= SSD_W4_MAX_ROWS, fp32 sums, each group's products scaled in fp32.
+ *   x: device, type SSD_TYPE_*, [rows][x_row_stride];  y: same type, [rows][y_row_stride]
+ *   residual: device [rows][res_row_stride] of the same type, or NULL; may be y itself
+ *   work: device, ssd_w4_work_bytes(), zeroed once before the first call, 16-byte aligned
+ * y must not overlap x. */
+SSD_API int64_t ssd_w4_work_bytes(int n, int k);
+SSD_API ssd_status ssd_w4_matmul(const void* packed, int n, int k, int group, const void* x, int type, int rows,
+                                 int64_t x_row_stride, void* y, int64_t y_row_stride, const void* residual,
+                                 int64_t res_row_stride, void* work, void* cuda_stream);
+
+/* The calling thread's last failure of a low-bit operator ("" if none). */
+SSD_API const char* ssd_op_last_error(void);
+
 SSD_API const char* ssd_status_string(ssd_status s);
 SSD_API const char* ssd_last_error(const ssd_ctx* ctx);
 

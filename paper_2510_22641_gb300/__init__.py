@@ -12,7 +12,7 @@ __all__ = ["build", "load", "SSDError", "SSD_ARCH_LLAMA", "SSD_ARCH_T5", "SSD_IN
            "SSD_MAX_GAMMA", "SSD_OPT_HOST_LOOP", "SSD_OPT_PREFILL_ROWS", "SSD_DLEN_CONTEXT", "SSD_DLEN_GENERATED",
            "SSD_FAULT_NONE", "SSD_FAULT_ALLOC",
            "SSD_FAULT_LAUNCH", "SSDModel", "bf16_bits_to_device", "encdec_device_weights", "config_dict",
-           "t5_config_dict", "set_fault_injection"]
+           "t5_config_dict", "set_fault_injection", "KV8Cache", "KV8Step", "W4Weight"]
 
 
 def set_fault_injection(kind: int, countdown: int) -> None:
@@ -22,10 +22,13 @@ def set_fault_injection(kind: int, countdown: int) -> None:
 
 
 def __getattr__(name):
-    # torch is only needed for the model wrapper; the ABI loader works without it.
+    # torch is only needed for the wrappers; the ABI loader works without it.
     if name in ("SSDModel", "bf16_bits_to_device", "encdec_device_weights"):
         from . import model
         return getattr(model, name)
+    if name in ("KV8Cache", "KV8Step", "W4Weight"):
+        from . import lowbit
+        return getattr(lowbit, name)
     raise AttributeError(name)
 
 

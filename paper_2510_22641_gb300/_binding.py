@@ -26,6 +26,14 @@ SSD_DLEN_GENERATED = 1
 SSD_FAULT_NONE = 0
 SSD_FAULT_ALLOC = 1
 SSD_FAULT_LAUNCH = 2
+SSD_TYPE_BF16 = 0
+SSD_TYPE_FP32 = 1
+SSD_KV8_MAX_BATCH = 1024
+SSD_KV8_NO_BLOCKS = 1
+SSD_KV8_LENGTH = 2
+SSD_KV8_SLOT = 4
+SSD_KV8_NON_FINITE = 8
+SSD_W4_MAX_ROWS = 16
 
 STATUS = {0: "SSD_OK", 1: "SSD_ERR_INVALID_ARG", 2: "SSD_ERR_OOM", 3: "SSD_ERR_CUDA", 4: "SSD_ERR_CAPACITY",
           5: "SSD_ERR_STATE", 6: "SSD_ERR_TIMEOUT", 7: "SSD_ERR_DEVICE", 8: "SSD_ERR_UNSUPPORTED"}
@@ -37,6 +45,9 @@ EXPORTED = ("ssd_create", "ssd_destroy", "ssd_prefill", "ssd_draft", "ssd_verify
             "ssd_last_launch_count", "ssd_prefill_batch", "ssd_decode_batch", "ssd_greedy_decode_batch",
             "ssd_generate_batch", "ssd_get_batch_stats", "ssd_get_batch_step_log", "ssd_lm_head",
             "ssd_lm_head_static", "ssd_profile_projection", "ssd_set_fault_injection", "ssd_probe_bounded_wait",
+            "ssd_kv8_data_bytes", "ssd_kv8_work_bytes", "ssd_kv8_step_ints", "ssd_kv8_plan", "ssd_kv8_append",
+            "ssd_kv8_read", "ssd_kv8_attention", "ssd_kv8_status", "ssd_w4_bytes", "ssd_w4_work_bytes", "ssd_w4_pack",
+            "ssd_w4_unpack", "ssd_w4_matmul", "ssd_op_last_error",
             "ssd_status_string", "ssd_last_error")
 
 
@@ -81,6 +92,16 @@ class SSDStats(ctypes.Structure):
                 "accept_hist": list(self.accept_hist), "kv_len": self.kv_len}
 
 
+class SSDKv8(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("n_layers", "n_heads", "n_kv_heads", "head_dim", "block_tokens", "n_blocks",
+                                            "max_batch", "max_blocks")] + \
+               [(n, ctypes.c_void_p) for n in ("data", "scales", "table", "pool", "work")]
+
+
+class SSDKv8Step(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("rows", ctypes.c_int), ("row_tile", ctypes.c_int), ("data", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -92,7 +113,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     if not os.path.exists(path):
         raise OSError(f"{path} not found: build it with paper_2510_22641_gb300.build.build()")
     lib = ctypes.CDLL(path)
-    i32, vp, pi32 = ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p
+    i32, i64, vp, pi32 = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p
     sig = {
         "ssd_create": [ctypes.POINTER(SSDConfig), ctypes.POINTER(SSDWeights), vp, ctypes.POINTER(vp)],
         "ssd_destroy": [vp],
@@ -121,6 +142,14 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "ssd_lm_head": [vp, vp, i32, vp, vp],
         "ssd_probe_bounded_wait": [vp, ctypes.c_int64],
         "ssd_lm_head_static": [vp, vp, vp, i32, i32, i32, ctypes.c_float, vp, vp, vp],
+        "ssd_kv8_plan": [vp, vp, vp, vp, vp, vp, vp],
+        "ssd_kv8_append": [vp, i32, vp, vp, i32, i32, i64, i64, i64, i64, vp, vp],
+        "ssd_kv8_read": [vp, i32, vp, i32, vp, vp, i32, vp],
+        "ssd_kv8_attention": [vp, i32, vp, vp, vp, i32, i64, i64, i64, i64, ctypes.c_float, vp, vp],
+        "ssd_kv8_status": [vp, vp, vp],
+        "ssd_w4_pack": [vp, i32, i32, i32, i64, i32, vp, vp],
+        "ssd_w4_unpack": [vp, i32, i32, i32, vp, vp],
+        "ssd_w4_matmul": [vp, i32, i32, i32, vp, i32, i32, i64, vp, i64, vp, i64, vp, vp],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -132,6 +161,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.ssd_draft_length.restype = ctypes.c_int
     lib.ssd_rel_bucket.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int]
     lib.ssd_rel_bucket.restype = ctypes.c_int
+    for name, args in {"ssd_kv8_data_bytes": [vp], "ssd_kv8_work_bytes": [vp], "ssd_kv8_step_ints": [i32, i32],
+                       "ssd_w4_bytes": [i32, i32, i32], "ssd_w4_work_bytes": [i32, i32]}.items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = i64
+    lib.ssd_op_last_error.argtypes = []
+    lib.ssd_op_last_error.restype = ctypes.c_char_p
     lib.ssd_status_string.argtypes = [ctypes.c_int]
     lib.ssd_status_string.restype = ctypes.c_char_p
     lib.ssd_last_error.argtypes = [vp]

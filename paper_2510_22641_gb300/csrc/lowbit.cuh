@@ -1,0 +1,148 @@
+// Shared definitions of the low-bit operators (paged 8-bit K/V cache, 4-bit weights): the byte
+// order of a cache tile, typed loads and stores, and the context-free error message.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace ssd {
+
+// Records the calling thread's message (a fixed buffer: nothing here throws) and returns `s`.
+ssd_status op_fail(ssd_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+// The status of a launch that has just been made.
+ssd_status op_launched(const char* what);
+
+// ------------------------------------------------------------------ cache layout
+//
+// A tile is 16 tokens of one block and kv head: 16 * D bytes of K, then 16 * D of V, a code c
+// held as the byte c + 128.  With mma.m16n8k16 a lane (g = lane / 4, t = lane % 4) needs, of K, the
+// keys of matrix rows g and g + 8 at four dimensions per 16-wide step, and of V, four keys at the
+// dimensions g and g + 8 of each 16.  Both are kept as one 4-byte word per lane and step, a lane's
+// words in 16-byte chunks, the 32 lanes' chunks next to each other: every 16-byte load of a warp is
+// one contiguous 512 bytes, and a lane reads back from shared memory the bytes it copied itself.
+//
+// Matrix row r of the score tile is token tile_token(r); the inverse is below.  Row r and r + 1
+// (r even) and r + 8, r + 9 are four consecutive tokens, which is what lets a V word hold them.
+
+constexpr int kTileTokens = 16;
+
+__host__ __device__ constexpr int kv8_tile_token(int r) {  // matrix row -> token of the tile
+  return 4 * ((r & 7) >> 1) + 2 * (r >> 3) + (r & 1);
+}
+
+// Byte of (token, dim) in the K half (resp. V half) of a tile.
+__host__ __device__ __forceinline__ constexpr int kv8_k_byte(int token, int d, int dim) {
+  const int row = 2 * (token >> 2) + (token & 1);  // matrix row modulo 8
+  const int j = (token >> 1) & 1;                  // 1: rows 8..15
+  const int word = j * (dim / 16) + (d >> 4);
+  const int lane = row * 4 + ((d >> 2) & 3);
+  return (word >> 2) * 512 + lane * 16 + (word & 3) * 4 + (d & 3);
+}
+__host__ __device__ __forceinline__ constexpr int kv8_v_byte(int token, int d) {
+  const int word = d >> 3;
+  const int lane = (d & 7) * 4 + (token >> 2);
+  return (word >> 2) * 512 + lane * 16 + (word & 3) * 4 + (token & 3);
+}
+
+// ------------------------------------------------------------------ typed access
+
+template <typename T>
+__device__ __forceinline__ float to_f32(T v);
+template <>
+__device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// Four consecutive elements.  VEC: p is aligned to them all.
+template <bool VEC>
+__device__ __forceinline__ float4 load4(const float* p) {
+  if constexpr (VEC) return *reinterpret_cast<const float4*>(p);
+  return make_float4(p[0], p[1], p[2], p[3]);
+}
+template <bool VEC>
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  if constexpr (VEC) {
+    const uint2 w = *reinterpret_cast<const uint2*>(p);
+    const float2 a = bf16x2_to_float2(w.x), b = bf16x2_to_float2(w.y);
+    return make_float4(a.x, a.y, b.x, b.y);
+  }
+  return make_float4(to_f32(p[0]), to_f32(p[1]), to_f32(p[2]), to_f32(p[3]));
+}
+
+// Whether rows at `p` with these strides (in elements of `size` bytes) can be read 4 elements at a time.
+inline bool aligned4(const void* p, int size, int64_t a, int64_t b) {
+  return reinterpret_cast<uintptr_t>(p) % (4 * size) == 0 && a % 4 == 0 && b % 4 == 0;
+}
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
+  return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+  return v;
+}
+
+// ------------------------------------------------------------------ the cache's workspace
+//
+// [64 ints: status word, plan ticket][attention tickets][attention partial states]
+
+constexpr int kKv8WorkHead = 64;  // ints
+
+inline bool kv8_shape_ok(const ssd_kv8* c) {
+  if (!c) return false;
+  const bool bs = c->block_tokens == 16 || c->block_tokens == 32 || c->block_tokens == 64 || c->block_tokens == 128;
+  if (!bs || (c->head_dim != 64 && c->head_dim != 128) || c->n_layers < 1 || c->n_kv_heads < 1 || c->n_blocks < 1)
+    return false;
+  if (c->n_heads < c->n_kv_heads || c->n_heads % c->n_kv_heads) return false;
+  if (c->max_batch < 1 || c->max_batch > SSD_KV8_MAX_BATCH || c->max_blocks < 1) return false;
+  // slots, row numbers and the attention's tile numbers fit 31 bits
+  const int64_t lim = 0x7fffffff;
+  const int64_t cap = static_cast<int64_t>(c->max_blocks) * c->block_tokens;
+  if (static_cast<int64_t>(c->n_blocks) * c->block_tokens > lim || cap > lim || c->n_heads > 65535) return false;
+  return cap * c->max_batch <= lim;
+}
+
+}  // namespace ssd
+
+namespace ssd {
+
+// The parts of a step's buffer (see ssd_kv8_step).
+struct StepView {
+  int64_t* work_start;
+  int32_t* seg_start;
+  int32_t* row_start;
+  int32_t* len;
+  int32_t* slot;
+};
+__host__ __device__ __forceinline__ StepView step_view(int32_t* d, int batch) {
+  StepView v;
+  v.work_start = reinterpret_cast<int64_t*>(d);
+  v.seg_start = d + 2 * (batch + 1);
+  v.row_start = v.seg_start + batch + 1;
+  v.len = v.row_start + batch + 1;
+  v.slot = v.len + batch;
+  return v;
+}
+
+// Query rows (of one kv head) one attention item takes.
+inline int step_row_tile(const ssd_kv8* c, const ssd_kv8_step* s) {
+  if (s->row_tile) return s->row_tile;
+  const int64_t r = static_cast<int64_t>((s->rows + s->batch - 1) / s->batch) * (c->n_heads / c->n_kv_heads);
+  return r <= 8 ? 8 : r <= 16 ? 16 : 32;
+}
+
+ssd_status kv8_check(const ssd_kv8* c, int layer);
+ssd_status kv8_check_step(const ssd_kv8* c, const ssd_kv8_step* s);
+
+}  // namespace ssd
