@@ -4,12 +4,27 @@
 
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace ssd {
 
 // Records the calling thread's message (a fixed buffer: nothing here throws) and returns `s`.
 ssd_status op_fail(ssd_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+// Raises a kernel's shared-memory limit, once per device (`ready`: a bit for each).
+template <typename K>
+ssd_status op_smem(K* kernel, int bytes, std::atomic<uint64_t>& ready, const char* what) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (e == cudaSuccess && ready.load(std::memory_order_relaxed) & bit) return SSD_OK;
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != cudaSuccess) return op_fail(SSD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+  ready.fetch_or(bit, std::memory_order_relaxed);
+  return SSD_OK;
+}
 // The status of a launch that has just been made.
 ssd_status op_launched(const char* what);
 
@@ -106,11 +121,11 @@ inline bool kv8_shape_ok(const ssd_kv8* c) {
     return false;
   if (c->n_heads < c->n_kv_heads || c->n_heads % c->n_kv_heads) return false;
   if (c->max_batch < 1 || c->max_batch > SSD_KV8_MAX_BATCH || c->max_blocks < 1) return false;
-  // slots, row numbers and the attention's tile numbers fit 31 bits
-  const int64_t lim = 0x7fffffff;
+  // slots, row numbers and positions fit 31 bits, with room to add a tile
+  const int64_t lim = 1 << 30;
   const int64_t cap = static_cast<int64_t>(c->max_blocks) * c->block_tokens;
   if (static_cast<int64_t>(c->n_blocks) * c->block_tokens > lim || cap > lim || c->n_heads > 65535) return false;
-  return cap * c->max_batch <= lim;
+  return cap * c->max_batch <= 0x7fffffff;
 }
 
 }  // namespace ssd
