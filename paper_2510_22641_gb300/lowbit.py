@@ -191,6 +191,7 @@ class W4Weight:
         size = self.lib.ssd_w4_bytes(self.n, self.k, group)
         if size < 0:
             _fail(self.lib.ssd_op_last_error().decode())
+        self._work = self.lib.ssd_w4_work_bytes(self.n, self.k)
         self.packed = torch.empty(size, dtype=torch.uint8, device=weight.device)
         _call(self.lib.ssd_w4_pack, weight.data_ptr(), _type(weight, "weight"), self.n, self.k, weight.stride(0),
               group, self.packed.data_ptr(), _stream(self.device))
@@ -220,9 +221,8 @@ class W4Weight:
             _fail(f"x: on {x.device}, the weight is on {self.device}")
         stream = _stream(self.device)
         work = _w4_work.get((self.device, stream))
-        if work is None:
-            work = _w4_work[(self.device, stream)] = torch.zeros(
-                self.lib.ssd_w4_work_bytes(self.n, self.k), dtype=torch.uint8, device=self.device)
+        if work is None or work.numel() < self._work:
+            work = _w4_work[(self.device, stream)] = torch.zeros(self._work, dtype=torch.uint8, device=self.device)
         _call(self.lib.ssd_w4_matmul, self.packed.data_ptr(), self.n, self.k, self.group, x.data_ptr(), _type(x, "x"),
               rows, x.stride(0), out.data_ptr(), out.stride(0), None if residual is None else residual.data_ptr(),
               0 if residual is None else residual.stride(0), work.data_ptr(), stream)
