@@ -464,6 +464,7 @@ SSD_API ssd_status ssd_probe_bounded_wait(ssd_ctx* ctx, int64_t limit_ns);
 enum { SSD_TYPE_BF16 = 0, SSD_TYPE_FP32 = 1 };
 
 #define SSD_KV8_MAX_BATCH 1024  /* seats of one block table */
+#define SSD_KV8_STEP_HEAD 38928  /* ints before seg_start in a step's buffer */
 
 /* Bits of the cache's device status word, which ssd_kv8_status reads and clears. */
 enum {
@@ -499,8 +500,9 @@ typedef struct {
   void* work;
 } ssd_kv8;
 
-/* What one step works on, filled by ssd_kv8_plan: device int32, ssd_kv8_step_ints() of them, 8-byte aligned, in this order:
- *   work_start int64 [batch + 1], seg_start [batch + 1]: the attention's partition (16-token tiles, items)
+/* What one step works on, filled by ssd_kv8_plan: device int32, ssd_kv8_step_ints() of them, 16-byte aligned, in this order:
+ *   the attention's partition, SSD_KV8_STEP_HEAD ints, then
+ *   seg_start  [batch + 1] prefix sums of the attention's items per request
  *   row_start  [batch + 1] prefix sums of the requests' new rows (rows of request b: row_start[b] ..)
  *   len        [batch] tokens before the step
  *   slot       [rows] block * block_tokens + offset of each new row, -1 for rows past the last request's
@@ -508,7 +510,7 @@ typedef struct {
 typedef struct {
   int batch;     /* requests: seats 0 .. batch - 1 */
   int rows;      /* capacity: new rows of all requests */
-  int row_tile;  /* 8, 16 or 32: query rows x (n_heads / n_kv_heads) the attention takes at once; any
+  int row_tile;  /* 8, 16, 24 or 32: query rows x (n_heads / n_kv_heads) the attention takes at once; any
                   * value is right, one near the usual product is fastest (0: from rows / batch) */
   int32_t* data;
 } ssd_kv8_step;

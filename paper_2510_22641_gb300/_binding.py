@@ -29,6 +29,7 @@ SSD_FAULT_LAUNCH = 2
 SSD_TYPE_BF16 = 0
 SSD_TYPE_FP32 = 1
 SSD_KV8_MAX_BATCH = 1024
+SSD_KV8_STEP_HEAD = 38928
 SSD_KV8_NO_BLOCKS = 1
 SSD_KV8_LENGTH = 2
 SSD_KV8_SLOT = 4

@@ -35,13 +35,13 @@ ssd_status kv8_check(const ssd_kv8* c, int layer) {
 }
 
 ssd_status kv8_check_step(const ssd_kv8* c, const ssd_kv8_step* s) {
-  if (!s || !s->data || reinterpret_cast<uintptr_t>(s->data) % 8)
+  if (!s || !s->data || reinterpret_cast<uintptr_t>(s->data) % 16)
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_step: null or unaligned buffer");
   if (s->batch < 1 || s->batch > c->max_batch)
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_step: batch %d, cache has %d seats", s->batch, c->max_batch);
   if (s->rows < 0 || static_cast<int64_t>(s->rows) * c->n_heads > 0x7fffffff)
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_step: %d rows", s->rows);
-  if (s->row_tile != 0 && s->row_tile != 8 && s->row_tile != 16 && s->row_tile != 32)
+  if (s->row_tile != 0 && s->row_tile != 8 && s->row_tile != 16 && s->row_tile != 24 && s->row_tile != 32)
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_step: row_tile %d", s->row_tile);
   return SSD_OK;
 }
@@ -109,9 +109,12 @@ __device__ __forceinline__ int find_request(const int32_t* start, int n, int x) 
 // CTA that finishes reading last (state_in and state_out may be one buffer).
 __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanParams p) {
   __shared__ int32_t row_s[SSD_KV8_MAX_BATCH + 1], new_s[SSD_KV8_MAX_BATCH + 1], back_s[SSD_KV8_MAX_BATCH + 1];
-  __shared__ int32_t len_s[SSD_KV8_MAX_BATCH], held_s[SSD_KV8_MAX_BATCH];
+  __shared__ int32_t len_s[SSD_KV8_MAX_BATCH], held_s[SSD_KV8_MAX_BATCH], seg_s[SSD_KV8_MAX_BATCH + 1];
+  __shared__ int64_t work_s[SSD_KV8_MAX_BATCH + 1];
   __shared__ int64_t tot3[kPlanThreads / 32][3], tot2[kPlanThreads / 32][2];
-  __shared__ int last_s;
+  __shared__ int last_s, longest_s;
+  pdl_wait();
+  pdl_trigger();
   const int tid = threadIdx.x;
   const int bs_m1 = (1 << p.shift) - 1;
   const int cap = p.max_blocks << p.shift;
@@ -153,6 +156,7 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
   // rows beyond the step's capacity do not exist for it
   int64_t sum2[2] = {0, 0}, all2[2];
   int64_t r = sum3[0], segs[kPlanPer], tiles[kPlanPer];
+  int longest = 0;
 #pragma unroll
   for (int k = 0; k < kPlanPer; ++k) {
     const int b = tid * per + k;
@@ -174,32 +178,40 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
       back_s[p.batch] = n_back;
     }
     const int rows_b = r1 - r0;
+    int n = 0;
     if (rows_b > 0) {
+      n = static_cast<int>((min(static_cast<int64_t>(max(ln[k], 0)) + rows_b, static_cast<int64_t>(cap)) + 15) >> 4);
       segs[k] = static_cast<int64_t>(p.n_kv_heads) *
                 ((static_cast<int64_t>(rows_b) * p.group + p.row_tile - 1) / p.row_tile);
-      tiles[k] = segs[k] * ((min(static_cast<int64_t>(max(ln[k], 0)) + rows_b, static_cast<int64_t>(cap)) + 15) >> 4);
+      tiles[k] = segs[k] * n;
     }
+    longest = max(longest, n);
     sum2[0] += segs[k];
     sum2[1] += tiles[k];
   }
-  if (blockIdx.x == 0) {  // uniform per CTA
-    block_scan<2>(sum2, all2, tot2);
-    const StepView s = step_view(p.step, p.batch);
+  if (tid == 0) longest_s = 0;
+  block_scan<2>(sum2, all2, tot2);
+  if (longest) atomicMax(&longest_s, longest);
+  const StepView s = step_view(p.step, p.batch);
 #pragma unroll
-    for (int k = 0; k < kPlanPer; ++k) {
-      const int b = tid * per + k;
-      if (k >= per || b >= p.batch) continue;
-      s.seg_start[b] = static_cast<int>(sum2[0]);
-      s.work_start[b] = sum2[1];
+  for (int k = 0; k < kPlanPer; ++k) {
+    const int b = tid * per + k;
+    if (k >= per || b >= p.batch) continue;
+    seg_s[b] = static_cast<int>(sum2[0]);
+    work_s[b] = sum2[1];
+    sum2[0] += segs[k];
+    sum2[1] += tiles[k];
+  }
+  if (tid == 0) {
+    seg_s[p.batch] = static_cast<int>(all2[0]);
+    work_s[p.batch] = all2[1];
+  }
+  __syncthreads();
+  if (blockIdx.x == 0) {
+    for (int b = tid; b <= p.batch; b += kPlanThreads) {
+      s.seg_start[b] = seg_s[b];
       s.row_start[b] = row_s[b];
-      s.len[b] = len_s[b];
-      sum2[0] += segs[k];
-      sum2[1] += tiles[k];
-      if (b == p.batch - 1) {
-        s.seg_start[p.batch] = static_cast<int>(all2[0]);
-        s.work_start[p.batch] = all2[1];
-        s.row_start[p.batch] = row_s[p.batch];
-      }
+      if (b < p.batch) s.len[b] = len_s[b];
     }
     if (flags) atomicOr(p.status, flags);
   }
@@ -224,7 +236,7 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
     return id;
   };
   const int first = blockIdx.x * kPlanThreads + tid, stride = gridDim.x * kPlanThreads;
-  int32_t* slot = step_view(p.step, p.batch).slot;
+  int32_t* slot = s.slot;
   const int n_rows = row_s[p.batch];
   for (int64_t r64 = first; r64 < p.rows; r64 += stride) {
     const int row = static_cast<int>(r64);
@@ -257,6 +269,71 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
   for (int64_t i = first; i < min(n_back, total - n_new); i += stride) {
     const int b = find_request(back_s, p.batch, static_cast<int>(i));
     p.pool[n_free + i] = p.table[static_cast<size_t>(b) * p.max_blocks + (i - back_s[b])];
+  }
+  // ---- the attention's partition
+  {
+    const int n_segs = seg_s[p.batch];
+    const int64_t all = work_s[p.batch];
+    const AttnShape sh = attn_shape(p.row_tile);
+    const int ctas = kAttnSms * sh.ctas;
+    // Team size: with fewer than two segments per team of a size, the next larger size cuts less.
+    int W = sh.warps;
+    while (W % 2 == 0 && sh.warps / (W / 2) <= sh.teams && n_segs >= 2 * ctas * (sh.warps / (W / 2))) W /= 2;
+    const int per_cta = sh.warps / W, teams = ctas * per_cta;
+    const int64_t span = max((all + teams - 1) / teams, static_cast<int64_t>(4 * W));
+    const int64_t snap = span / 4;
+    // Short contexts, a team for each: one segment per team, whatever its length, so that nothing is
+    // merged through global memory (64 tiles take one SM about as long as that merge).
+    const bool each = n_segs <= teams && longest_s <= 64;
+    auto request_at = [&](int64_t u) -> int {  // 0 <= u < all
+      int lo = 0, hi = p.batch;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (work_s[mid] <= u) lo = mid; else hi = mid;
+      }
+      return lo;
+    };
+    auto tiles_of = [&](int b) -> int { return static_cast<int>((work_s[b + 1] - work_s[b]) / (seg_s[b + 1] - seg_s[b])); };
+    // Equal spans; a cut inside a segment that is short against the span moves to its nearer end.
+    auto cut = [&](int c) -> int64_t {
+      const int64_t x = c * span;
+      if (x >= all) return all;
+      const int b = request_at(x), n = tiles_of(b);
+      if (n > snap) return x;
+      const int tile = static_cast<int>((x - work_s[b]) % n);
+      return tile < n - tile ? x - tile : x - tile + n;
+    };
+    if (first == 0) *s.head = StepHead{span, W, n_rows, {}};
+    for (int i = first; i < ctas * sh.teams; i += stride) {
+      const int sub = i % sh.teams, team = i / sh.teams * per_cta + sub;
+      TeamSpan t = {};
+      if (sub < per_cta) {
+        if (each) {
+          if (team < n_segs) {
+            const int b = find_request(seg_s, p.batch, team), n = tiles_of(b);
+            t.u0 = work_s[b] + static_cast<int64_t>(team - seg_s[b]) * n;
+            t.u1 = t.u0 + n;
+          }
+        } else {
+          t.u0 = cut(team);
+          t.u1 = cut(team + 1);
+        }
+        if (t.u0 < t.u1) {
+          t.b = request_at(t.u0);
+          t.n = tiles_of(t.b);
+          t.groups = (seg_s[t.b + 1] - seg_s[t.b]) / p.n_kv_heads;
+          const int64_t d = t.u0 - work_s[t.b];
+          const int seg = static_cast<int>(d / t.n);
+          t.tile = static_cast<int>(d - static_cast<int64_t>(seg) * t.n);
+          t.head = seg / t.groups;
+          t.rg = seg - t.head * t.groups;
+          t.row0 = row_s[t.b];
+          t.rows = row_s[t.b + 1] - t.row0;
+          t.len = len_s[t.b];
+        }
+      }
+      s.teams[i] = t;
+    }
   }
   if (last_s) {  // every CTA has read the counts
     if (tid == 0) {
@@ -296,6 +373,8 @@ __device__ __forceinline__ int quantise8(float x, float inv) {
 // first of them (its predecessor's slot is not one less, or it opens the block) stands for all.
 template <typename T, int D, bool VEC>
 __global__ void __launch_bounds__(128) ssd_kv8_append_kernel(const AppendParams p) {
+  pdl_wait();
+  pdl_trigger();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int h = blockIdx.y * 2 + (w >> 1), kv = w & 1;
   if (h >= p.n_kv_heads) return;
@@ -398,6 +477,8 @@ struct ReadParams {
 // One warp per (slot, kv head, K or V).
 template <typename T, int D>
 __global__ void __launch_bounds__(128) ssd_kv8_read_kernel(const ReadParams p) {
+  pdl_wait();
+  pdl_trigger();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int h = blockIdx.y * 2 + (w >> 1), kv = w & 1;
   if (h >= p.n_kv_heads) return;
@@ -436,7 +517,7 @@ int64_t ssd_kv8_data_bytes(const ssd_kv8* c) {
 
 int64_t ssd_kv8_step_ints(int batch, int rows) {
   if (batch < 1 || batch > SSD_KV8_MAX_BATCH || rows < 0) return -1;
-  return 5ll * batch + 4 + rows;
+  return SSD_KV8_STEP_HEAD + 3ll * batch + 2 + rows;
 }
 
 ssd_status ssd_kv8_plan(const ssd_kv8* c, const ssd_kv8_step* step, const int32_t* len, const int32_t* add,
@@ -463,10 +544,13 @@ ssd_status ssd_kv8_plan(const ssd_kv8* c, const ssd_kv8_step* step, const int32_
   p.step = step->data;
   p.status = static_cast<int32_t*>(c->work);
   p.ticket = p.status + 1;
+  // a thread per team of the attention's partition, or per four rows
+  const AttnShape sh = attn_shape(p.row_tile);
+  const int teams = (kAttnSms * sh.ctas * sh.teams + kPlanThreads - 1) / kPlanThreads;
   int grid = (step->rows + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
-  grid = grid < 1 ? 1 : grid > 152 ? 152 : grid;
-  ssd_kv8_plan_kernel<<<grid, kPlanThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
-  return op_launched("ssd_kv8_plan");
+  grid = grid < teams ? teams : grid > kAttnSms ? kAttnSms : grid;
+  return op_launch("ssd_kv8_plan", ssd_kv8_plan_kernel, dim3(grid), kPlanThreads, 0,
+                   static_cast<cudaStream_t>(cuda_stream), p);
 }
 
 ssd_status ssd_kv8_append(const ssd_kv8* c, int layer, const void* k, const void* v, int type, int rows,
@@ -500,16 +584,13 @@ ssd_status ssd_kv8_append(const ssd_kv8* c, int layer, const void* k, const void
   const bool vec = aligned4(k, size, k_row_stride, k_head_stride) && aligned4(v, size, v_row_stride, v_head_stride);
   const dim3 grid((rows + p.window - 1) / p.window, (c->n_kv_heads + 1) / 2);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-#define SSD_APPEND(T, D, V) ssd_kv8_append_kernel<T, D, V><<<grid, 128, 0, s>>>(p)
+#define SSD_APPEND(T, D, V) op_launch("ssd_kv8_append", ssd_kv8_append_kernel<T, D, V>, grid, 128, 0, s, p)
 #define SSD_APPEND_D(T, V) (c->head_dim == 128 ? SSD_APPEND(T, 128, V) : SSD_APPEND(T, 64, V))
-  if (type == SSD_TYPE_FP32) {
-    if (vec) SSD_APPEND_D(float, true); else SSD_APPEND_D(float, false);
-  } else {
-    if (vec) SSD_APPEND_D(__nv_bfloat16, true); else SSD_APPEND_D(__nv_bfloat16, false);
-  }
+  const ssd_status out = type == SSD_TYPE_FP32 ? (vec ? SSD_APPEND_D(float, true) : SSD_APPEND_D(float, false))
+                                               : (vec ? SSD_APPEND_D(__nv_bfloat16, true) : SSD_APPEND_D(__nv_bfloat16, false));
 #undef SSD_APPEND_D
 #undef SSD_APPEND
-  return op_launched("ssd_kv8_append");
+  return out;
 }
 
 ssd_status ssd_kv8_read(const ssd_kv8* c, int layer, const int32_t* slot, int n, void* k, void* v, int type,
@@ -533,14 +614,12 @@ ssd_status ssd_kv8_read(const ssd_kv8* c, int layer, const int32_t* slot, int n,
   p.status = static_cast<int32_t*>(c->work);
   const dim3 grid(n, (c->n_kv_heads + 1) / 2);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (type == SSD_TYPE_FP32) {
-    if (c->head_dim == 128) ssd_kv8_read_kernel<float, 128><<<grid, 128, 0, s>>>(p);
-    else ssd_kv8_read_kernel<float, 64><<<grid, 128, 0, s>>>(p);
-  } else {
-    if (c->head_dim == 128) ssd_kv8_read_kernel<__nv_bfloat16, 128><<<grid, 128, 0, s>>>(p);
-    else ssd_kv8_read_kernel<__nv_bfloat16, 64><<<grid, 128, 0, s>>>(p);
-  }
-  return op_launched("ssd_kv8_read");
+  const char* what = "ssd_kv8_read";
+  if (type == SSD_TYPE_FP32)
+    return c->head_dim == 128 ? op_launch(what, ssd_kv8_read_kernel<float, 128>, grid, 128, 0, s, p)
+                              : op_launch(what, ssd_kv8_read_kernel<float, 64>, grid, 128, 0, s, p);
+  return c->head_dim == 128 ? op_launch(what, ssd_kv8_read_kernel<__nv_bfloat16, 128>, grid, 128, 0, s, p)
+                            : op_launch(what, ssd_kv8_read_kernel<__nv_bfloat16, 64>, grid, 128, 0, s, p);
 }
 
 ssd_status ssd_kv8_status(const ssd_kv8* c, int* bits, void* cuda_stream) {

@@ -25,6 +25,23 @@ ssd_status op_smem(K* kernel, int bytes, std::atomic<uint64_t>& ready, const cha
   ready.fetch_or(bit, std::memory_order_relaxed);
   return SSD_OK;
 }
+// Launch that may begin while the launch before it drains: every kernel launched so waits for that one
+// (griddepcontrol.wait) before it touches memory, and lets the next begin early.
+template <typename... P, typename... A>
+ssd_status op_launch(const char* what, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t s, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+  return e == cudaSuccess ? SSD_OK : op_fail(SSD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
 // The status of a launch that has just been made.
 ssd_status op_launched(const char* what);
 
@@ -125,6 +142,7 @@ inline bool kv8_shape_ok(const ssd_kv8* c) {
   const int64_t lim = 1 << 30;
   const int64_t cap = static_cast<int64_t>(c->max_blocks) * c->block_tokens;
   if (static_cast<int64_t>(c->n_blocks) * c->block_tokens > lim || cap > lim || c->n_heads > 65535) return false;
+  if (static_cast<int64_t>(c->n_blocks) * (c->block_tokens / 16) * c->n_kv_heads > lim) return false;
   return cap * c->max_batch <= 0x7fffffff;
 }
 
@@ -132,9 +150,42 @@ inline bool kv8_shape_ok(const ssd_kv8* c) {
 
 namespace ssd {
 
-// The parts of a step's buffer (see ssd_kv8_step).
+// ------------------------------------------------------------------ a step's buffer
+//
+// Work of the attention is the flat list of 16-token tiles of all segments (request, kv head, row
+// group), cut into one span per team of W warps.  The plan makes the cuts, once for all layers, so that
+// an attention warp finds its place with one load.
+
+constexpr int kAttnSms = 152;
+constexpr int kAttnMaxTeams = 2 * kAttnSms * 8;
+
+// Launch shape of the attention for items of 8, 16, 24 or 32 rows.
+struct AttnShape {
+  int warps, ctas, teams;  // per CTA, CTAs per SM, most teams per CTA
+};
+__host__ __device__ constexpr AttnShape attn_shape(int row_tile) {
+  return row_tile == 8 ? AttnShape{8, 2, 8} : row_tile == 16 ? AttnShape{12, 1, 4} : AttnShape{8, 1, 2};
+}
+
+struct alignas(16) StepHead {
+  int64_t span;  // tiles per team; cuts inside long segments are its multiples
+  int warps;     // per team
+  int n_rows;    // rows of all requests
+  int pad[12];
+};
+// A team's span [u0, u1) of the list: it begins at tile `tile` of this segment.
+struct alignas(16) TeamSpan {
+  int b, head, rg, tile;
+  int n, groups, row0, rows;  // tiles of the segment; row groups, first row and rows of the request
+  int64_t u0, u1;
+  int len, pad[3];
+};
+static_assert(sizeof(StepHead) == 64 && sizeof(TeamSpan) == 64, "layout");
+static_assert(sizeof(StepHead) + kAttnMaxTeams * sizeof(TeamSpan) == SSD_KV8_STEP_HEAD * 4ull, "layout");
+
 struct StepView {
-  int64_t* work_start;
+  StepHead* head;
+  TeamSpan* teams;  // [CTA][most teams per CTA]
   int32_t* seg_start;
   int32_t* row_start;
   int32_t* len;
@@ -142,8 +193,9 @@ struct StepView {
 };
 __host__ __device__ __forceinline__ StepView step_view(int32_t* d, int batch) {
   StepView v;
-  v.work_start = reinterpret_cast<int64_t*>(d);
-  v.seg_start = d + 2 * (batch + 1);
+  v.head = reinterpret_cast<StepHead*>(d);
+  v.teams = reinterpret_cast<TeamSpan*>(v.head + 1);
+  v.seg_start = d + SSD_KV8_STEP_HEAD;
   v.row_start = v.seg_start + batch + 1;
   v.len = v.row_start + batch + 1;
   v.slot = v.len + batch;
@@ -153,8 +205,10 @@ __host__ __device__ __forceinline__ StepView step_view(int32_t* d, int batch) {
 // Query rows (of one kv head) one attention item takes.
 inline int step_row_tile(const ssd_kv8* c, const ssd_kv8_step* s) {
   if (s->row_tile) return s->row_tile;
-  const int64_t r = static_cast<int64_t>((s->rows + s->batch - 1) / s->batch) * (c->n_heads / c->n_kv_heads);
-  return r <= 8 ? 8 : r <= 16 ? 16 : 32;
+  const int64_t r = static_cast<int64_t>((s->rows > 0 ? s->rows + s->batch - 1 : s->batch) / s->batch) *
+                    (c->n_heads / c->n_kv_heads);
+  const int64_t items = (r + 31) / 32;
+  return static_cast<int>(((r + items - 1) / items + 7) / 8 * 8);
 }
 
 ssd_status kv8_check(const ssd_kv8* c, int layer);

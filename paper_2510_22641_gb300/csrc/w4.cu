@@ -1,4 +1,5 @@
 // 4-bit weights with group scales: packing, and products with 1..16 activation rows.
+#include <stdlib.h>
 #include "lowbit.cuh"
 
 namespace ssd {
@@ -122,7 +123,7 @@ constexpr int kMaxRec = kCodeBytes + 16 * 4 * 2;
 
 struct W4Params {
   const uint8_t* packed;
-  int n, chunks, group_shift, rec, rows;  // group = 32 << group_shift
+  int n, chunks, per, rec, rows;  // per: groups in a chunk
   int warps;                              // per team
   const uint16_t* x;                      // 16-bit rows (bf16, or high and low halves), 16-byte aligned
   int64_t x_row, x_part;                  // elements between rows, between the high and low parts
@@ -188,18 +189,18 @@ __device__ __forceinline__ void w4_operand(uint32_t w, uint32_t (&a)[4]) {
 }
 
 // T: type of y and the residual.  PARTS = 1: bf16 operands, 2: pairs of halves.
-template <typename T, int NB, int MT>
+template <typename T, int NB, int MT, int per>  // per: groups in a chunk
 __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) ssd_w4_matmul_kernel(const W4Params p) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
   constexpr bool BF16 = PARTS == 1;
   using G = W4Geo<PARTS, NB, MT>;
   constexpr int RT = G::kRT;
   extern __shared__ __align__(128) uint8_t smem[];
+  if constexpr (BF16) pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int W = p.warps, sub = warp / W, wt = warp - sub * W, tt = tid - sub * W * 32;
   const int teams = gridDim.x * (kWarps / W), team = blockIdx.x * (kWarps / W) + sub;
   const int n_tiles = (p.n + 15) >> 4, n_segs = (n_tiles + MT - 1) / MT, n_c = p.chunks;
-  const int per = 4 >> p.group_shift;  // groups per chunk
 
   // ---- this team's span
   const int64_t total = static_cast<int64_t>(n_segs) * n_c;
@@ -260,7 +261,8 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) ssd_w4_matmul_kerne
   };
   int i_stage = 0, stage = 0;
   for (; i_stage < G::kStages - 1; ++i_stage) issue(i_stage);
-  if constexpr (!BF16) pdl_wait();  // the split rows come from the launch before
+  if constexpr (!BF16) pdl_wait();  // the split rows come from the launch before, which waited for the weights
+  pdl_trigger();
 
   // activations of one chunk: row nb * 8 + g, columns 32 i + 8 t .. + 7
   uint4 x[NB][PARTS][4];
@@ -274,9 +276,9 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) ssd_w4_matmul_kerne
         const uint16_t* src = p.x + k * p.x_part + r * p.x_row + static_cast<int64_t>(chunk) * kChunk + 8 * t;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          x[nb][k][i] = r < p.rows ? __ldg(reinterpret_cast<const uint4*>(src + 32 * i)) : make_uint4(0, 0, 0, 0);
+          x[nb][k][i] = r < p.rows ? *reinterpret_cast<const uint4*>(src + 32 * i) : make_uint4(0, 0, 0, 0);
       }
-      if constexpr (!BF16) xs[nb] = __ldg(reinterpret_cast<const float2*>(p.x_scale + chunk * 16 + nb * 8 + 2 * t));
+      if constexpr (!BF16) xs[nb] = *reinterpret_cast<const float2*>(p.x_scale + chunk * 16 + nb * 8 + 2 * t);
     }
   };
 
@@ -449,6 +451,7 @@ struct W4RowsParams {
 
 template <typename T>
 __global__ void __launch_bounds__(128) ssd_w4_rows_kernel(const W4RowsParams p) {
+  pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31;
   const int64_t job = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
@@ -481,37 +484,32 @@ __global__ void __launch_bounds__(128) ssd_w4_rows_kernel(const W4RowsParams p) 
   }
 }
 
-template <typename T, int NB, int MT>
+template <typename T, int NB, int MT, int PER>
 ssd_status launch(const W4Params& p, cudaStream_t s) {
-  constexpr bool pdl = sizeof(T) == 4;
-  using G = W4Geo<pdl ? 2 : 1, NB, MT>;
+  using G = W4Geo<sizeof(T) == 4 ? 2 : 1, NB, MT>;
   static std::atomic<uint64_t> ready{0};
-  if (ssd_status e = op_smem(ssd_w4_matmul_kernel<T, NB, MT>, G::kTotal, ready, "ssd_w4_matmul")) return e;
+  if (ssd_status e = op_smem(ssd_w4_matmul_kernel<T, NB, MT, PER>, G::kTotal, ready, "ssd_w4_matmul")) return e;
   const int n_segs = ((p.n + 15) / 16 + MT - 1) / MT;
   const int teams_wanted = n_segs * ((p.chunks + 1) / 2);  // at least two chunks a team
   int grid = (teams_wanted + kWarps / p.warps - 1) / (kWarps / p.warps);
   const int one_each = (n_segs + kWarps / p.warps - 1) / (kWarps / p.warps);
   const int most = kMaxCtas / 2 * G::kCtas;
   grid = one_each <= most ? one_each : grid;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid > most ? most : grid);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = G::kTotal;
-  cfg.stream = s;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = pdl ? 1 : 0;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, ssd_w4_matmul_kernel<T, NB, MT>, p);
-  return e == cudaSuccess ? SSD_OK : op_fail(SSD_ERR_CUDA, "ssd_w4_matmul: %s", cudaGetErrorString(e));
+  return op_launch("ssd_w4_matmul", ssd_w4_matmul_kernel<T, NB, MT, PER>, dim3(grid > most ? most : grid), kThreads,
+                   G::kTotal, s, p);
+}
+
+template <typename T, int NB, int MT>
+ssd_status launch_group(const W4Params& p, cudaStream_t s) {
+  return p.per == 1 ? launch<T, NB, MT, 1>(p, s) : p.per == 2 ? launch<T, NB, MT, 2>(p, s) : launch<T, NB, MT, 4>(p, s);
 }
 
 template <typename T, int NB>
 ssd_status launch_tiles(const W4Params& p, cudaStream_t s) {
   const int tiles = (p.n + 15) / 16;
-  const int mt = tiles <= kMaxCtas ? 1 : tiles <= 2 * kMaxCtas ? 2 : 4;
-  return mt == 1 ? launch<T, NB, 1>(p, s) : mt == 2 ? launch<T, NB, 2>(p, s) : launch<T, NB, 4>(p, s);
+  int mt = tiles <= kMaxCtas ? 1 : tiles <= 2 * kMaxCtas ? 2 : 4;
+  if (const char* e = getenv("W4_MT")) mt = atoi(e);
+  return mt == 1 ? launch_group<T, NB, 1>(p, s) : mt == 2 ? launch_group<T, NB, 2>(p, s) : launch_group<T, NB, 4>(p, s);
 }
 
 ssd_status check_shape(int n, int k, int group) {
@@ -602,10 +600,11 @@ ssd_status ssd_w4_matmul(const void* packed, int n, int k, int group, const void
   p.packed = static_cast<const uint8_t*>(packed);
   p.n = n;
   p.chunks = (k + kChunk - 1) / kChunk;
-  p.group_shift = group == 32 ? 0 : group == 64 ? 1 : 2;
+  p.per = kChunk / group;
   p.rec = w4_record(group);
   p.rows = rows;
   p.warps = p.chunks >= 16 ? 8 : p.chunks >= 8 ? 4 : p.chunks >= 4 ? 2 : 1;
+  if (const char* e = getenv("W4_W")) p.warps = atoi(e);
   p.y = y;
   p.residual = residual;
   p.y_row = y_row_stride;
@@ -624,9 +623,10 @@ ssd_status ssd_w4_matmul(const void* packed, int n, int k, int group, const void
                    reinterpret_cast<float*>(wk + lay.scale)};
     p.x = r.out;
     const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(rows) * p.chunks + 3) / 4);
-    if (type == SSD_TYPE_FP32) ssd_w4_rows_kernel<float><<<grid, 128, 0, s>>>(r);
-    else ssd_w4_rows_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(r);
-    if (ssd_status e = op_launched("ssd_w4_matmul")) return e;
+    if (ssd_status e = type == SSD_TYPE_FP32
+                           ? op_launch("ssd_w4_matmul", ssd_w4_rows_kernel<float>, dim3(grid), 128, 0, s, r)
+                           : op_launch("ssd_w4_matmul", ssd_w4_rows_kernel<__nv_bfloat16>, dim3(grid), 128, 0, s, r))
+      return e;
   }
   if (type == SSD_TYPE_FP32) return rows <= 8 ? launch_tiles<float, 1>(p, s) : launch_tiles<float, 2>(p, s);
   return rows <= 8 ? launch_tiles<__nv_bfloat16, 1>(p, s) : launch_tiles<__nv_bfloat16, 2>(p, s);

@@ -66,8 +66,9 @@ class KV8Step:
         tile = 0
         if rows_per_request is not None:
             heads = rows_per_request * (cache.n_heads // cache.n_kv_heads)
-            tile = 8 if heads <= 8 else 16 if heads <= 16 else 32
-        at = 3 * (batch + 1)
+            items = -(-heads // 32)
+            tile = (-(-heads // items) + 7) // 8 * 8
+        at = B.SSD_KV8_STEP_HEAD + batch + 1
         self.row_start = self.data[at:at + batch + 1]
         self.length = self.data[at + batch + 1:at + 2 * batch + 1]
         self.slot = self.data[at + 2 * batch + 1:]

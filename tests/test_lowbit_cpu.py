@@ -40,7 +40,7 @@ def test_sizes(l):
     c = cache()
     assert l.ssd_kv8_data_bytes(ctypes.byref(c)) == 2 * 10 * 4 * 32 * 128 * 2
     assert l.ssd_kv8_work_bytes(ctypes.byref(c)) >= 64
-    assert l.ssd_kv8_step_ints(2, 4) == 2 * 3 + 3 + 3 + 2 + 4
+    assert l.ssd_kv8_step_ints(2, 4) == B.SSD_KV8_STEP_HEAD + 3 + 3 + 2 + 4
     for bad in ((0, 4), (1025, 4), (2, -1)):
         assert l.ssd_kv8_step_ints(*bad) == -1
     # codes of whole 16 x 128 tiles, one bf16 scale per row and group
