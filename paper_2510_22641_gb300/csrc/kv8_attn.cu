@@ -34,13 +34,14 @@ struct Kv8AttnParams {
   const uint32_t* row_mask;
   int32_t* step;
   int batch, rows, group, n_heads, n_kv_heads, shift, n_blocks, max_blocks;
-  int q_vec, o_vec;  // rows can be read / written 4 elements at a time
+  int q_vec;           // q rows can be read 4 elements at a time
+  unsigned group_inv;  // ceil(2^32 / group): high half of R * group_inv = R / group for R < 2^32 / group
   float scale_log2;
   const uint8_t* data;
   const float* scales;
   const int32_t* table;
   unsigned* tickets;  // [kAttnMaxTeams], zero between launches
-  float* part;        // [2 * teams][8 NB][D], then [2 * teams][8 NB][2] (maximum, sum)
+  float* part;        // [2 * teams][8 NB][D] states, then [2 * teams][8 NB][2] (maximum, sum)
 };
 
 // Launch shape by rows per item.  Up to 8 rows: query fragments in registers, 128 registers a thread, 16
@@ -57,15 +58,15 @@ struct Geo {
   static constexpr int kTile = 32 * D;                      // bytes of 16 tokens, K and V: one step
   static constexpr int kRing = NB >= 3 ? 20480 : 12288;     // per warp
   static constexpr int kStages = kRing / kTile;
-  static constexpr int kStat = kWarps * kRing;              // (maximum, sum) of 8 rows per warp
-  static constexpr int kOff = kStat + kWarps * 8 * 8;       // where each warp's merge record lies
+  static constexpr int kStat = kWarps * kRing;              // (maximum, sum, unit) of 8 rows per warp
+  static constexpr int kOff = kStat + kWarps * 8 * 16;      // where each warp's merge record lies
   static constexpr int kFlag = kOff + kWarps * 4;
   static constexpr int kScale = (kFlag + kWarps * 4 + 15) / 16 * 16;
   static constexpr int kQ = kScale + kWarps * kStages * 8;
   static constexpr int kQTeam = kSharedQ ? 2 * (D / 16) * NB * 32 * 8 + 8 * NB * 4 : 0;  // fragments, row factors
   static constexpr int kTotal = kQ + kTeams * kQTeam;
   static_assert(kScale % 16 == 0 && kQ % 16 == 0 && kQTeam % 16 == 0, "alignment");
-  static_assert(kTile >= 8 * D * 4, "a merge record of 8 rows fits one stage");
+  static_assert(kTile >= 8 * D * 4, "a state of 8 rows fits one stage");
   static_assert(kTotal * kCtas <= 231424, "shared memory");
 };
 
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
   for (; i_stage < G::kStages - 1; ++i_stage) issue(i_stage);
   int stage = 0;
 
-  float2* stat_s = reinterpret_cast<float2*>(smem + G::kStat);
+  float4* stat_s = reinterpret_cast<float4*>(smem + G::kStat);
   volatile int* off_s = reinterpret_cast<volatile int*>(smem + G::kOff);
   volatile int* flag_s = reinterpret_cast<volatile int*>(smem + G::kFlag);
   uint2* q_s = reinterpret_cast<uint2*>(smem + G::kQ + sub * G::kQTeam);
@@ -250,7 +251,7 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
     // row r of the segment -> (step row of the request, query head of the kv head)
     auto row_of = [&](int r, int& i, int& hq) {
       const int R = rg * RT + r;
-      i = R / p.group;
+      i = p.group == 1 ? R : static_cast<int>(__umulhi(static_cast<unsigned>(R), p.group_inv));
       hq = head * p.group + R - i * p.group;
     };
 
@@ -473,101 +474,180 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
       }
     }
 
-    // ---- merge the team's warps, eight rows at a time
+    // ---- merge.  States stay in the accumulators' layout: a lane holds, for each 16-dimension tile, the
+    // dimensions g and g + 8 of its rows 2t and 2t + 1.
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int x = 4; x <= 16; x <<= 1) l[nb][e] += __shfl_xor_sync(~0u, l[nb][e], x);
     const bool whole = c_piece.a == 0 && c_piece.e == c_piece.n;
     const int slot = team * 2 + (c_piece.a == 0 ? 1 : 0);
-    float* part_o = p.part + static_cast<size_t>(slot) * RT * D;
-    float2* part_s = reinterpret_cast<float2*>(p.part + static_cast<size_t>(2) * gridDim.x * G::kTeams * RT * D) + slot * RT;
-    auto write_row = [&](int r, int d, const float4& v, float sum) {
-      if (r >= r_valid) return;
+    float4* part_o = reinterpret_cast<float4*>(p.part);                                          // [slot][NB][KS][lane]
+    float2* part_s = reinterpret_cast<float2*>(p.part + static_cast<size_t>(2) * gridDim.x * G::kTeams * RT * D);
+    // the rows 2t and 2t + 1 of block nb: where they go, or null
+    auto out_row = [&](int nb, int e) -> T* {
+      const int r = nb * 8 + 2 * t + e;
+      if (r >= r_valid) return nullptr;
       int i, hq;
       row_of(r, i, hq);
-      T* dst = static_cast<T*>(p.o) + (row0 + i) * p.o_row + hq * p.o_head + d;
-      const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-      const T e[4] = {from_f32<T>(v.x * f), from_f32<T>(v.y * f), from_f32<T>(v.z * f), from_f32<T>(v.w * f)};
-      if (p.o_vec) {
-        if constexpr (PARTS == 2) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(e);
-        else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(e);
-      } else {
-        dst[0] = e[0], dst[1] = e[1], dst[2] = e[2], dst[3] = e[3];
+      return static_cast<T*>(p.o) + (row0 + i) * p.o_row + hq * p.o_head + g;
+    };
+    auto write = [&](T* d0, T* d1, int i, const float4& v, float f0, float f1) {
+      if (d0) {
+        d0[16 * i] = from_f32<T>(v.x * f0);
+        d0[16 * i + 8] = from_f32<T>(v.z * f0);
+      }
+      if (d1) {
+        d1[16 * i] = from_f32<T>(v.y * f1);
+        d1[16 * i + 8] = from_f32<T>(v.w * f1);
       }
     };
-    // The free stage of each warp's ring (the next to be filled, after the last barrier here) holds its
-    // record: 8 rows of D floats, 4-float pieces of row r at r ^ piece, against bank conflicts.
-    __syncwarp();  // every lane has read that stage
-    float* mine = reinterpret_cast<float*>(ring + i_stage * G::kTile);
-    if (lane == 0) off_s[warp] = i_stage * G::kTile;
+    auto over = [](float sum) -> float { return sum == 0.0f ? 0.0f : 1.0f / sum; };
+    if (W == 1) {
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float sum = l[nb][e];
-#pragma unroll
-        for (int x = 4; x <= 16; x <<= 1) sum += __shfl_xor_sync(~0u, sum, x);
-        const int r = 2 * t + e;
-        if (g == 0) stat_s[warp * 8 + r] = make_float2(m[nb][e], sum);
-        const float back = unit[nb][e] * 0x1p-7f;
-#pragma unroll
-        for (int i = 0; i < KS; ++i)
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int d = 16 * i + 8 * half + g;
-            mine[r * D + (d ^ (r << 2))] = o[nb][i][e + 2 * half] * back;
-          }
-      }
-      named_bar_sync(1 + sub, W * 32);
-      for (int x = tt; x < 8 * D / 4; x += W * 32) {
-        const int r = x / (D / 4), d = (x % (D / 4)) * 4;
-        float high = -3.402823466e38f;
-        for (int w = 0; w < W; ++w) high = fmaxf(high, stat_s[(sub * W + w) * 8 + r].x);
-        float sum = 0.0f;
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int w = 0; w < W; ++w) {
-          const float2 ms = stat_s[(sub * W + w) * 8 + r];
-          const float f = ex2(ms.x - high);
-          const float4 v = *reinterpret_cast<const float4*>(smem + (sub * W + w) * G::kRing + off_s[sub * W + w] +
-                                                            (r * D + (d ^ (r << 2))) * 4);
-          sum += ms.y * f;
-          acc.x += v.x * f, acc.y += v.y * f, acc.z += v.z * f, acc.w += v.w * f;
-        }
+      for (int nb = 0; nb < NB; ++nb) {
+        const float b0 = unit[nb][0] * 0x1p-7f, b1 = unit[nb][1] * 0x1p-7f;
         if (whole) {
-          write_row(nb * 8 + r, d, acc, sum);
+          T *d0 = out_row(nb, 0), *d1 = out_row(nb, 1);
+          const float f0 = b0 * over(l[nb][0]), f1 = b1 * over(l[nb][1]);
+#pragma unroll
+          for (int i = 0; i < KS; ++i) write(d0, d1, i, make_float4(o[nb][i][0], o[nb][i][1], o[nb][i][2], o[nb][i][3]), f0, f1);
         } else {
-          *reinterpret_cast<float4*>(part_o + (nb * 8 + r) * D + d) = acc;
-          if (d == 0) part_s[nb * 8 + r] = make_float2(high, sum);
+#pragma unroll
+          for (int i = 0; i < KS; ++i)
+            part_o[((static_cast<size_t>(slot) * NB + nb) * KS + i) * 32 + lane] =
+                make_float4(o[nb][i][0] * b0, o[nb][i][1] * b1, o[nb][i][2] * b0, o[nb][i][3] * b1);
+          if (g == 0)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) part_s[slot * RT + nb * 8 + 2 * t + e] = make_float2(m[nb][e], l[nb][e]);
         }
       }
-      named_bar_sync(1 + sub, W * 32);
+    } else {
+      // Through shared memory: the free stage of each warp's ring (the next to be filled, after the last
+      // barrier here) holds its state of eight rows; each warp merges some of the 16-dimension tiles.
+      __syncwarp();  // every lane has read that stage
+      float4* mine = reinterpret_cast<float4*>(ring + i_stage * G::kTile);
+      if (lane == 0) off_s[warp] = i_stage * G::kTile;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+        for (int i = 0; i < KS; ++i) mine[i * 32 + lane] = make_float4(o[nb][i][0], o[nb][i][1], o[nb][i][2], o[nb][i][3]);
+        if (g == 0)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            stat_s[warp * 8 + 2 * t + e] = make_float4(m[nb][e], l[nb][e], unit[nb][e] * 0x1p-7f, 0.0f);
+        named_bar_sync(1 + sub, W * 32);
+        if (wt < KS) {
+          const float4* stat = stat_s + sub * W * 8 + 2 * t;
+          float m0 = -3.402823466e38f, m1 = m0;
+#pragma unroll 2
+          for (int w = 0; w < W; ++w) {
+            m0 = fmaxf(m0, stat[w * 8].x);
+            m1 = fmaxf(m1, stat[w * 8 + 1].x);
+          }
+          T *d0 = nullptr, *d1 = nullptr;
+          if (whole) d0 = out_row(nb, 0), d1 = out_row(nb, 1);
+#pragma unroll 1
+          for (int i = wt; i < KS; i += W) {
+            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            float l0 = 0.0f, l1 = 0.0f;
+#pragma unroll 2
+            for (int w = 0; w < W; ++w) {
+              const float4 s0 = stat[w * 8], s1 = stat[w * 8 + 1];
+              const float4 v = reinterpret_cast<const float4*>(smem + (sub * W + w) * G::kRing + off_s[sub * W + w])[i * 32 + lane];
+              const float f0 = ex2(s0.x - m0), f1 = ex2(s1.x - m1);
+              l0 += s0.y * f0;
+              l1 += s1.y * f1;
+              const float b0 = f0 * s0.z, b1 = f1 * s1.z;
+              acc.x += v.x * b0, acc.y += v.y * b1, acc.z += v.z * b0, acc.w += v.w * b1;
+            }
+            if (whole) {
+              write(d0, d1, i, acc, over(l0), over(l1));
+            } else {
+              part_o[((static_cast<size_t>(slot) * NB + nb) * KS + i) * 32 + lane] = acc;
+              if (i == 0 && g == 0) {
+                part_s[slot * RT + nb * 8 + 2 * t] = make_float2(m0, l0);
+                part_s[slot * RT + nb * 8 + 2 * t + 1] = make_float2(m1, l1);
+              }
+            }
+          }
+        }
+        named_bar_sync(1 + sub, W * 32);
+      }
     }
     if (!whole) {
       // the teams that share the segment: those of the cuts inside it
       const int64_t s0 = c_piece.u - c_piece.a, s1 = s0 + c_piece.n;
       const int t0 = static_cast<int>(s0 / span), t1 = static_cast<int>((s1 - 1) / span);
+      __syncwarp();  // a team of one warp: its states are written
       if (tt == 0) flag_s[sub] = atom_add_acq_rel_gpu(p.tickets + t0, 1u) == static_cast<unsigned>(t1 - t0);
       named_bar_sync(1 + sub, W * 32);
-      if (flag_s[sub]) {
+      const bool last = flag_s[sub];
+      named_bar_sync(1 + sub, W * 32);
+      if (last) {
         if (tt == 0) p.tickets[t0] = 0;
-        const float2* all_s = reinterpret_cast<const float2*>(p.part + static_cast<size_t>(2) * gridDim.x * G::kTeams * RT * D);
-        for (int x = tt; x < RT * D / 4; x += W * 32) {
-          const int r = x / (D / 4), d = (x % (D / 4)) * 4;
-          if (r >= r_valid) break;
-          float high = -3.402823466e38f;
-          for (int c = t0; c <= t1; ++c) high = fmaxf(high, __ldcg(all_s + (2 * c + (c == t0)) * RT + r).x);
-          float sum = 0.0f;
-          float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-          for (int c = t0; c <= t1; ++c) {
-            const int from = 2 * c + (c == t0);
-            const float2 ms = __ldcg(all_s + from * RT + r);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + (static_cast<size_t>(from) * RT + r) * D + d));
-            const float f = ex2(ms.x - high);
-            sum += ms.y * f;
-            acc.x += v.x * f, acc.y += v.y * f, acc.z += v.z * f, acc.w += v.w * f;
+        auto slot_of = [&](int c) -> int { return 2 * c + (c == t0); };
+        // One pass in team order, each state rescaled to the larger maximum; several states' loads in flight.
+        auto stats = [&](int c, int nb) -> float4 {  // (m, l) of the rows 2t, 2t + 1
+          return __ldcg(reinterpret_cast<const float4*>(part_s + slot_of(c) * RT + nb * 8 + 2 * t));
+        };
+        auto state = [&](int c, int nb, int i) -> float4 {
+          return __ldcg(part_o + ((static_cast<size_t>(slot_of(c)) * NB + nb) * KS + i) * 32 + lane);
+        };
+        struct Sum {
+          float m0, m1, l0, l1, old0, old1, new0, new1;
+          __device__ __forceinline__ void begin() { m0 = m1 = -3.402823466e38f, l0 = l1 = 0.0f; }
+          __device__ __forceinline__ void add(const float4& z) {
+            const float a0 = fmaxf(m0, z.x), a1 = fmaxf(m1, z.z);
+            old0 = ex2(m0 - a0), old1 = ex2(m1 - a1), new0 = ex2(z.x - a0), new1 = ex2(z.z - a1);
+            l0 = l0 * old0 + z.y * new0;
+            l1 = l1 * old1 + z.w * new1;
+            m0 = a0, m1 = a1;
           }
-          write_row(r, d, acc, sum);
+          __device__ __forceinline__ void fold(float4& acc, const float4& v) const {
+            acc.x = acc.x * old0 + v.x * new0;
+            acc.y = acc.y * old1 + v.y * new1;
+            acc.z = acc.z * old0 + v.z * new0;
+            acc.w = acc.w * old1 + v.w * new1;
+          }
+        };
+        if (NB == 1 && W == 1) {
+          Sum z;
+          float4 acc[KS];
+          z.begin();
+#pragma unroll
+          for (int i = 0; i < KS; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
+          for (int c = t0; c <= t1; ++c) {
+            z.add(stats(c, 0));
+#pragma unroll
+            for (int i = 0; i < KS; ++i) z.fold(acc[i], state(c, 0, i));
+          }
+          T *d0 = out_row(0, 0), *d1 = out_row(0, 1);
+          const float f0 = over(z.l0), f1 = over(z.l1);
+#pragma unroll
+          for (int i = 0; i < KS; ++i) write(d0, d1, i, acc[i], f0, f1);
+        } else {
+#pragma unroll 1
+          for (int i = wt; i < KS; i += W) {
+            Sum z[NB];
+            float4 acc[NB];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) z[nb].begin(), acc[nb] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+            for (int c = t0; c <= t1; ++c)
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) {
+                z[nb].add(stats(c, nb));
+                z[nb].fold(acc[nb], state(c, nb, i));
+              }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) write(out_row(nb, 0), out_row(nb, 1), i, acc[nb], over(z[nb].l0), over(z[nb].l1));
+          }
         }
       }
-      named_bar_sync(1 + sub, W * 32);
     }
   }
   cp_async_wait_all();
@@ -613,6 +693,8 @@ ssd_status ssd_kv8_attention(const ssd_kv8* c, int layer, const ssd_kv8_step* st
   if (ssd_status s = kv8_check_step(c, step)) return s;
   if (type != SSD_TYPE_BF16 && type != SSD_TYPE_FP32) return op_fail(SSD_ERR_INVALID_ARG, "type %d", type);
   if (step->rows == 0) return SSD_OK;
+  const int64_t g = c->n_heads / c->n_kv_heads;
+  if (step->rows * g * g >= 1ll << 32) return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_attention: %d rows", step->rows);
   if (!q || !o) return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_attention: null buffer");
   const int size = type == SSD_TYPE_FP32 ? 4 : 2;
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(o)) % size)
@@ -629,13 +711,13 @@ ssd_status ssd_kv8_attention(const ssd_kv8* c, int layer, const ssd_kv8_step* st
   p.batch = step->batch;
   p.rows = step->rows;
   p.group = c->n_heads / c->n_kv_heads;
+  p.group_inv = static_cast<unsigned>((0xffffffffull + p.group) / p.group);
   p.n_heads = c->n_heads;
   p.n_kv_heads = c->n_kv_heads;
   p.shift = 31 - __builtin_clz(c->block_tokens);
   p.n_blocks = c->n_blocks;
   p.max_blocks = c->max_blocks;
   p.q_vec = aligned4(q, size, q_row_stride, q_head_stride);
-  p.o_vec = aligned4(o, size, o_row_stride, o_head_stride);
 
   p.scale_log2 = scale * 1.4426950408889634f;
   const size_t recs = static_cast<size_t>(layer) * c->n_blocks * c->n_kv_heads;
