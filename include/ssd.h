@@ -586,7 +586,7 @@ SSD_API ssd_status ssd_w4_unpack(const void* packed, int n, int k, int group, fl
 /* y = x W^T (+ residual), rows <= SSD_W4_MAX_ROWS, fp32 sums, each group's products scaled in fp32.
  *   x: device, type SSD_TYPE_*, [rows][x_row_stride];  y: same type, [rows][y_row_stride]
  *   residual: device [rows][res_row_stride] of the same type, or NULL; may be y itself
- *   work: device, ssd_w4_work_bytes(), zeroed once before the first call, 16-byte aligned
+ *   work: device, ssd_w4_work_bytes(), 16-byte aligned
  * y must not overlap x. */
 SSD_API int64_t ssd_w4_work_bytes(int n, int k);
 SSD_API ssd_status ssd_w4_matmul(const void* packed, int n, int k, int group, const void* x, int type, int rows,

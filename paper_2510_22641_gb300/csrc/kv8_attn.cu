@@ -61,7 +61,8 @@ struct Geo {
   static constexpr int kStat = kWarps * kRing;              // (maximum, sum, unit) of 8 rows per warp
   static constexpr int kOff = kStat + kWarps * 8 * 16;      // where each warp's merge record lies
   static constexpr int kFlag = kOff + kWarps * 4;
-  static constexpr int kScale = (kFlag + kWarps * 4 + 15) / 16 * 16;
+  static constexpr int kPlace = (kFlag + kWarps * 4 + 15) / 16 * 16;
+  static constexpr int kScale = kPlace + kWarps * 16;
   static constexpr int kQ = kScale + kWarps * kStages * 8;
   static constexpr int kQTeam = kSharedQ ? 2 * (D / 16) * NB * 32 * 8 + 8 * NB * 4 : 0;  // fragments, row factors
   static constexpr int kTotal = kQ + kTeams * kQTeam;
@@ -115,8 +116,7 @@ __device__ __forceinline__ uint4 lds128(const uint8_t* p) { return *reinterpret_
 // A team's part of one segment (row group rg of kv head `head` of request b): tiles [a, e) of n.
 struct Piece {
   int b, head, rg, groups, n, a, e;
-  int row0, rows, len;  // of the request
-  int64_t u;            // flat position of tile a
+  int u;  // position of tile a in the team's span
 };
 
 template <typename T, int D, int NB>
@@ -162,37 +162,36 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
   c_piece.a = field(0, 3);
   c_piece.n = field(1, 0);
   c_piece.groups = field(1, 1);
-  c_piece.row0 = field(1, 2);
-  c_piece.rows = field(1, 3);
+  int row0 = field(1, 2), rows_b = field(1, 3), len = field(3, 0);  // of the consumed piece's request
   const int64_t u0 = static_cast<int64_t>(static_cast<uint32_t>(field(2, 0))) | static_cast<int64_t>(field(2, 1)) << 32;
   const int64_t u1 = static_cast<int64_t>(static_cast<uint32_t>(field(2, 2))) | static_cast<int64_t>(field(2, 3)) << 32;
-  c_piece.len = field(3, 0);
   if (u0 >= u1) return;
-  c_piece.u = u0;
-  c_piece.e = static_cast<int>(min(static_cast<int64_t>(c_piece.n), c_piece.a + (u1 - u0)));
+  const int u_len = static_cast<int>(u1 - u0);  // a span is far below 2^31 tiles
+  c_piece.u = 0;
+  c_piece.e = c_piece.a + min(c_piece.n - c_piece.a, u_len);
+  int64_t* place_s = reinterpret_cast<int64_t*>(smem + G::kPlace) + warp * 2;  // needed at merges only
+  if (lane == 0) place_s[0] = u0, place_s[1] = span;
 
   const int64_t cap = static_cast<int64_t>(p.max_blocks) << p.shift;
   auto next_piece = [&](Piece& x) -> bool {
     x.u += x.e - x.a;
-    if (x.u >= u1) return false;
+    if (x.u >= u_len) return false;
     if (++x.rg >= x.groups) {
       x.rg = 0;
       if (++x.head >= p.n_kv_heads) {
         x.head = 0;
         int segs;
-        do {  // u < u1: a later request has work
+        do {  // u < u_len: a later request has work
           ++x.b;
           segs = st.seg_start[x.b + 1] - st.seg_start[x.b];
         } while (segs == 0);
-        x.row0 = st.row_start[x.b];
-        x.rows = st.row_start[x.b + 1] - x.row0;
-        x.len = st.len[x.b];
-        x.n = static_cast<int>((min(static_cast<int64_t>(x.len) + x.rows, cap) + 15) >> 4);
+        const int rows = st.row_start[x.b + 1] - st.row_start[x.b];
+        x.n = static_cast<int>((min(static_cast<int64_t>(st.len[x.b]) + rows, cap) + 15) >> 4);
         x.groups = segs / p.n_kv_heads;
       }
     }
     x.a = 0;
-    x.e = static_cast<int>(min(static_cast<int64_t>(x.n), u1 - x.u));
+    x.e = min(x.n, u_len - x.u);
     return true;
   };
 
@@ -244,9 +243,9 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
   uint2* q_s = reinterpret_cast<uint2*>(smem + G::kQ + sub * G::kQTeam);
   float* rs_s = reinterpret_cast<float*>(smem + G::kQ + sub * G::kQTeam + 2 * KS * NB * 32 * 8);
 
-  for (bool more = true; more; more = next_piece(c_piece)) {
-    const int head = c_piece.head, rg = c_piece.rg, row0 = c_piece.row0, len = c_piece.len;
-    const int r_valid = static_cast<int>(min(static_cast<int64_t>(c_piece.rows) * p.group - static_cast<int64_t>(rg) * RT,
+  for (;;) {
+    const int head = c_piece.head, rg = c_piece.rg;
+    const int r_valid = static_cast<int>(min(static_cast<int64_t>(rows_b) * p.group - static_cast<int64_t>(rg) * RT,
                                              static_cast<int64_t>(RT)));
     // row r of the segment -> (step row of the request, query head of the kv head)
     auto row_of = [&](int r, int& i, int& hq) {
@@ -579,7 +578,7 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
     }
     if (!whole) {
       // the teams that share the segment: those of the cuts inside it
-      const int64_t s0 = c_piece.u - c_piece.a, s1 = s0 + c_piece.n;
+      const int64_t s0 = place_s[0] + c_piece.u - c_piece.a, s1 = s0 + c_piece.n, span = place_s[1];
       const int t0 = static_cast<int>(s0 / span), t1 = static_cast<int>((s1 - 1) / span);
       __syncwarp();  // a team of one warp: its states are written
       if (tt == 0) flag_s[sub] = atom_add_acq_rel_gpu(p.tickets + t0, 1u) == static_cast<unsigned>(t1 - t0);
@@ -648,6 +647,13 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
           }
         }
       }
+    }
+    const int b = c_piece.b;
+    if (!next_piece(c_piece)) break;
+    if (c_piece.b != b) {
+      row0 = st.row_start[c_piece.b];
+      rows_b = st.row_start[c_piece.b + 1] - row0;
+      len = st.len[c_piece.b];
     }
   }
   cp_async_wait_all();

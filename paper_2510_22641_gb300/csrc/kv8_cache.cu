@@ -1,7 +1,6 @@
 // The paged 8-bit K/V cache: block tables and slot maps (plan), quantising writes (append), reads.
 #include <stdarg.h>
 #include <stdio.h>
-#include <stdlib.h>  // SWEEP
 
 #include "lowbit.cuh"
 
@@ -57,7 +56,6 @@ constexpr int kPlanPer = SSD_KV8_MAX_BATCH / kPlanThreads;
 struct PlanParams {
   int batch, rows, max_batch, max_blocks, n_blocks, shift;  // block_tokens = 1 << shift
   int n_kv_heads, group, row_tile;
-  int force_w;  // SWEEP
   const int32_t *len, *add, *state_in;
   int32_t *state_out, *table, *pool, *step, *status, *ticket;
 };
@@ -280,7 +278,7 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
     const int ctas = kAttnSms * sh.ctas;
     // Short contexts, a CTA for each: one segment per team, whatever its length, so that nothing is
     // merged through global memory (64 tiles take one SM about as long as that merge).
-    const bool each = n_segs <= ctas && longest_s <= 64 && p.force_w == 0;  // SWEEP
+    const bool each = n_segs <= ctas && longest_s <= 64;
     // Else CTAs, unless there are segments for all teams of a smaller size.  Then single warps where
     // segments are short (they share nothing but the states of cut segments), and quarter or half CTAs
     // where they are long, which cut fewer (measured, 8 rows: 640 segments of 42 tiles 34 us with single
@@ -290,7 +288,6 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
       const int small = sh.warps / sh.teams, mid = sh.warps == 12 ? 3 : 4;
       W = all < static_cast<int64_t>(128) * n_segs ? small : mid;
     }
-    if (p.force_w > 0 && sh.warps % p.force_w == 0 && sh.warps / p.force_w <= sh.teams) W = p.force_w;  // SWEEP
     const int per_cta = sh.warps / W, teams = ctas * per_cta;
     const int64_t span = max((all + teams - 1) / teams, static_cast<int64_t>(4 * W));
     const int64_t snap = span / 4;
@@ -544,7 +541,6 @@ ssd_status ssd_kv8_plan(const ssd_kv8* c, const ssd_kv8_step* step, const int32_
   p.n_kv_heads = c->n_kv_heads;
   p.group = c->n_heads / c->n_kv_heads;
   p.row_tile = step_row_tile(c, step);
-  p.force_w = getenv("ATT_W") ? atoi(getenv("ATT_W")) : 0;  // SWEEP
   p.len = len;
   p.add = add;
   p.state_in = state_in;
