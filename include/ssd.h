@@ -545,7 +545,7 @@ SSD_API ssd_status ssd_kv8_append(const ssd_kv8* c, int layer, const void* k, co
                                   int64_t v_head_stride, const int32_t* slot, void* cuda_stream);
 
 /* The values the cache holds at n slots: k, v = c * s, type SSD_TYPE_*, device [n][n_kv_heads][head_dim]
- * (contiguous); zeros where slot is negative. */
+ * (contiguous, 16-byte aligned); zeros where slot is negative. */
 SSD_API ssd_status ssd_kv8_read(const ssd_kv8* c, int layer, const int32_t* slot, int n, void* k, void* v, int type,
                                 void* cuda_stream);
 

@@ -61,17 +61,17 @@ struct PlanParams {
 };
 
 // Exclusive sums of N values per thread over the CTA; total[] gets the sums.
-template <int N>
-__device__ __forceinline__ void block_scan(int64_t (&v)[N], int64_t (&total)[N], int64_t (*tot)[N]) {
+template <int N, typename I>
+__device__ __forceinline__ void block_scan(I (&v)[N], I (&total)[N], I (*tot)[N]) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  int64_t x[N];
+  I x[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = v[i];
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int64_t y = __shfl_up_sync(~0u, x[i], o);
+      const I y = __shfl_up_sync(~0u, x[i], o);
       if (lane >= o) x[i] += y;
     }
   }
@@ -81,7 +81,8 @@ __device__ __forceinline__ void block_scan(int64_t (&v)[N], int64_t (&total)[N],
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    int64_t before = 0, all = 0;
+    I before = 0, all = 0;
+#pragma unroll
     for (int k = 0; k < kPlanThreads / 32; ++k) {
       if (k < w) before += tot[k][i];
       all += tot[k][i];
@@ -109,9 +110,11 @@ __device__ __forceinline__ int find_request(const int32_t* start, int n, int x) 
 // CTA that finishes reading last (state_in and state_out may be one buffer).
 __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanParams p) {
   __shared__ int32_t row_s[SSD_KV8_MAX_BATCH + 1], new_s[SSD_KV8_MAX_BATCH + 1], back_s[SSD_KV8_MAX_BATCH + 1];
-  __shared__ int32_t len_s[SSD_KV8_MAX_BATCH], held_s[SSD_KV8_MAX_BATCH], seg_s[SSD_KV8_MAX_BATCH + 1];
+  __shared__ int32_t len_s[SSD_KV8_MAX_BATCH], held_s[SSD_KV8_MAX_BATCH], seg_s[SSD_KV8_MAX_BATCH + 1],
+      n_s[SSD_KV8_MAX_BATCH];
   __shared__ int64_t work_s[SSD_KV8_MAX_BATCH + 1];
-  __shared__ int64_t tot3[kPlanThreads / 32][3], tot2[kPlanThreads / 32][2];
+  __shared__ int32_t tot3[kPlanThreads / 32][3];
+  __shared__ int64_t tot2[kPlanThreads / 32][2];
   __shared__ int last_s, longest_s;
   pdl_wait();
   pdl_trigger();
@@ -127,7 +130,7 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
     flags |= SSD_KV8_LENGTH;
   }
   int ln[kPlanPer], ad[kPlanPer], hd[kPlanPer], nw[kPlanPer];
-  int64_t sum3[3] = {0, 0, 0}, all3[3];
+  int32_t sum3[3] = {0, 0, 0}, all3[3];  // at most max_blocks * block_tokens * max_batch < 2^31
 #pragma unroll
   for (int k = 0; k < kPlanPer; ++k) {
     const int b = tid * per + k;
@@ -146,10 +149,10 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
     sum3[1] += nw[k];
     sum3[2] += l < 0 ? h : 0;
   }
-  block_scan<3>(sum3, all3, tot3);
+  block_scan(sum3, all3, tot3);
   if (all3[0] > p.rows) flags |= SSD_KV8_LENGTH;
-  const int n_new = static_cast<int>(all3[1]);
-  const int n_back = static_cast<int>(min(all3[2], static_cast<int64_t>(p.n_blocks - n_free)));
+  const int n_new = all3[1];
+  const int n_back = min(all3[2], p.n_blocks - n_free);
   if (all3[2] > n_back) flags |= SSD_KV8_LENGTH;
   const int total = n_free + n_back;
   if (n_new > total) flags |= SSD_KV8_NO_BLOCKS;
@@ -166,8 +169,8 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
     r += ad[k];
     const int r1 = static_cast<int>(min(r, static_cast<int64_t>(p.rows)));
     row_s[b] = r0;
-    new_s[b] = static_cast<int>(sum3[1]);
-    back_s[b] = static_cast<int>(min(sum3[2], static_cast<int64_t>(n_back)));
+    new_s[b] = sum3[1];
+    back_s[b] = min(sum3[2], n_back);
     sum3[1] += nw[k];
     sum3[2] += ln[k] < 0 ? hd[k] : 0;
     len_s[b] = max(ln[k], 0);
@@ -185,12 +188,13 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
                 ((static_cast<int64_t>(rows_b) * p.group + p.row_tile - 1) / p.row_tile);
       tiles[k] = segs[k] * n;
     }
+    n_s[b] = n;
     longest = max(longest, n);
     sum2[0] += segs[k];
     sum2[1] += tiles[k];
   }
   if (tid == 0) longest_s = 0;
-  block_scan<2>(sum2, all2, tot2);
+  block_scan(sum2, all2, tot2);
   if (longest) atomicMax(&longest_s, longest);
   const StepView s = step_view(p.step, p.batch);
 #pragma unroll
@@ -215,8 +219,9 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
     }
     if (flags) atomicOr(p.status, flags);
   }
-  if (tid == 0) last_s = atomicAdd(p.ticket, 1) == static_cast<int>(gridDim.x) - 1;
-  __syncthreads();
+  // the ticket that says whether all CTAs have read the counts; its answer is awaited at the end
+  int ticket = 0;
+  if (tid == 0) ticket = atomicAdd(p.ticket, 1);
 
   // the block handed out i-th, or -1
   auto handed = [&](int i) -> int {
@@ -235,38 +240,50 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
     }
     return id;
   };
-  const int first = blockIdx.x * kPlanThreads + tid, stride = gridDim.x * kPlanThreads;
+  // Four lists are filled (rows, new table entries, returned blocks, team spans), each from another CTA on,
+  // so that for a small step their loads' latencies do not add up.
+  const int stride = gridDim.x * kPlanThreads;
+  auto begin = [&](int cta) -> int { return (blockIdx.x + gridDim.x - cta) % gridDim.x * kPlanThreads + tid; };
+  const int first = begin(0);
   int32_t* slot = s.slot;
   const int n_rows = row_s[p.batch];
-  for (int64_t r64 = first; r64 < p.rows; r64 += stride) {
+  // four rows per thread: usually of one request and one block
+  auto block_of = [&](int b, int j) -> int {  // id of the seat's j-th block after this call, or -1
+    if (j >= held_s[b]) return handed(new_s[b] + j - held_s[b]);
+    const int id = p.table[static_cast<size_t>(b) * p.max_blocks + j];
+    if (id < p.n_blocks) return id;
+    atomicOr(p.status, SSD_KV8_SLOT);
+    return -1;
+  };
+  const bool quads = (reinterpret_cast<uintptr_t>(slot) & 15) == 0;
+  for (int64_t r64 = 4ll * first; r64 < p.rows; r64 += 4ll * stride) {
     const int row = static_cast<int>(r64);
-    int out = -1;
+    int out[4] = {-1, -1, -1, -1};
     if (row < n_rows) {
-      const int b = find_request(row_s, p.batch, row);
-      const int64_t pos = static_cast<int64_t>(len_s[b]) + (row - row_s[b]);
-      if (pos < cap) {
-        const int j = static_cast<int>(pos >> p.shift);
-        int id;
-        if (j < held_s[b]) {
-          id = p.table[static_cast<size_t>(b) * p.max_blocks + j];
-          if (id >= p.n_blocks) {
-            atomicOr(p.status, SSD_KV8_SLOT);
-            id = -1;
-          }
-        } else {
-          id = handed(new_s[b] + j - held_s[b]);
-        }
-        if (id >= 0) out = (id << p.shift) + static_cast<int>(pos & bs_m1);
+      int b = find_request(row_s, p.batch, row), j = -1, id = -1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (row + k >= n_rows) break;
+        while (row + k >= row_s[b + 1]) ++b, j = -1;
+        const int64_t pos = static_cast<int64_t>(len_s[b]) + (row + k - row_s[b]);
+        if (pos >= cap) continue;
+        const int block = static_cast<int>(pos >> p.shift);
+        if (block != j) j = block, id = block_of(b, j);
+        if (id >= 0) out[k] = (id << p.shift) + static_cast<int>(pos & bs_m1);
       }
     }
-    slot[row] = out;
+    if (quads && row + 4 <= p.rows) {
+      *reinterpret_cast<int4*>(slot + row) = make_int4(out[0], out[1], out[2], out[3]);
+    } else {
+      for (int k = 0; k < 4 && row + k < p.rows; ++k) slot[row + k] = out[k];
+    }
   }
-  for (int64_t i = first; i < n_new; i += stride) {
+  for (int64_t i = begin(1); i < n_new; i += stride) {
     const int b = find_request(new_s, p.batch, static_cast<int>(i));
     p.table[static_cast<size_t>(b) * p.max_blocks + held_s[b] + (i - new_s[b])] = handed(static_cast<int>(i));
   }
   // returned blocks that are not handed out again stay on the stack
-  for (int64_t i = first; i < min(n_back, total - n_new); i += stride) {
+  for (int64_t i = begin(2); i < min(n_back, total - n_new); i += stride) {
     const int b = find_request(back_s, p.batch, static_cast<int>(i));
     p.pool[n_free + i] = p.table[static_cast<size_t>(b) * p.max_blocks + (i - back_s[b])];
   }
@@ -289,7 +306,18 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
       W = all < static_cast<int64_t>(128) * n_segs ? small : mid;
     }
     const int per_cta = sh.warps / W, teams = ctas * per_cta;
-    const int64_t span = max((all + teams - 1) / teams, static_cast<int64_t>(4 * W));
+    // quotient and remainder, in 32 bits where they fit (64-bit division is many times slower)
+    auto divide = [](int64_t x, int64_t y, int64_t& rest) -> int64_t {
+      if (((x | y) >> 32) == 0) {
+        const uint32_t q = static_cast<uint32_t>(x) / static_cast<uint32_t>(y);
+        rest = static_cast<uint32_t>(x) - q * static_cast<uint32_t>(y);
+        return q;
+      }
+      rest = x % y;
+      return x / y;
+    };
+    int64_t rest;
+    const int64_t span = max(divide(all + teams - 1, teams, rest), static_cast<int64_t>(4 * W));
     const int64_t snap = span / 4;
     auto request_at = [&](int64_t u) -> int {  // 0 <= u < all
       int lo = 0, hi = p.batch;
@@ -299,24 +327,24 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
       }
       return lo;
     };
-    auto tiles_of = [&](int b) -> int { return static_cast<int>((work_s[b + 1] - work_s[b]) / (seg_s[b + 1] - seg_s[b])); };
     // Equal spans; a cut inside a segment that is short against the span moves to its nearer end.
     auto cut = [&](int c) -> int64_t {
       const int64_t x = c * span;
       if (x >= all) return all;
-      const int b = request_at(x), n = tiles_of(b);
+      const int b = request_at(x), n = n_s[b];
       if (n > snap) return x;
-      const int tile = static_cast<int>((x - work_s[b]) % n);
+      int64_t tile;
+      divide(x - work_s[b], n, tile);
       return tile < n - tile ? x - tile : x - tile + n;
     };
     if (first == 0) *s.head = StepHead{span, W, n_rows, {}};
-    for (int i = first; i < ctas * sh.teams; i += stride) {
+    for (int i = begin(3); i < ctas * sh.teams; i += stride) {
       const int sub = i % sh.teams, team = i / sh.teams * per_cta + sub;
       TeamSpan t = {};
       if (sub < per_cta) {
         if (each) {
           if (team < n_segs) {
-            const int b = find_request(seg_s, p.batch, team), n = tiles_of(b);
+            const int b = find_request(seg_s, p.batch, team), n = n_s[b];
             t.u0 = work_s[b] + static_cast<int64_t>(team - seg_s[b]) * n;
             t.u1 = t.u0 + n;
           }
@@ -326,11 +354,11 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
         }
         if (t.u0 < t.u1) {
           t.b = request_at(t.u0);
-          t.n = tiles_of(t.b);
+          t.n = n_s[t.b];
           t.groups = (seg_s[t.b + 1] - seg_s[t.b]) / p.n_kv_heads;
-          const int64_t d = t.u0 - work_s[t.b];
-          const int seg = static_cast<int>(d / t.n);
-          t.tile = static_cast<int>(d - static_cast<int64_t>(seg) * t.n);
+          int64_t tile;
+          const int seg = static_cast<int>(divide(t.u0 - work_s[t.b], t.n, tile));
+          t.tile = static_cast<int>(tile);
           t.head = seg / t.groups;
           t.rg = seg - t.head * t.groups;
           t.row0 = row_s[t.b];
@@ -341,6 +369,8 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
       s.teams[i] = t;
     }
   }
+  if (tid == 0) last_s = ticket == static_cast<int>(gridDim.x) - 1;
+  __syncthreads();
   if (last_s) {  // every CTA has read the counts
     if (tid == 0) {
       *p.ticket = 0;
@@ -364,107 +394,353 @@ struct AppendParams {
   const void *k, *v;
   int64_t k_row, k_head, v_row, v_head;
   const int32_t* slot;
-  int rows, window, shift, n_blocks, n_kv_heads;
+  int rows, takers, shift, n_blocks, n_kv_heads;  // takers: CTAs that share a window of rows
   uint8_t* data;   // this layer's
   float* scales;
   int32_t* status;
 };
 
-__device__ __forceinline__ int quantise8(float x, float inv) {
-  const float q = rintf(x * inv);
-  return x != x ? 0 : static_cast<int>(fminf(fmaxf(q, -127.0f), 127.0f));
+// Codes plus 128 of four values as bytes.  The product is rounded to fp32, then the addition of
+// 1.5 2^23 + 128 rounds it to an integer (ties to even) whose low byte is the code: |x inv| <= 127.5 here.
+__device__ __forceinline__ uint32_t code8(float x, float inv) { return __float_as_uint(__fadd_rn(__fmul_rn(x, inv), 12583040.0f)); }
+__device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+// The same for values that may be NaN (code 0) or infinite (the largest code).
+__device__ __forceinline__ float tame(float x, float scale) {
+  return x != x ? 0.0f : fminf(fmaxf(x, -127.0f * scale), 127.0f * scale);
+}
+// The four codes of a word at a scale `ratio` times as large.
+__device__ __forceinline__ uint32_t rescale8(uint32_t word, float ratio) {
+  uint32_t q[4];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) q[b] = code8(static_cast<float>(static_cast<int>(word >> (8 * b) & 255u) - 128), ratio);
+  return pack4(q[0], q[1], q[2], q[3]);
+}
+// Maximum that keeps a NaN.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
 
-// One warp per (block that the call touches, kv head, K or V): the rows of a block are neighbours, the
-// first of them (its predecessor's slot is not one less, or it opens the block) stands for all.
+// E consecutive elements of a row, as they lie in memory.
+template <typename T, int E>
+struct Piece {
+  uint32_t w[E * sizeof(T) / 4];
+  template <bool VEC>
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (!VEC) {
+      T e[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) e[i] = p[i];
+#pragma unroll
+      for (int i = 0; i < E * static_cast<int>(sizeof(T)) / 4; ++i) w[i] = reinterpret_cast<const uint32_t*>(e)[i];
+    } else if constexpr (sizeof(w) == 16) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p);
+      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else if constexpr (sizeof(w) == 8) {
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      w[0] = v.x, w[1] = v.y;
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (uint32_t& x : w) x = 0;
+  }
+  __device__ __forceinline__ float operator[](int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return i & 1 ? __uint_as_float(w[i / 2] & 0xffff0000u) : __uint_as_float(w[i / 2] << 16);
+  }
+};
+
+// Decode steps: few rows per block.  One warp per (row that stands for a block, kv head, K or V), which
+// takes the rows of the block that follow it; the lanes go over (row, 4 dimensions).  Latency bound: the
+// rows are read twice (the second time from L1) so that a warp needs few registers and all are resident.
 template <typename T, int D, bool VEC>
-__global__ void __launch_bounds__(128) ssd_kv8_append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(128) ssd_kv8_append_rows_kernel(const AppendParams p) {
+  constexpr int D4 = D / 4;
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int h = blockIdx.y * 2 + (w >> 1), kv = w & 1;
+  const int h = blockIdx.y * 2 + (w >> 1), kv = w & 1, r = blockIdx.x;
   if (h >= p.n_kv_heads) return;
   const int bs = 1 << p.shift;
-  const T* src = static_cast<const T*>(kv ? p.v : p.k);
+  // the slots from the row before on: one load shows whether this row stands for its block, and which follow
+  const int at = r - 1 + lane;
+  int s = at >= 0 && at < p.rows ? p.slot[at] : -1;
+  const int before = __shfl_sync(~0u, s, 0), s0 = __shfl_sync(~0u, s, 1);
+  if (s0 < 0) return;
+  if (s0 >= p.n_blocks << p.shift) {
+    if (lane == 0) atomicOr(p.status, SSD_KV8_SLOT);
+    return;
+  }
+  const int off = s0 & (bs - 1);
+  if (off != 0 && r > 0 && before == s0 - 1) return;
+  unsigned m = __ballot_sync(~0u, lane > 0 && s == s0 + lane - 1 && off + lane - 1 < bs) >> 1;
+  int n = m == 0x7fffffffu ? 31 : __ffs(~m) - 1;  // rows of this block
+  for (int base = 31; n == base && base < bs - off; base += 32) {
+    const int i = base + lane;
+    m = __ballot_sync(~0u, i < bs - off && r + i < p.rows && p.slot[r + i] == s0 + i);
+    n += m == ~0u ? 32 : __ffs(~m) - 1;
+  }
+  const T* src = static_cast<const T*>(kv ? p.v : p.k) + h * (kv ? p.v_head : p.k_head) + r * (kv ? p.v_row : p.k_row);
   const int64_t row_stride = kv ? p.v_row : p.k_row;
-  src += h * (kv ? p.v_head : p.k_head);
-  const int64_t r_begin = static_cast<int64_t>(blockIdx.x) * p.window;
-  const int r_end = static_cast<int>(min(r_begin + p.window, static_cast<int64_t>(p.rows)));
+  const size_t rec = static_cast<size_t>(s0 >> p.shift) * p.n_kv_heads + h;
+  uint8_t* blk = p.data + rec * (static_cast<size_t>(bs) * 2 * D) + kv * (16 * D);
+  float* sc = p.scales + rec * 2 + kv;
+  const float s_old = off ? *sc : 0.0f;
+
+  float amax = 0.0f;
+  bool bad = false;
+#pragma unroll 4
+  for (int c = lane; c < n * D4; c += 32) {
+    const float4 x = load4<VEC>(src + c / D4 * row_stride + c % D4 * 4);
+    const float e[4] = {fabsf(x.x), fabsf(x.y), fabsf(x.z), fabsf(x.w)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool fin = e[i] <= 3.402823466e38f;
+      bad |= !fin;
+      amax = fmaxf(amax, fin ? e[i] : 0.0f);
+    }
+  }
+  if (bad) atomicOr(p.status, SSD_KV8_NON_FINITE);
+  amax = warp_max(amax);
+  const float s_new = fmaxf(s_old, fmaxf(amax / 127.0f, 0x1p-100f));
+  const float inv = 1.0f / s_new;
+  if (off && s_new > s_old) {
+    // older tokens of the block; a word may hold later ones too, which are rewritten or stale
+    const float ratio = s_old / s_new;
+    const int tiles = (off + 15) >> 4;
+#pragma unroll 4
+    for (int i = lane; i < tiles * (4 * D); i += 32) {
+      uint32_t* word = reinterpret_cast<uint32_t*>(blk + i / (4 * D) * (32 * D) + i % (4 * D) * 4);
+      *word = rescale8(*word, ratio);
+    }
+  }
+  __syncwarp();
+  if (lane == 0) *sc = s_new;
+#pragma unroll 4
+  for (int c = lane; c < n * D4; c += 32) {
+    const float4 x = load4<VEC>(src + c / D4 * row_stride + c % D4 * 4);
+    const int token = off + c / D4, d = c % D4 * 4;
+    const uint32_t q[4] = {code8(tame(x.x, s_new), inv), code8(tame(x.y, s_new), inv), code8(tame(x.z, s_new), inv),
+                           code8(tame(x.w, s_new), inv)};
+    uint8_t* tile = blk + (token >> 4) * (32 * D);
+    if (kv == 0) {
+      *reinterpret_cast<uint32_t*>(tile + kv8_k_byte(token & 15, d, D)) = pack4(q[0], q[1], q[2], q[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tile[kv8_v_byte(token & 15, d + i)] = static_cast<uint8_t>(q[i]);
+    }
+  }
+}
+
+// The entries of a window of a slot list that begin a run (consecutive slots, cut where a slot is a
+// multiple of `cut`), listed by the whole CTA of 8 warps (a ballot per 32 entries).  A run that began in
+// the window before is that window's, and negative entries or ones past the cache are none; with `all`
+// the window's first entry begins a run, and each such entry is one.  Returns how many; flags bad slots.
+constexpr int kWindow = 512;
+
+struct Runs {
+  uint16_t first[kWindow];  // index in the window
+  int32_t slot[kWindow];    // its slot
+  int count[kWindow / 32];
+};
+
+__device__ __forceinline__ int list_runs(Runs& runs, const int32_t* slot, int begin, int end, int most, int cut, bool all,
+                                         int& flags) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  unsigned mine[2];
+  int own[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = begin + (w + 8 * i) * 32 + lane;
+    const int s = r < end ? slot[r] : -1;
+    own[i] = s;
+    if (s >= most) flags |= SSD_KV8_SLOT;
+    const bool in = s >= 0 && s < most;
+    const bool starts = in ? (s & (cut - 1)) == 0 || r == 0 || (all && r == begin) || slot[r - 1] != s - 1 : all;
+    mine[i] = __ballot_sync(~0u, r < end && starts);
+    if (lane == 0) runs.count[w + 8 * i] = __popc(mine[i]);
+  }
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int k = 0; k < kWindow / 32; ++k) {
+      before += k < w + 8 * i ? runs.count[k] : 0;
+      total += runs.count[k];
+    }
+    if (mine[i] >> lane & 1u) {
+      const int o = before + __popc(mine[i] & ((1u << lane) - 1));
+      runs.first[o] = static_cast<uint16_t>((w + 8 * i) * 32 + lane);
+      runs.slot[o] = own[i];
+    }
+  }
+  __syncthreads();
+  return total;
+}
+
+// A job is the rows that the call puts into one block, for one kv head and K or V: the rows of a block
+// are neighbours, and the first of them (its predecessor's slot is not one less, or it opens the block)
+// stands for all.  Each 16-token tile of the block has a warp, which holds the tile's new values in
+// registers between the maximum and the rounding (a lane D / 32 dimensions of all 16 tokens), so rows
+// are read once.  A word of V holds four tokens of one dimension: where old tokens share it with new
+// ones, or the scale has grown, it is read first.
+//
+// Prompts; bound: bytes.  A CTA of 8 warps takes 8 / (block / 16) jobs at a time and every `takers`-th of
+// its window's blocks, so that rows that stand for none cost nothing.
+template <typename T, int D, bool VEC>
+__global__ void __launch_bounds__(256, 2) ssd_kv8_append_kernel(const AppendParams p) {
+  constexpr int E = D / 32;
+  __shared__ Runs runs;
+  __shared__ float amax_s[8];
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int bs = 1 << p.shift, log_tiles = p.shift - 4, tiles = 1 << log_tiles;
+  const int job = (blockIdx.y * 8 + w) >> log_tiles, tile = w & (tiles - 1);
+  const int h = job >> 1, kv = job & 1;
+  const bool live = h < p.n_kv_heads;  // a warp without a job still takes part in the barriers
+  const T* src = static_cast<const T*>(kv ? p.v : p.k) + lane * E;
+  const int64_t row_stride = kv ? p.v_row : p.k_row;
+  if (live) src += h * (kv ? p.v_head : p.k_head);
+  const int window = blockIdx.x / p.takers, taker = blockIdx.x - window * p.takers;
+  const int r_begin = window * kWindow, r_end = min(r_begin + kWindow, p.rows);
   int flags = 0;
-  for (int r = static_cast<int>(r_begin); r < r_end; ++r) {
-    const int s0 = p.slot[r];
-    if (s0 < 0) continue;
-    if (s0 >= (p.n_blocks << p.shift)) {
-      flags |= SSD_KV8_SLOT;
-      continue;
-    }
-    const int off = s0 & (bs - 1);
-    if (off != 0 && r > 0 && p.slot[r - 1] == s0 - 1) continue;
-    int n = 1;  // rows of this block
-    for (int base = 1; base < bs - off; base += 32) {
-      const int i = base + lane;
-      const bool mine = i < bs - off && r + i < p.rows && p.slot[r + i] == s0 + i;
-      const unsigned m = __ballot_sync(~0u, mine);
-      const int run = m == ~0u ? 32 : __ffs(~m) - 1;
-      n += run;
-      if (run < 32) break;
-    }
-    const size_t rec = static_cast<size_t>(s0 >> p.shift) * p.n_kv_heads + h;
-    uint8_t* blk = p.data + rec * (static_cast<size_t>(bs) * 2 * D) + kv * (16 * D);
+  const int total = list_runs(runs, p.slot, r_begin, r_end, p.n_blocks << p.shift, bs, false, flags);
+
+  for (int o = taker; o < total; o += p.takers) {  // the same for all warps of the CTA
+    const int r = r_begin + runs.first[o];
+    const int s0 = runs.slot[o], off = s0 & (bs - 1);
+    const size_t rec = static_cast<size_t>(s0 >> p.shift) * p.n_kv_heads + (live ? h : 0);
     float* sc = p.scales + rec * 2 + kv;
     const float s_old = off ? *sc : 0.0f;
-
-    constexpr int D4 = D / 4;
-    float amax = 0.0f;
-    bool bad = false;
-#pragma unroll 4
-    for (int c = lane; c < n * D4; c += 32) {
-      const float4 x = load4<VEC>(src + (r + c / D4) * row_stride + (c % D4) * 4);
-      const float e[4] = {fabsf(x.x), fabsf(x.y), fabsf(x.z), fabsf(x.w)};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool fin = e[i] <= 3.402823466e38f;
-        bad |= !fin;
-        amax = fmaxf(amax, fin ? e[i] : 0.0f);
-      }
+    int n = 0;  // rows that go on in this block
+    for (int base = 0; base < bs - off; base += 32) {
+      const int i = base + lane;
+      const unsigned m = __ballot_sync(~0u, i < bs - off && r + i < p.rows && p.slot[r + i] == s0 + i);
+      n += m == ~0u ? 32 : __ffs(~m) - 1;
+      if (m != ~0u) break;
     }
-    if (bad) flags |= SSD_KV8_NON_FINITE;
+    // tokens first .. last - 1 of the tile are new, those before them older (16: all of the tile)
+    const int first = min(max(off - 16 * tile, 0), 16), last = live ? min(off + n - 16 * tile, 16) : 0;
+    const T* rows = src + (r + 16 * tile - off) * row_stride;  // token i at rows + i * row_stride
+    Piece<T, E> x[16];
+    float amax = 0.0f;
+    bool full = first == 0 && last == 16;
+    if (full) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i].template load<VEC>(rows + i * row_stride);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) amax = max_nan(amax, fabsf(x[i][e]));
+      full = !__any_sync(~0u, !(amax <= 3.402823466e38f));
+    }
+    if (!full) {  // part of a tile, or one with NaN or infinities
+      amax = 0.0f;
+      bool bad = false;
+#pragma unroll 4
+      for (int i = first; i < last; ++i) {
+        Piece<T, E> y;
+        y.template load<VEC>(rows + i * row_stride);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float a = fabsf(y[e]);
+          const bool fin = a <= 3.402823466e38f;
+          bad |= !fin;
+          amax = fmaxf(amax, fin ? a : 0.0f);
+        }
+      }
+      if (bad) flags |= SSD_KV8_NON_FINITE;
+    }
     amax = warp_max(amax);
+    if (tiles > 1) {
+      if (lane == 0) amax_s[w] = amax;
+      __syncthreads();
+      for (int i = 0; i < tiles; ++i) amax = fmaxf(amax, amax_s[(w & ~(tiles - 1)) + i]);
+      __syncthreads();  // before the next block's maxima
+    }
+    if (!live) continue;
     const float s_new = fmaxf(s_old, fmaxf(amax / 127.0f, 0x1p-100f));
     const float inv = 1.0f / s_new;
-    if (off && s_new > s_old) {
-      // older tokens of the block; a word may hold later ones too, which are rewritten or stale
-      const float ratio = s_old / s_new;
-      const int tiles = (off + 15) >> 4;
-      for (int i = lane; i < tiles * (4 * D); i += 32) {
-        uint32_t* word = reinterpret_cast<uint32_t*>(blk + (i / (4 * D)) * (32 * D) + (i % (4 * D)) * 4);
-        const uint32_t old = *word;
-        uint32_t now = 0;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int q = static_cast<int>((old >> (8 * b)) & 255u) - 128;
-          now |= static_cast<uint32_t>(static_cast<int>(rintf(q * ratio)) + 128) << (8 * b);
-        }
-        *word = now;
-      }
-    }
+    // (every warp of the job has read the old scale before the barrier; a block of one tile is one warp's)
     __syncwarp();
-    if (lane == 0) *sc = s_new;
-#pragma unroll 4
-    for (int c = lane; c < n * D4; c += 32) {
-      const float4 x = load4<VEC>(src + (r + c / D4) * row_stride + (c % D4) * 4);
-      const int token = off + c / D4, d = (c % D4) * 4;
-      const int q[4] = {quantise8(x.x, inv) + 128, quantise8(x.y, inv) + 128, quantise8(x.z, inv) + 128,
-                        quantise8(x.w, inv) + 128};
-      uint8_t* tile = blk + (token >> 4) * (32 * D);
+    if (tile == 0 && lane == 0) *sc = s_new;
+    uint8_t* dst = p.data + rec * (static_cast<size_t>(bs) * 2 * D) + tile * (32 * D) + kv * (16 * D);
+    if (full) {
+      auto code = [&](int i, int e) -> uint32_t { return code8(x[i][e], inv); };
       if (kv == 0) {
-        *reinterpret_cast<uint32_t*>(tile + kv8_k_byte(token & 15, d, D)) = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          uint8_t* at = dst + kv8_k_byte(i, lane * E, D);
+          if constexpr (E == 4) *reinterpret_cast<uint32_t*>(at) = pack4(code(i, 0), code(i, 1), code(i, 2), code(i, 3));
+          else *reinterpret_cast<uint16_t*>(at) = static_cast<uint16_t>(__byte_perm(code(i, 0), code(i, 1), 0x0040));
+        }
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tile[kv8_v_byte(token & 15, d + i)] = static_cast<uint8_t>(q[i]);
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            *reinterpret_cast<uint32_t*>(dst + kv8_v_byte(4 * t, lane * E + e)) =
+                pack4(code(4 * t, e), code(4 * t + 1, e), code(4 * t + 2, e), code(4 * t + 3, e));
+      }
+      continue;
+    }
+    const bool grown = off && s_new > s_old;
+    const float ratio = s_old / s_new;
+    if (kv == 0) {
+#pragma unroll 4
+      for (int i = grown ? 0 : first; i < max(first, last); ++i) {
+        uint8_t* at = dst + kv8_k_byte(i, lane * E, D);
+        uint32_t word;
+        if (i < first) {
+          if constexpr (E == 4) word = *reinterpret_cast<const uint32_t*>(at);
+          else word = *reinterpret_cast<const uint16_t*>(at);
+          word = rescale8(word, ratio);
+        } else {
+          Piece<T, E> y;
+          y.template load<VEC>(rows + i * row_stride);
+          word = 0;
+#pragma unroll
+          for (int e = 0; e < E; ++e) word |= (code8(tame(y[e], s_new), inv) & 255u) << (8 * e);
+        }
+        if constexpr (E == 4) *reinterpret_cast<uint32_t*>(at) = word;
+        else *reinterpret_cast<uint16_t*>(at) = static_cast<uint16_t>(word);
+      }
+    } else {
+#pragma unroll 1
+      for (int t = 0; t < 4; ++t) {
+        const bool has_new = 4 * t + 3 >= first && 4 * t < last;
+        if (!has_new && !(grown && 4 * t < first)) continue;
+        uint32_t word[E], put = 0;  // the bytes of new tokens
+#pragma unroll
+        for (int e = 0; e < E; ++e) word[e] = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (4 * t + i >= first && 4 * t + i < last) {
+            Piece<T, E> y;
+            y.template load<VEC>(rows + (4 * t + i) * row_stride);
+            put |= 255u << (8 * i);
+#pragma unroll
+            for (int e = 0; e < E; ++e) word[e] |= (code8(tame(y[e], s_new), inv) & 255u) << (8 * i);
+          }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          uint32_t* at = reinterpret_cast<uint32_t*>(dst + kv8_v_byte(4 * t, lane * E + e));
+          uint32_t old = *at;
+          if (grown) old = rescale8(old, ratio);
+          *at = (old & ~put) | word[e];
+        }
       }
     }
-    __syncwarp();
   }
   if (flags) atomicOr(p.status, flags);
 }
@@ -473,35 +749,94 @@ __global__ void __launch_bounds__(128) ssd_kv8_append_kernel(const AppendParams 
 
 struct ReadParams {
   const int32_t* slot;
-  int n, shift, n_blocks, n_kv_heads;
+  int n, takers, shift, n_blocks, n_kv_heads;
   const uint8_t* data;
   const float* scales;
   void *k, *v;
   int32_t* status;
 };
 
-// One warp per (slot, kv head, K or V).
+template <typename T, int E>
+__device__ __forceinline__ void store_row(T* p, const float (&x)[E]) {
+  if constexpr (sizeof(T) == 4) {
+    if constexpr (E == 4) *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    else *reinterpret_cast<float2*>(p) = make_float2(x[0], x[1]);
+  } else {
+    __nv_bfloat162 h[E / 2];
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) h[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    if constexpr (E == 4) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(h);
+    else *reinterpret_cast<uint32_t*>(p) = *reinterpret_cast<const uint32_t*>(h);
+  }
+}
+
+// The value of byte `b` of a word: the byte goes into the mantissa of 2^23.
+__device__ __forceinline__ float value8(uint32_t word, int b, float scale) {
+  return (__uint_as_float(__byte_perm(word, 0x4b000000u, 0x7440 + b)) - 8388736.0f) * scale;
+}
+
+// A warp per run of slots inside a 16-token tile (list_runs), kv head and K or V.  Bound: bytes, mostly
+// those written.
 template <typename T, int D>
-__global__ void __launch_bounds__(128) ssd_kv8_read_kernel(const ReadParams p) {
+__global__ void __launch_bounds__(256, 3) ssd_kv8_read_kernel(const ReadParams p) {
+  constexpr int E = D / 32;
+  __shared__ Runs runs;
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int h = blockIdx.y * 2 + (w >> 1), kv = w & 1;
+  const int bs = 1 << p.shift, most = p.n_blocks << p.shift;
+  const int window = blockIdx.x / p.takers, taker = blockIdx.x - window * p.takers;
+  const int i_begin = window * kWindow, i_end = min(i_begin + kWindow, p.n);
+  int flags = 0;
+  const int total = list_runs(runs, p.slot, i_begin, i_end, most, 16, true, flags);
+  if (flags) atomicOr(p.status, flags);
+  const int h = blockIdx.y * 4 + (w >> 1), kv = w & 1;
   if (h >= p.n_kv_heads) return;
-  const int i = blockIdx.x;
-  int s = p.slot[i];
-  if (s >= (p.n_blocks << p.shift)) {
-    if (lane == 0) atomicOr(p.status, SSD_KV8_SLOT);
-    s = -1;
-  }
-  T* out = static_cast<T*>(kv ? p.v : p.k) + (static_cast<size_t>(i) * p.n_kv_heads + h) * D;
-  const int bs = 1 << p.shift, token = s & (bs - 1);
-  const size_t rec = static_cast<size_t>(s < 0 ? 0 : s >> p.shift) * p.n_kv_heads + h;
-  const uint8_t* tile = p.data + rec * (static_cast<size_t>(bs) * 2 * D) + (token >> 4) * (32 * D) + kv * (16 * D);
-  const float sc = s < 0 ? 0.0f : p.scales[rec * 2 + kv];
-  for (int d = lane; d < D; d += 32) {
-    const int byte = kv ? kv8_v_byte(token & 15, d) : kv8_k_byte(token & 15, d, D);
-    out[d] = from_f32<T>(s < 0 ? 0.0f : (static_cast<int>(tile[byte]) - 128) * sc);
+  const size_t row = static_cast<size_t>(p.n_kv_heads) * D;
+  T* out0 = static_cast<T*>(kv ? p.v : p.k) + static_cast<size_t>(h) * D + lane * E;
+#pragma unroll 1
+  for (int o = taker; o < total; o += p.takers) {
+    const int i0 = i_begin + runs.first[o], n = (o + 1 < total ? i_begin + runs.first[o + 1] : i_end) - i0;
+    T* out = out0 + i0 * row;
+    const int s0 = runs.slot[o];
+    float x[E];
+    if (s0 < 0 || s0 >= most) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = 0.0f;
+      store_row<T, E>(out, x);  // an entry of its own
+      continue;
+    }
+    const size_t rec = static_cast<size_t>(s0 >> p.shift) * p.n_kv_heads + h;
+    const uint8_t* tile = p.data + rec * (static_cast<size_t>(bs) * 2 * D) + ((s0 & (bs - 1)) >> 4) * (32 * D) + kv * (16 * D);
+    const float scale = p.scales[rec * 2 + kv];
+    // the whole tile's words, whatever part of it is asked for: all loads are in flight at once
+    const int t0 = s0 & 15;
+    T* base = out - t0 * static_cast<int64_t>(row);
+    uint32_t word[4 * E];  // K: token by token (E == 2: two tokens a word); V: four tokens of a dimension
+    if (kv) {
+#pragma unroll
+      for (int j = 0; j < 4 * E; ++j) word[j] = *reinterpret_cast<const uint32_t*>(tile + kv8_v_byte(4 * (j / E), lane * E + j % E));
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = value8(word[i / 4 * E + e], i & 3, scale);
+        if (i >= t0 && i < t0 + n) store_row<T, E>(base + i * row, x);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint8_t* at = tile + kv8_k_byte(i, lane * E, D);
+        if constexpr (E == 4) word[i] = *reinterpret_cast<const uint32_t*>(at);
+        else if (i % 2 == 0) word[i / 2] = *reinterpret_cast<const uint16_t*>(at);
+        else word[i / 2] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(at)) << 16;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = E == 4 ? value8(word[i], e, scale) : value8(word[i / 2], i % 2 * 2 + e, scale);
+        if (i >= t0 && i < t0 + n) store_row<T, E>(base + i * row, x);
+      }
+    }
   }
 }
 
@@ -554,7 +889,7 @@ ssd_status ssd_kv8_plan(const ssd_kv8* c, const ssd_kv8_step* step, const int32_
   const AttnShape sh = attn_shape(p.row_tile);
   const int teams = (kAttnSms * sh.ctas * sh.teams + kPlanThreads - 1) / kPlanThreads;
   int grid = (step->rows + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
-  grid = grid < teams ? teams : grid > kAttnSms ? kAttnSms : grid;
+  grid = grid < teams + 3 ? teams + 3 : grid > kAttnSms ? kAttnSms : grid;
   return op_launch("ssd_kv8_plan", ssd_kv8_plan_kernel, dim3(grid), kPlanThreads, 0,
                    static_cast<cudaStream_t>(cuda_stream), p);
 }
@@ -564,7 +899,7 @@ ssd_status ssd_kv8_append(const ssd_kv8* c, int layer, const void* k, const void
                           const int32_t* slot, void* cuda_stream) {
   if (ssd_status s = kv8_check(c, layer)) return s;
   if (type != SSD_TYPE_BF16 && type != SSD_TYPE_FP32) return op_fail(SSD_ERR_INVALID_ARG, "type %d", type);
-  if (rows < 0) return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_append: %d rows", rows);
+  if (rows < 0 || rows > 1 << 30) return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_append: %d rows", rows);
   if (rows == 0) return SSD_OK;
   if (!k || !v || !slot) return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_append: null buffer");
   const int size = type == SSD_TYPE_FP32 ? 4 : 2;
@@ -579,7 +914,9 @@ ssd_status ssd_kv8_append(const ssd_kv8* c, int layer, const void* k, const void
   p.v_head = v_head_stride;
   p.slot = slot;
   p.rows = rows;
-  p.window = rows <= 4096 ? 1 : c->block_tokens;
+  // as many CTAs per window as blocks usually begin in it: every block_tokens rows, and with each request
+  const int in_window = rows < kWindow ? rows : kWindow;
+  p.takers = static_cast<int>(in_window / c->block_tokens + static_cast<int64_t>(c->max_batch) * in_window / rows + 1);
   p.shift = log2_of(c->block_tokens);
   p.n_blocks = c->n_blocks;
   p.n_kv_heads = c->n_kv_heads;
@@ -588,9 +925,16 @@ ssd_status ssd_kv8_append(const ssd_kv8* c, int layer, const void* k, const void
   p.scales = c->scales + recs * 2;
   p.status = static_cast<int32_t*>(c->work);
   const bool vec = aligned4(k, size, k_row_stride, k_head_stride) && aligned4(v, size, v_row_stride, v_head_stride);
-  const dim3 grid((rows + p.window - 1) / p.window, (c->n_kv_heads + 1) / 2);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-#define SSD_APPEND(T, D, V) op_launch("ssd_kv8_append", ssd_kv8_append_kernel<T, D, V>, grid, 128, 0, s, p)
+  // A warp per row and head where rows of a block are few (at most the 16 rows of a decode step for every
+  // seat); a warp per 16 tokens of a block else.  112 rows of 16 requests, 40 heads: 7 and 16 us; a prompt of
+  // 640 rows, 32 heads: 60 and 8 us.
+  const bool few = rows <= SSD_MAX_ROWS * c->max_batch;
+  const int per_cta = 128 / c->block_tokens;  // jobs
+  const dim3 grid = few ? dim3(rows, (c->n_kv_heads + 1) / 2)
+                        : dim3((rows + kWindow - 1) / kWindow * p.takers, (2 * c->n_kv_heads + per_cta - 1) / per_cta);
+#define SSD_APPEND(T, D, V) (few ? op_launch("ssd_kv8_append", ssd_kv8_append_rows_kernel<T, D, V>, grid, 128, 0, s, p) \
+                             : op_launch("ssd_kv8_append", ssd_kv8_append_kernel<T, D, V>, grid, 256, 0, s, p))
 #define SSD_APPEND_D(T, V) (c->head_dim == 128 ? SSD_APPEND(T, 128, V) : SSD_APPEND(T, 64, V))
   const ssd_status out = type == SSD_TYPE_FP32 ? (vec ? SSD_APPEND_D(float, true) : SSD_APPEND_D(float, false))
                                                : (vec ? SSD_APPEND_D(__nv_bfloat16, true) : SSD_APPEND_D(__nv_bfloat16, false));
@@ -603,9 +947,11 @@ ssd_status ssd_kv8_read(const ssd_kv8* c, int layer, const int32_t* slot, int n,
                         void* cuda_stream) {
   if (ssd_status s = kv8_check(c, layer)) return s;
   if (type != SSD_TYPE_BF16 && type != SSD_TYPE_FP32) return op_fail(SSD_ERR_INVALID_ARG, "type %d", type);
-  if (n < 0) return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_read: %d slots", n);
+  if (n < 0 || n > 1 << 30) return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_read: %d slots", n);
   if (n == 0) return SSD_OK;
   if (!k || !v || !slot) return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_read: null buffer");
+  if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16)
+    return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_read: k and v must be 16-byte aligned");
   ReadParams p;
   p.slot = slot;
   p.n = n;
@@ -618,14 +964,17 @@ ssd_status ssd_kv8_read(const ssd_kv8* c, int layer, const int32_t* slot, int n,
   p.k = k;
   p.v = v;
   p.status = static_cast<int32_t*>(c->work);
-  const dim3 grid(n, (c->n_kv_heads + 1) / 2);
+  // a tile per warp where that fills the GPU no more than once (latency), else four
+  const int in_window = n < kWindow ? n : kWindow;
+  p.takers = n <= 4096 ? in_window / 16 + 1 : in_window / 64;
+  const dim3 grid((n + kWindow - 1) / kWindow * p.takers, (c->n_kv_heads + 3) / 4);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const char* what = "ssd_kv8_read";
   if (type == SSD_TYPE_FP32)
-    return c->head_dim == 128 ? op_launch(what, ssd_kv8_read_kernel<float, 128>, grid, 128, 0, s, p)
-                              : op_launch(what, ssd_kv8_read_kernel<float, 64>, grid, 128, 0, s, p);
-  return c->head_dim == 128 ? op_launch(what, ssd_kv8_read_kernel<__nv_bfloat16, 128>, grid, 128, 0, s, p)
-                            : op_launch(what, ssd_kv8_read_kernel<__nv_bfloat16, 64>, grid, 128, 0, s, p);
+    return c->head_dim == 128 ? op_launch(what, ssd_kv8_read_kernel<float, 128>, grid, 256, 0, s, p)
+                              : op_launch(what, ssd_kv8_read_kernel<float, 64>, grid, 256, 0, s, p);
+  return c->head_dim == 128 ? op_launch(what, ssd_kv8_read_kernel<__nv_bfloat16, 128>, grid, 256, 0, s, p)
+                            : op_launch(what, ssd_kv8_read_kernel<__nv_bfloat16, 64>, grid, 256, 0, s, p);
 }
 
 ssd_status ssd_kv8_status(const ssd_kv8* c, int* bits, void* cuda_stream) {
