@@ -15,40 +15,43 @@ import torch
 from . import _binding as B
 
 _TYPES = {torch.bfloat16: B.SSD_TYPE_BF16, torch.float32: B.SSD_TYPE_FP32}
+_stream = torch._C._cuda_getCurrentRawStream   # of a device index; the public wrapper makes an object per call
 
 
 def _fail(msg: str):
     raise B.SSDError(1, msg)
 
 
-def _call(fn, *args) -> None:
-    status = fn(*args)
-    if status != 0:
-        raise B.SSDError(status, B.load().ssd_op_last_error().decode())
+def _raise(status: int):
+    raise B.SSDError(status, B.load().ssd_op_last_error().decode())
 
 
-def _stream(device) -> int:
-    return torch._C._cuda_getCurrentRawStream(device.index)
+# The checks below run on every call of a decode loop: they compare whole shapes and device indices.
 
-
-def _type(t: torch.Tensor, what: str) -> int:
-    code = _TYPES.get(t.dtype)
-    if code is None:
-        _fail(f"{what}: bfloat16 or float32 expected, got {t.dtype}")
-    return code
-
-
-def _rows3(t: torch.Tensor, shape: tuple, what: str) -> None:
-    """[rows][heads][dim] with any row and head strides and contiguous elements."""
+def _rows3(t: torch.Tensor, shape: tuple, index: int, what: str) -> tuple:
+    """[rows][heads][dim] with any row and head strides and contiguous elements; returns its strides."""
     if t.shape != shape:
         _fail(f"{what}: shape {shape} expected, got {tuple(t.shape)}")
-    if t.stride(2) != 1 and t.numel():
+    if t.get_device() != index:
+        _fail(f"{what}: on cuda:{index} expected, got {t.device}")
+    st = t.stride()
+    if st[2] != 1 and t.numel():
         _fail(f"{what}: the last dimension must be contiguous")
+    return st
 
 
-def _int32(t: torch.Tensor, n: int, what: str) -> None:
-    if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous() or not t.is_cuda:
-        _fail(f"{what}: a contiguous int32 CUDA tensor of {n} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
+def _int32(t: torch.Tensor, shape: tuple, index: int, what: str) -> int:
+    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        _fail(f"{what}: a contiguous int32 tensor of shape {shape} on cuda:{index} expected, got {t.dtype} "
+              f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _type(dtype: torch.dtype, what: str) -> int:
+    code = _TYPES.get(dtype)
+    if code is None:
+        _fail(f"{what}: bfloat16 or float32 expected, got {dtype}")
+    return code
 
 
 class KV8Step:
@@ -72,6 +75,8 @@ class KV8Step:
         self.row_start = self.data[at:at + batch + 1]
         self.length = self.data[at + batch + 1:at + 2 * batch + 1]
         self.slot = self.data[at + 2 * batch + 1:]
+        self._batch, self._q, self._kv = (batch,), (rows, cache.n_heads, cache.head_dim), (rows, cache.n_kv_heads, cache.head_dim)
+        self._slot = self.slot.data_ptr()
         self._c = B.SSDKv8Step(batch=batch, rows=rows, row_tile=tile, data=self.data.data_ptr())
         self._ref = ctypes.byref(self._c)
 
@@ -112,6 +117,7 @@ class KV8Cache:
         c = self._c
         c.data, c.scales, c.table = self.data.data_ptr(), self.scales.data_ptr(), self.table.data_ptr()
         c.pool, c.work = self.pool.data_ptr(), self.work.data_ptr()
+        self._index, self._state, self._scale = device.index, (1 + max_batch,), 1.0 / math.sqrt(head_dim)
 
     def new_step(self, batch: int, rows: int, rows_per_request: int | None = None) -> KV8Step:
         """A plan's buffer for `rows` new rows of `batch` requests.  rows_per_request: the usual number, if
@@ -122,62 +128,70 @@ class KV8Cache:
              state_out: torch.Tensor | None = None) -> KV8Step:
         """ssd_kv8_plan: hand out blocks for add[b] new rows after length[b] cached ones (-1: give the
         seat's blocks back) and fill `step`.  Updates self.state in place unless told otherwise."""
-        _int32(length, step.batch, "length")
-        _int32(add, step.batch, "add")
+        i = self._index
         state = self.state if state is None else state
-        state_out = state if state_out is None else state_out
-        _int32(state, 1 + self.max_batch, "state")
-        _int32(state_out, 1 + self.max_batch, "state_out")
-        _call(self.lib.ssd_kv8_plan, self._ref, step._ref, length.data_ptr(), add.data_ptr(), state.data_ptr(),
-              state_out.data_ptr(), _stream(self.device))
+        state_in = _int32(state, self._state, i, "state")
+        status = self.lib.ssd_kv8_plan(
+            self._ref, step._ref, _int32(length, step._batch, i, "length"), _int32(add, step._batch, i, "add"), state_in,
+            state_in if state_out is None else _int32(state_out, self._state, i, "state_out"), _stream(i))
+        if status:
+            _raise(status)
         return step
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, step: KV8Step) -> None:
         """ssd_kv8_append: quantise the step's new rows k, v [rows][n_kv_heads][head_dim] into the cache."""
-        shape = (step.rows, self.n_kv_heads, self.head_dim)
-        _rows3(k, shape, "k")
-        _rows3(v, shape, "v")
-        if k.dtype is not v.dtype or k.device != self.device or v.device != self.device:
-            _fail(f"k and v: one type on {self.device} expected, got {k.dtype} on {k.device}, {v.dtype} on {v.device}")
-        ks, vs = k.stride(), v.stride()
-        _call(self.lib.ssd_kv8_append, self._ref, layer, k.data_ptr(), v.data_ptr(), _type(k, "k"), step.rows, ks[0],
-              ks[1], vs[0], vs[1], step.slot.data_ptr(), _stream(self.device))
+        i = self._index
+        ks, vs = _rows3(k, step._kv, i, "k"), _rows3(v, step._kv, i, "v")
+        dtype = k.dtype
+        if v.dtype is not dtype:
+            _fail(f"k and v: one type expected, got {dtype} and {v.dtype}")
+        status = self.lib.ssd_kv8_append(self._ref, layer, k.data_ptr(), v.data_ptr(), _type(dtype, "k"), step.rows, ks[0],
+                                         ks[1], vs[0], vs[1], step._slot, _stream(i))
+        if status:
+            _raise(status)
 
     def read(self, layer: int, slots: torch.Tensor, dtype: torch.dtype = torch.float32):
         """ssd_kv8_read: the (k, v) values held at int32 `slots`, each [n][n_kv_heads][head_dim]."""
-        _int32(slots, slots.shape[0], "slots")
-        out = torch.empty((2, slots.shape[0], self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
-        _call(self.lib.ssd_kv8_read, self._ref, layer, slots.data_ptr(), slots.shape[0], out[0].data_ptr(),
-              out[1].data_ptr(), _type(out, "dtype"), _stream(self.device))
-        return out[0], out[1]
+        i, n = self._index, slots.numel()
+        at, code = _int32(slots, (n,), i, "slots"), _type(dtype, "dtype")
+        shape = (n, self.n_kv_heads, self.head_dim)
+        k = torch.empty(shape, dtype=dtype, device=self.device)
+        v = torch.empty(shape, dtype=dtype, device=self.device)
+        status = self.lib.ssd_kv8_read(self._ref, layer, at, n, k.data_ptr(), v.data_ptr(), code, _stream(i))
+        if status:
+            _raise(status)
+        return k, v
 
     def attention(self, layer: int, q: torch.Tensor, step: KV8Step, out: torch.Tensor | None = None,
                   scale: float | None = None, row_mask: torch.Tensor | None = None) -> torch.Tensor:
         """ssd_kv8_attention: softmax(scale q k^T) v of the step's rows q [rows][n_heads][head_dim] over
         their requests' cached tokens and, causally or by row_mask (int32 bits, [rows]), the step's own
         rows.  scale defaults to 1 / sqrt(head_dim)."""
-        shape = (step.rows, self.n_heads, self.head_dim)
-        _rows3(q, shape, "q")
+        i = self._index
+        qs, dtype = _rows3(q, step._q, i, "q"), q.dtype
         if out is None:
-            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+            out = torch.empty(step._q, dtype=dtype, device=self.device)
+            os = out.stride()
         else:
-            _rows3(out, shape, "out")
-        if q.device != self.device or out.device != self.device or out.dtype is not q.dtype:
-            _fail(f"q and out: one type on {self.device} expected, got {q.dtype} on {q.device}, {out.dtype} on {out.device}")
-        if row_mask is not None:
-            _int32(row_mask, step.rows, "row_mask")
-        qs, os = q.stride(), out.stride()
-        _call(self.lib.ssd_kv8_attention, self._ref, layer, step._ref, q.data_ptr(), out.data_ptr(), _type(q, "q"),
-              qs[0], qs[1], os[0], os[1], 1.0 / math.sqrt(self.head_dim) if scale is None else scale,
-              None if row_mask is None else row_mask.data_ptr(), _stream(self.device))
+            os = _rows3(out, step._q, i, "out")
+            if out.dtype is not dtype:
+                _fail(f"q and out: one type expected, got {dtype} and {out.dtype}")
+        status = self.lib.ssd_kv8_attention(
+            self._ref, layer, step._ref, q.data_ptr(), out.data_ptr(), _type(dtype, "q"), qs[0], qs[1], os[0], os[1],
+            self._scale if scale is None else scale,
+            None if row_mask is None else _int32(row_mask, (step.rows,), i, "row_mask"), _stream(i))
+        if status:
+            _raise(status)
         return out
 
     def check(self) -> None:
         """Wait for the stream and raise SSDError if a call met bad lengths, slots or values (ssd_kv8_status)."""
-        _call(self.lib.ssd_kv8_status, self._ref, None, _stream(self.device))
+        status = self.lib.ssd_kv8_status(self._ref, None, _stream(self._index))
+        if status:
+            _raise(status)
 
 
-_w4_work: dict = {}   # (device, stream) -> workspace: products on different streams must not share one
+_w4_work: dict = {}   # (device, stream) -> workspace (pointer, size, tensor): streams must not share one
 
 
 class W4Weight:
@@ -193,38 +207,52 @@ class W4Weight:
         if size < 0:
             _fail(self.lib.ssd_op_last_error().decode())
         self._work = self.lib.ssd_w4_work_bytes(self.n, self.k)
+        self._index = weight.get_device()
         self.packed = torch.empty(size, dtype=torch.uint8, device=weight.device)
-        _call(self.lib.ssd_w4_pack, weight.data_ptr(), _type(weight, "weight"), self.n, self.k, weight.stride(0),
-              group, self.packed.data_ptr(), _stream(self.device))
+        self._packed = self.packed.data_ptr()
+        status = self.lib.ssd_w4_pack(weight.data_ptr(), _type(weight.dtype, "weight"), self.n, self.k, weight.stride(0),
+                                      group, self._packed, _stream(self._index))
+        if status:
+            _raise(status)
 
     def dequantize(self) -> torch.Tensor:
         """The fp32 values [n][k] the packed codes stand for."""
         out = torch.empty((self.n, self.k), dtype=torch.float32, device=self.device)
-        _call(self.lib.ssd_w4_unpack, self.packed.data_ptr(), self.n, self.k, self.group, out.data_ptr(),
-              _stream(self.device))
+        status = self.lib.ssd_w4_unpack(self._packed, self.n, self.k, self.group, out.data_ptr(), _stream(self._index))
+        if status:
+            _raise(status)
         return out
+
+    def _rows(self, t: torch.Tensor, shape: tuple, dtype: torch.dtype, what: str) -> int:
+        """Row stride of a [rows][columns] tensor with contiguous rows."""
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index:
+            _fail(f"{what}: {dtype} {shape} on {self.device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        st = t.stride()
+        if st[1] != 1 and shape[1] > 1:
+            _fail(f"{what}: contiguous rows expected")
+        return st[0]
 
     def matmul(self, x: torch.Tensor, out: torch.Tensor | None = None,
                residual: torch.Tensor | None = None) -> torch.Tensor:
         """x W^T (+ residual) for x [rows][k] in bfloat16 or float32, rows <= 16 (ssd_w4_matmul)."""
-        if x.dim() != 2 or x.shape[1] != self.k or x.stride(1) != 1:
-            _fail(f"x: [rows][{self.k}] with contiguous rows expected, got {tuple(x.shape)}")
-        rows = x.shape[0]
+        if x.dim() != 2:
+            _fail(f"x: [rows][{self.k}] expected, got {tuple(x.shape)}")
+        rows, dtype, i = x.shape[0], x.dtype, self._index
+        xs, code = self._rows(x, (rows, self.k), dtype, "x"), _type(dtype, "x")
         if out is None:
-            out = torch.empty((rows, self.n), dtype=x.dtype, device=x.device)
-        for t, what in ((out, "out"), (residual, "residual")):
-            if t is None:
-                continue
-            if t.shape != (rows, self.n) or t.dtype is not x.dtype or t.device != x.device or \
-                    (t.stride(1) != 1 and self.n > 1):
-                _fail(f"{what}: {x.dtype} [{rows}][{self.n}] with contiguous rows expected")
-        if x.device != self.device:
-            _fail(f"x: on {x.device}, the weight is on {self.device}")
-        stream = _stream(self.device)
-        work = _w4_work.get((self.device, stream))
-        if work is None or work.numel() < self._work:
-            work = _w4_work[(self.device, stream)] = torch.zeros(self._work, dtype=torch.uint8, device=self.device)
-        _call(self.lib.ssd_w4_matmul, self.packed.data_ptr(), self.n, self.k, self.group, x.data_ptr(), _type(x, "x"),
-              rows, x.stride(0), out.data_ptr(), out.stride(0), None if residual is None else residual.data_ptr(),
-              0 if residual is None else residual.stride(0), work.data_ptr(), stream)
+            out = torch.empty((rows, self.n), dtype=dtype, device=self.device)
+            os = self.n
+        else:
+            os = self._rows(out, (rows, self.n), dtype, "out")
+        stream = _stream(i)
+        work = _w4_work.get((i, stream))
+        if work is None or work[1] < self._work:
+            t = torch.empty(self._work, dtype=torch.uint8, device=self.device)
+            work = _w4_work[(i, stream)] = (t.data_ptr(), self._work, t)
+        status = self.lib.ssd_w4_matmul(
+            self._packed, self.n, self.k, self.group, x.data_ptr(), code, rows, xs, out.data_ptr(), os,
+            None if residual is None else residual.data_ptr(),
+            0 if residual is None else self._rows(residual, (rows, self.n), dtype, "residual"), work[0], stream)
+        if status:
+            _raise(status)
         return out
