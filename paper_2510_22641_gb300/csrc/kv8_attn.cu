@@ -44,19 +44,17 @@ struct Kv8AttnParams {
   float* part;        // [2 * teams][8 NB][D] states, then [2 * teams][8 NB][2] (maximum, sum)
 };
 
-// Launch shape by rows per item.  Up to 8 rows: query fragments in registers, 128 registers a thread, 16
-// warps per SM.  More rows: query fragments in shared memory (one copy per team, so at most kTeams of
-// them), as many warps as the accumulators leave registers for.
+// Up to 8 rows: query fragments in registers.  More: in shared memory, one copy per team.
 template <int D, int NB>
 struct Geo {
-  static constexpr AttnShape kShape = attn_shape(8 * NB);
+  static constexpr AttnShape kShape = attn_shape(8 * NB, D);
   static constexpr int kWarps = kShape.warps;
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kCtas = kShape.ctas;
   static constexpr bool kSharedQ = NB > 1;
   static constexpr int kTeams = kShape.teams;
   static constexpr int kTile = 32 * D;                      // bytes of 16 tokens, K and V: one step
-  static constexpr int kRing = NB >= 3 ? 20480 : 12288;     // per warp
+  static constexpr int kRing = kCtas == 2 && kSharedQ ? 10240 : kWarps * kCtas > 8 ? 12288 : 20480;  // per warp
   static constexpr int kStages = kRing / kTile;
   static constexpr int kStat = kWarps * kRing;              // (maximum, sum, unit) of 8 rows per warp
   static constexpr int kOff = kStat + kWarps * 8 * 16;      // where each warp's merge record lies
@@ -684,11 +682,13 @@ extern "C" {
 
 int64_t ssd_kv8_work_bytes(const ssd_kv8* c) {
   if (!kv8_shape_ok(c)) return -1;
-  // two partial states per team, [8 NB][D] and a (maximum, sum) per row: most for 24 rows and 4 teams
-  auto bytes = [&](int rows, int64_t teams) { return 2 * teams * rows * (c->head_dim + 2) * 4; };
-  int64_t most = bytes(8, 2 * kAttnSms * 8);
-  if (bytes(24, kAttnSms * 4) > most) most = bytes(24, kAttnSms * 4);
-  if (bytes(32, kAttnSms * 2) > most) most = bytes(32, kAttnSms * 2);
+  // two partial states per team, [rows][D] and a (maximum, sum) per row
+  int64_t most = 0;
+  for (int rows = 8; rows <= 32; rows += 8) {
+    const AttnShape sh = attn_shape(rows, c->head_dim);
+    const int64_t bytes = 2ll * kAttnSms * sh.ctas * sh.teams * rows * (c->head_dim + 2) * 4;
+    most = bytes > most ? bytes : most;
+  }
   return kKv8WorkHead * 4 + kAttnMaxTeams * 4 + most;
 }
 

@@ -55,7 +55,7 @@ constexpr int kPlanPer = SSD_KV8_MAX_BATCH / kPlanThreads;
 
 struct PlanParams {
   int batch, rows, max_batch, max_blocks, n_blocks, shift;  // block_tokens = 1 << shift
-  int n_kv_heads, group, row_tile;
+  int n_kv_heads, group, row_tile, dim;
   const int32_t *len, *add, *state_in;
   int32_t *state_out, *table, *pool, *step, *status, *ticket;
 };
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(kPlanThreads) ssd_kv8_plan_kernel(const PlanPa
   {
     const int n_segs = seg_s[p.batch];
     const int64_t all = work_s[p.batch];
-    const AttnShape sh = attn_shape(p.row_tile);
+    const AttnShape sh = attn_shape(p.row_tile, p.dim);
     const int ctas = kAttnSms * sh.ctas;
     // Short contexts, a CTA for each: one segment per team, whatever its length, so that nothing is
     // merged through global memory (64 tiles take one SM about as long as that merge).
@@ -876,6 +876,7 @@ ssd_status ssd_kv8_plan(const ssd_kv8* c, const ssd_kv8_step* step, const int32_
   p.n_kv_heads = c->n_kv_heads;
   p.group = c->n_heads / c->n_kv_heads;
   p.row_tile = step_row_tile(c, step);
+  p.dim = c->head_dim;
   p.len = len;
   p.add = add;
   p.state_in = state_in;
@@ -886,7 +887,7 @@ ssd_status ssd_kv8_plan(const ssd_kv8* c, const ssd_kv8_step* step, const int32_
   p.status = static_cast<int32_t*>(c->work);
   p.ticket = p.status + 1;
   // a thread per team of the attention's partition, or per four rows
-  const AttnShape sh = attn_shape(p.row_tile);
+  const AttnShape sh = attn_shape(p.row_tile, p.dim);
   const int teams = (kAttnSms * sh.ctas * sh.teams + kPlanThreads - 1) / kPlanThreads;
   int grid = (step->rows + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
   grid = grid < teams + 3 ? teams + 3 : grid > kAttnSms ? kAttnSms : grid;
