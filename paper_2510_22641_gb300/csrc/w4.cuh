@@ -67,12 +67,14 @@ struct W4Params {
   int each, more;     // row tiles per team, teams that have one more
 };
 
-template <int NB, int MT>
+template <int PARTS, int NB, int MT>
 struct W4Geo {
-  static constexpr int kCtas = NB == 1 ? 2 : 1;        // per SM
-  static constexpr int kStages = NB == 1 ? 9 : 18;     // records
+  static constexpr int kCtas = PARTS * NB <= 2 ? 2 : 1;             // per SM
+  static constexpr int kStages = kCtas == 1 ? 18 : NB == 1 ? 9 : 8;  // records
+  // whether the next chunk's activations are fetched ahead (registers: 16 a part and 8 rows)
+  static constexpr bool kAhead = PARTS * NB == 1 || PARTS * NB == 4;
   static constexpr int kRing = kStages * kW4MaxRec;    // per warp
-  static constexpr int kPart = MT > 4 ? MT / 2 : MT;   // tiles merged at a time
+  static constexpr int kPart = MT > 4 ? MT / 2 : NB == 2 && MT > 2 ? 2 : MT;  // tiles merged at a time
   static constexpr int kPad = 16 * kPart + 4;
   static constexpr int kSum = kW4Warps * kRing;
   static constexpr int kTotal = kSum + kW4Warps * 8 * NB * kPad * 4;
@@ -127,10 +129,10 @@ __device__ __forceinline__ void w4_operand(uint32_t w, uint32_t (&a)[4]) {
 
 // T: type of y and the residual.  bf16: bf16 operands; float: pairs of halves.
 template <typename T, int NB, int MT, int per>  // per: groups in a chunk
-__global__ void __launch_bounds__(kW4Threads, W4Geo<NB, MT>::kCtas) ssd_w4_matmul_kernel(const W4Params p) {
+__global__ void __launch_bounds__(kW4Threads, W4Geo<sizeof(T) / 2, NB, MT>::kCtas) ssd_w4_matmul_kernel(const W4Params p) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
   constexpr bool BF16 = PARTS == 1;
-  using G = W4Geo<NB, MT>;
+  using G = W4Geo<PARTS, NB, MT>;
   extern __shared__ __align__(128) uint8_t smem[];
   if constexpr (BF16) pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -193,7 +195,7 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<NB, MT>::kCtas) ssd_w4_matmu
 
   float* sum_s = reinterpret_cast<float*>(smem + G::kSum);
   Rows cur, next;
-  load_x(next, wt);
+  if constexpr (G::kAhead) load_x(next, wt);
   for (int tile0 = tile_begin; tile0 < tile_end; tile0 += MT) {
     const int cnt = min(MT, tile_end - tile0);
     float y[MT][NB][4];
@@ -202,8 +204,12 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<NB, MT>::kCtas) ssd_w4_matmu
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) y[mt][nb][0] = y[mt][nb][1] = y[mt][nb][2] = y[mt][nb][3] = 0.0f;
     for (int chunk = wt; chunk < n_c; chunk += W) {
-      cur = next;
-      load_x(next, chunk + W < n_c ? chunk + W : wt);  // (the next pass begins again)
+      if constexpr (G::kAhead) {
+        cur = next;
+        load_x(next, chunk + W < n_c ? chunk + W : wt);  // (the next pass begins again)
+      } else {
+        load_x(cur, chunk);
+      }
       // what the constant offset of the codes adds, per group
       float off[4][NB][2];
       if constexpr (BF16) {
@@ -288,6 +294,7 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<NB, MT>::kCtas) ssd_w4_matmu
           if (r < p.rows)
 #pragma unroll
             for (int mt = 0; mt < G::kPart; ++mt) {
+              if (m0 + mt >= MT) break;
               mine[r * G::kPad + 16 * mt + g] = y[m0 + mt][nb][e];
               mine[r * G::kPad + 16 * mt + g + 8] = y[m0 + mt][nb][e + 2];
             }
@@ -318,7 +325,7 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<NB, MT>::kCtas) ssd_w4_matmu
 
 template <typename T, int NB, int MT, int PER>
 ssd_status w4_launch(W4Params p, cudaStream_t s) {
-  using G = W4Geo<NB, MT>;
+  using G = W4Geo<sizeof(T) / 2, NB, MT>;
   static std::atomic<uint64_t> ready{0};
   if (ssd_status e = op_smem(ssd_w4_matmul_kernel<T, NB, MT, PER>, G::kTotal, ready, "ssd_w4_matmul")) return e;
   const int tiles = (p.n + 15) / 16, per_cta = kW4Warps >> p.log_warps, most = kW4Sms * G::kCtas;
@@ -333,7 +340,7 @@ template <typename T, int NB, int PER>
 ssd_status w4_launch_tiles(const W4Params& p, cudaStream_t s) {
   // the most tiles a team gets, in the fewest passes of at most kMost, evenly
   constexpr int kMost = NB == 1 ? 8 : 4;
-  const int teams = kW4Sms * W4Geo<NB, 1>::kCtas * (kW4Warps >> p.log_warps);
+  const int teams = kW4Sms * W4Geo<sizeof(T) / 2, NB, 1>::kCtas * (kW4Warps >> p.log_warps);
   const int tiles = ((p.n + 15) / 16 + teams - 1) / teams, passes = (tiles + kMost - 1) / kMost;
   const int mt = (tiles + passes - 1) / passes;
   if constexpr (NB == 1) {
