@@ -500,7 +500,7 @@ typedef struct {
   void* work;
 } ssd_kv8;
 
-/* What one step works on, filled by ssd_kv8_plan: device int32, ssd_kv8_step_ints() of them, 16-byte aligned, in this order:
+/* What one step works on, filled by ssd_kv8_plan for the cache that its calls then get: device int32, ssd_kv8_step_ints() of them, 16-byte aligned, in this order:
  *   the attention's partition, SSD_KV8_STEP_HEAD ints, then
  *   seg_start  [batch + 1] prefix sums of the attention's items per request
  *   row_start  [batch + 1] prefix sums of the requests' new rows (rows of request b: row_start[b] ..)

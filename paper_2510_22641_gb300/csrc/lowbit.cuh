@@ -141,7 +141,7 @@ inline bool kv8_shape_ok(const ssd_kv8* c) {
   // slots, row numbers and positions fit 31 bits, with room to add a tile
   const int64_t lim = 1 << 30;
   const int64_t cap = static_cast<int64_t>(c->max_blocks) * c->block_tokens;
-  if (static_cast<int64_t>(c->n_blocks) * c->block_tokens > lim || cap > lim || c->n_heads > 65535) return false;
+  if (static_cast<int64_t>(c->n_blocks) * c->block_tokens > lim || cap > lim || c->n_heads > 16384) return false;
   if (static_cast<int64_t>(c->n_blocks) * (c->block_tokens / 16) * c->n_kv_heads > lim) return false;
   return cap * c->max_batch <= 0x7fffffff;
 }

@@ -228,7 +228,8 @@ ssd_status ssd_w4_matmul(const void* packed, int n, int k, int group, const void
       return e;
   }
   const int per = kChunk / group;
-  if (type == SSD_TYPE_FP32) return rows <= 8 ? w4_matmul_fp32_8(per, p, s) : w4_matmul_fp32_16(per, p, s);
+  if (type == SSD_TYPE_FP32)
+    return rows <= 4 ? w4_matmul_fp32_4(per, p, s) : rows <= 8 ? w4_matmul_fp32_8(per, p, s) : w4_matmul_fp32_16(per, p, s);
   return rows <= 8 ? w4_matmul_bf16_8(per, p, s) : w4_matmul_bf16_16(per, p, s);
 }
 

@@ -127,11 +127,17 @@ __device__ __forceinline__ void w4_operand(uint32_t w, uint32_t (&a)[4]) {
   }
 }
 
-// T: type of y and the residual.  bf16: bf16 operands; float: pairs of halves.
-template <typename T, int NB, int MT, int per>  // per: groups in a chunk
-__global__ void __launch_bounds__(kW4Threads, W4Geo<sizeof(T) / 2, NB, MT>::kCtas) ssd_w4_matmul_kernel(const W4Params p) {
-  constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
-  constexpr bool BF16 = PARTS == 1;
+// Parts of a row that are operands of their own products.
+template <typename T, bool PAIR>
+constexpr int kW4Parts = sizeof(T) == 4 && !PAIR ? 2 : 1;
+
+// T: type of y and the residual.  bf16: bf16 operands; float: pairs of halves.  PAIR: up to four fp32 rows,
+// whose high and low halves are columns r and r + 4 of one product.  per: groups in a chunk.
+template <typename T, int NB, int MT, int per, bool PAIR>
+__global__ void __launch_bounds__(kW4Threads, W4Geo<kW4Parts<T, PAIR>, NB, MT>::kCtas) ssd_w4_matmul_kernel(const W4Params p) {
+  constexpr int PARTS = kW4Parts<T, PAIR>;
+  constexpr bool BF16 = sizeof(T) == 2;
+  static_assert(!PAIR || (NB == 1 && !BF16), "four rows of halves fill one block of columns");
   using G = W4Geo<PARTS, NB, MT>;
   extern __shared__ __align__(128) uint8_t smem[];
   if constexpr (BF16) pdl_wait();
@@ -181,15 +187,15 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<sizeof(T) / 2, NB, MT>::kCta
     if (chunk >= n_c) return;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const int row = nb * 8 + g;
+      const int row = PAIR ? g & 3 : nb * 8 + g;
 #pragma unroll
       for (int k = 0; k < PARTS; ++k) {
-        const uint16_t* src = p.x + k * p.x_part + row * p.x_row + static_cast<int64_t>(chunk) * kChunk + 8 * t;
+        const uint16_t* src = p.x + (PAIR ? g >> 2 : k) * p.x_part + row * p.x_row + static_cast<int64_t>(chunk) * kChunk + 8 * t;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           r.x[nb][k][i] = row < p.rows ? *reinterpret_cast<const uint4*>(src + 32 * i) : make_uint4(0, 0, 0, 0);
       }
-      if constexpr (!BF16) r.scale[nb] = *reinterpret_cast<const float2*>(p.x_scale + chunk * 16 + nb * 8 + 2 * t);
+      if constexpr (!BF16) r.scale[nb] = *reinterpret_cast<const float2*>(p.x_scale + chunk * 16 + (PAIR ? 2 * t & 3 : nb * 8 + 2 * t));
     }
   };
 
@@ -291,7 +297,7 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<sizeof(T) / 2, NB, MT>::kCta
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int r = nb * 8 + 2 * t + e;
-          if (r < p.rows)
+          if ((PAIR ? r & 3 : r) < p.rows)
 #pragma unroll
             for (int mt = 0; mt < G::kPart; ++mt) {
               if (m0 + mt >= MT) break;
@@ -305,10 +311,12 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<sizeof(T) / 2, NB, MT>::kCta
         const int r = i / (4 * G::kPart), col = i % (4 * G::kPart) * 4;
         if (col >= width) continue;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int w = 0; w < W; ++w) {
-          const float4 z = *reinterpret_cast<const float4*>(sum_s + ((sub * W + w) * 8 * NB + r) * G::kPad + col);
-          v.x += z.x, v.y += z.y, v.z += z.z, v.w += z.w;
-        }
+        for (int w = 0; w < W; ++w)
+#pragma unroll
+          for (int q = PAIR ? 4 : 0; q >= 0; q -= 4) {  // low halves first
+            const float4 z = *reinterpret_cast<const float4*>(sum_s + ((sub * W + w) * 8 * NB + r + q) * G::kPad + col);
+            v.x += z.x, v.y += z.y, v.z += z.z, v.w += z.w;
+          }
         const float e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -323,46 +331,47 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<sizeof(T) / 2, NB, MT>::kCta
   cp_async_wait_all();
 }
 
-template <typename T, int NB, int MT, int PER>
+template <typename T, int NB, int MT, int PER, bool PAIR>
 ssd_status w4_launch(W4Params p, cudaStream_t s) {
-  using G = W4Geo<sizeof(T) / 2, NB, MT>;
+  using G = W4Geo<kW4Parts<T, PAIR>, NB, MT>;
   static std::atomic<uint64_t> ready{0};
-  if (ssd_status e = op_smem(ssd_w4_matmul_kernel<T, NB, MT, PER>, G::kTotal, ready, "ssd_w4_matmul")) return e;
+  if (ssd_status e = op_smem(ssd_w4_matmul_kernel<T, NB, MT, PER, PAIR>, G::kTotal, ready, "ssd_w4_matmul")) return e;
   const int tiles = (p.n + 15) / 16, per_cta = kW4Warps >> p.log_warps, most = kW4Sms * G::kCtas;
   int grid = (tiles + per_cta - 1) / per_cta;
   grid = grid < most ? grid : most;
   p.each = tiles / (grid * per_cta);
   p.more = tiles % (grid * per_cta);
-  return op_launch("ssd_w4_matmul", ssd_w4_matmul_kernel<T, NB, MT, PER>, dim3(grid), kW4Threads, G::kTotal, s, p);
+  return op_launch("ssd_w4_matmul", ssd_w4_matmul_kernel<T, NB, MT, PER, PAIR>, dim3(grid), kW4Threads, G::kTotal, s, p);
 }
 
-template <typename T, int NB, int PER>
+template <typename T, int NB, int PER, bool PAIR>
 ssd_status w4_launch_tiles(const W4Params& p, cudaStream_t s) {
   // the most tiles a team gets, in the fewest passes of at most kMost, evenly
   constexpr int kMost = NB == 1 ? 8 : 4;
-  const int teams = kW4Sms * W4Geo<sizeof(T) / 2, NB, 1>::kCtas * (kW4Warps >> p.log_warps);
+  const int teams = kW4Sms * W4Geo<kW4Parts<T, PAIR>, NB, 1>::kCtas * (kW4Warps >> p.log_warps);
   const int tiles = ((p.n + 15) / 16 + teams - 1) / teams, passes = (tiles + kMost - 1) / kMost;
   const int mt = (tiles + passes - 1) / passes;
   if constexpr (NB == 1) {
-    if (mt > 6) return w4_launch<T, NB, 8, PER>(p, s);
-    if (mt > 4) return w4_launch<T, NB, 6, PER>(p, s);
+    if (mt > 6) return w4_launch<T, NB, 8, PER, PAIR>(p, s);
+    if (mt > 4) return w4_launch<T, NB, 6, PER, PAIR>(p, s);
   }
-  return mt > 3 ? w4_launch<T, NB, 4, PER>(p, s)
-         : mt > 2 ? w4_launch<T, NB, 3, PER>(p, s)
-         : mt > 1 ? w4_launch<T, NB, 2, PER>(p, s)
-                  : w4_launch<T, NB, 1, PER>(p, s);
+  return mt > 3 ? w4_launch<T, NB, 4, PER, PAIR>(p, s)
+         : mt > 2 ? w4_launch<T, NB, 3, PER, PAIR>(p, s)
+         : mt > 1 ? w4_launch<T, NB, 2, PER, PAIR>(p, s)
+                  : w4_launch<T, NB, 1, PER, PAIR>(p, s);
 }
 
-template <typename T, int NB>
+template <typename T, int NB, bool PAIR = false>
 ssd_status w4_launch_group(int per, const W4Params& p, cudaStream_t s) {
-  return per == 1   ? w4_launch_tiles<T, NB, 1>(p, s)
-         : per == 2 ? w4_launch_tiles<T, NB, 2>(p, s)
-                    : w4_launch_tiles<T, NB, 4>(p, s);
+  return per == 1   ? w4_launch_tiles<T, NB, 1, PAIR>(p, s)
+         : per == 2 ? w4_launch_tiles<T, NB, 2, PAIR>(p, s)
+                    : w4_launch_tiles<T, NB, 4, PAIR>(p, s);
 }
 
-// One translation unit each: products of bf16 / fp32 rows, up to 8 or 16 of them.
+// One translation unit each: products of bf16 / fp32 rows, up to so many of them.
 ssd_status w4_matmul_bf16_8(int per, const W4Params& p, cudaStream_t s);
 ssd_status w4_matmul_bf16_16(int per, const W4Params& p, cudaStream_t s);
+ssd_status w4_matmul_fp32_4(int per, const W4Params& p, cudaStream_t s);
 ssd_status w4_matmul_fp32_8(int per, const W4Params& p, cudaStream_t s);
 ssd_status w4_matmul_fp32_16(int per, const W4Params& p, cudaStream_t s);
 

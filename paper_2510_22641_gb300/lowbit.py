@@ -64,7 +64,7 @@ class KV8Step:
         n = B.load().ssd_kv8_step_ints(batch, rows)
         if n < 0 or batch > cache.max_batch:
             _fail(f"step of {rows} rows of {batch} requests (the cache has {cache.max_batch} seats)")
-        self.batch, self.rows = batch, rows
+        self.batch, self.rows, self.cache = batch, rows, cache
         self.data = torch.zeros(n, dtype=torch.int32, device=cache.device)
         tile = 0
         if rows_per_request is not None:
@@ -129,6 +129,8 @@ class KV8Cache:
         """ssd_kv8_plan: hand out blocks for add[b] new rows after length[b] cached ones (-1: give the
         seat's blocks back) and fill `step`.  Updates self.state in place unless told otherwise."""
         i = self._index
+        if step.cache is not self:
+            _fail("the step was made for another cache")
         state = self.state if state is None else state
         state_in = _int32(state, self._state, i, "state")
         status = self.lib.ssd_kv8_plan(
@@ -168,6 +170,8 @@ class KV8Cache:
         their requests' cached tokens and, causally or by row_mask (int32 bits, [rows]), the step's own
         rows.  scale defaults to 1 / sqrt(head_dim)."""
         i = self._index
+        if step.cache is not self:
+            _fail("the step was made for another cache")
         qs, dtype = _rows3(q, step._q, i, "q"), q.dtype
         if out is None:
             out = torch.empty(step._q, dtype=dtype, device=self.device)

@@ -497,7 +497,9 @@ def test_wrapper_refusals():
              lambda: c.append(0, good_kv.transpose(1, 2).contiguous().transpose(1, 2), good_kv, step),
              lambda: c.attention(0, good_kv, step), lambda: c.attention(0, good_q, step, out=good_q.bfloat16()),
              lambda: c.attention(0, good_q, step, row_mask=ints([1, 2])), lambda: c.attention(-1, good_q, step),
-             lambda: c.read(0, l.long()), lambda: c.read(0, l, torch.float16)]
+             lambda: c.read(0, l.long()), lambda: c.read(0, l, torch.float16),
+             lambda: lib.KV8Cache(1, 4, 2, 64, 16, 8, 2, 4).plan(step, l, a),
+             lambda: lib.KV8Cache(1, 4, 2, 64, 16, 8, 2, 4).attention(0, good_q, step)]
     for i, f in enumerate(calls):
         with pytest.raises(lib.SSDError) as e:
             f()
