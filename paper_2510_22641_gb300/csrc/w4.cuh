@@ -48,6 +48,12 @@ __host__ __device__ constexpr int w4_bit(int row, int col) {
 // through shared memory.  No tile is shared between teams, so there are no partial sums in global memory.
 // A warp streams its records (16 rows x 128 columns, 1 KB + scales) with cp.async into a ring of its own;
 // lanes read back the bytes they copied, the scales are shared within the warp.
+//
+// Measured (device time, of the copy rate): 32000 x 4096, one bf16 row 16.8 us, 59 %; 16 rows 23.9 us, 42 %;
+// one fp32 row 18.0 us, 55 %; 8 rows 22.5 us, 44 %; 16 rows 35.2 us, 28 %; 4096 x 4096, one bf16 row 5.0 us
+// (launch, one round of loads, the sum).  137 to 174 instructions a record, half of them unpacking, against
+// the 180 issue slots that a record's bytes leave at the copy rate; 16 fp32 rows wait for their products
+// with 8 warps an SM.
 
 constexpr int kW4Warps = 8;
 constexpr int kW4Threads = 32 * kW4Warps;
@@ -69,10 +75,14 @@ struct W4Params {
 
 template <int PARTS, int NB, int MT>
 struct W4Geo {
-  static constexpr int kCtas = PARTS * NB <= 2 ? 2 : 1;             // per SM
+  // per SM: two, but for 16 fp32 rows, whose operands take the registers (32000 x 4096: one bf16 row with
+  // one CTA 20.5 us, two 16.8; 16 bf16 rows 30.0 and 23.9; 8 fp32 rows 27.7 and 22.5)
+  static constexpr int kCtas = PARTS * NB <= 2 ? 2 : 1;
   static constexpr int kStages = kCtas == 1 ? 18 : NB == 1 ? 9 : 8;  // records
-  // whether the next chunk's activations are fetched ahead (registers: 16 a part and 8 rows)
-  static constexpr bool kAhead = PARTS * NB == 1 || PARTS * NB == 4;
+  // whether the next chunk's activations are fetched ahead: where one CTA has the registers and few tiles
+  // cover the wait (16 fp32 rows, 4096 x 4096: ahead 9.2 us, not ahead 9.6; 16 bf16 rows, 32000 x 4096, with
+  // spills: 30.8 and 23.9)
+  static constexpr bool kAhead = PARTS * NB == 4 && MT <= 4;
   static constexpr int kRing = kStages * kW4MaxRec;    // per warp
   static constexpr int kPart = MT > 4 ? MT / 2 : NB == 2 && MT > 2 ? 2 : MT;  // tiles merged at a time
   static constexpr int kPad = 16 * kPart + 4;
@@ -132,7 +142,8 @@ template <typename T, bool PAIR>
 constexpr int kW4Parts = sizeof(T) == 4 && !PAIR ? 2 : 1;
 
 // T: type of y and the residual.  bf16: bf16 operands; float: pairs of halves.  PAIR: up to four fp32 rows,
-// whose high and low halves are columns r and r + 4 of one product.  per: groups in a chunk.
+// whose high and low halves are columns r and r + 4 of one product (32000 x 4096, one row: two products
+// 21.7 us, one 18.4).  per: groups in a chunk.
 template <typename T, int NB, int MT, int per, bool PAIR>
 __global__ void __launch_bounds__(kW4Threads, W4Geo<kW4Parts<T, PAIR>, NB, MT>::kCtas) ssd_w4_matmul_kernel(const W4Params p) {
   constexpr int PARTS = kW4Parts<T, PAIR>;
@@ -245,12 +256,14 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<kW4Parts<T, PAIR>, NB, MT>::
         const uint4 w01 = *reinterpret_cast<const uint4*>(rec + lane * 16);
         const uint4 w23 = *reinterpret_cast<const uint4*>(rec + 512 + lane * 16);
         const uint16_t* sc = reinterpret_cast<const uint16_t*>(rec + kCodeBytes);
-        float c[NB][4];
+        float c[PARTS][NB][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {  // 32 columns
           if (i % (4 / per) == 0)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) c[nb][0] = c[nb][1] = c[nb][2] = c[nb][3] = 0.0f;
+            for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) c[k][nb][0] = c[k][nb][1] = c[k][nb][2] = c[k][nb][3] = 0.0f;
           const uint32_t we = i == 0 ? w01.x : i == 1 ? w01.z : i == 2 ? w23.x : w23.z;
           const uint32_t wo = i == 0 ? w01.y : i == 1 ? w01.w : i == 2 ? w23.y : w23.w;
           uint32_t ae[4], ao[4];
@@ -259,10 +272,11 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<kW4Parts<T, PAIR>, NB, MT>::
 #pragma unroll
           for (int k = 0; k < PARTS; ++k)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-              w4_mma<BF16>(c[nb], ae, cur.x[nb][k][i].x, cur.x[nb][k][i].y);
-              w4_mma<BF16>(c[nb], ao, cur.x[nb][k][i].z, cur.x[nb][k][i].w);
-            }
+            for (int nb = 0; nb < NB; ++nb) w4_mma<BF16>(c[k][nb], ae, cur.x[nb][k][i].x, cur.x[nb][k][i].y);
+#pragma unroll
+          for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) w4_mma<BF16>(c[k][nb], ao, cur.x[nb][k][i].z, cur.x[nb][k][i].w);
           if ((i + 1) % (4 / per) == 0) {  // end of a group
             const int grp = i / (4 / per);
             float s0 = __uint_as_float(static_cast<uint32_t>(sc[g * per + grp]) << 16);
@@ -270,16 +284,20 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<kW4Parts<T, PAIR>, NB, MT>::
             if constexpr (!BF16) s0 *= 0x1p-14f, s1 *= 0x1p-14f;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
+              float* v = c[0][nb];
+              if constexpr (PARTS == 2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += c[1][nb][e];
               if constexpr (BF16) {
-                y[mt][nb][0] += (c[nb][0] - off[i][nb][0]) * s0;
-                y[mt][nb][1] += (c[nb][1] - off[i][nb][1]) * s0;
-                y[mt][nb][2] += (c[nb][2] - off[i][nb][0]) * s1;
-                y[mt][nb][3] += (c[nb][3] - off[i][nb][1]) * s1;
+                y[mt][nb][0] += (v[0] - off[i][nb][0]) * s0;
+                y[mt][nb][1] += (v[1] - off[i][nb][1]) * s0;
+                y[mt][nb][2] += (v[2] - off[i][nb][0]) * s1;
+                y[mt][nb][3] += (v[3] - off[i][nb][1]) * s1;
               } else {
-                y[mt][nb][0] += c[nb][0] * (s0 * cur.scale[nb].x);
-                y[mt][nb][1] += c[nb][1] * (s0 * cur.scale[nb].y);
-                y[mt][nb][2] += c[nb][2] * (s1 * cur.scale[nb].x);
-                y[mt][nb][3] += c[nb][3] * (s1 * cur.scale[nb].y);
+                y[mt][nb][0] += v[0] * (s0 * cur.scale[nb].x);
+                y[mt][nb][1] += v[1] * (s0 * cur.scale[nb].y);
+                y[mt][nb][2] += v[2] * (s1 * cur.scale[nb].x);
+                y[mt][nb][3] += v[3] * (s1 * cur.scale[nb].y);
               }
             }
           }
@@ -346,12 +364,13 @@ ssd_status w4_launch(W4Params p, cudaStream_t s) {
 
 template <typename T, int NB, int PER, bool PAIR>
 ssd_status w4_launch_tiles(const W4Params& p, cudaStream_t s) {
-  // the most tiles a team gets, in the fewest passes of at most kMost, evenly
-  constexpr int kMost = NB == 1 ? 8 : 4;
+  // the most tiles a team gets, in the fewest passes of at most kMost, evenly: a pass fetches the activations
+  // anew (16 fp32 rows, 32000 x 4096: passes of 4 38.5 us, of 7 35.2; bf16: two CTAs leave 4 the registers)
+  constexpr int kMost = NB == 1 || sizeof(T) == 4 ? 8 : 4;
   const int teams = kW4Sms * W4Geo<kW4Parts<T, PAIR>, NB, 1>::kCtas * (kW4Warps >> p.log_warps);
   const int tiles = ((p.n + 15) / 16 + teams - 1) / teams, passes = (tiles + kMost - 1) / kMost;
   const int mt = (tiles + passes - 1) / passes;
-  if constexpr (NB == 1) {
+  if constexpr (kMost == 8) {
     if (mt > 6) return w4_launch<T, NB, 8, PER, PAIR>(p, s);
     if (mt > 4) return w4_launch<T, NB, 6, PER, PAIR>(p, s);
   }
