@@ -586,8 +586,10 @@ SSD_API ssd_status ssd_w4_unpack(const void* packed, int n, int k, int group, fl
 /* y = x W^T (+ residual), rows <= SSD_W4_MAX_ROWS, fp32 sums, each group's products scaled in fp32.
  *   x: device, type SSD_TYPE_*, [rows][x_row_stride];  y: same type, [rows][y_row_stride]
  *   residual: device [rows][res_row_stride] of the same type, or NULL; may be y itself
- *   work: device, ssd_w4_work_bytes(), 16-byte aligned
- * y must not overlap x. */
+ *   work: device, ssd_w4_work_bytes(), 16-byte aligned, of this call alone until it has run.  Neither read
+ *     nor written for bf16 rows with k and x_row_stride multiples of 128 and 8 and x 16-byte aligned.
+ * y must not overlap x.  Sums of bf16 rows run over (128 + u) x with u in 0..15 before 136 x is taken off:
+ * finite rows above about 2^113 can overflow to NaN, and an infinity gives NaN. */
 SSD_API int64_t ssd_w4_work_bytes(int n, int k);
 SSD_API ssd_status ssd_w4_matmul(const void* packed, int n, int k, int group, const void* x, int type, int rows,
                                  int64_t x_row_stride, void* y, int64_t y_row_stride, const void* residual,

@@ -195,9 +195,6 @@ class KV8Cache:
             _raise(status)
 
 
-_w4_work: dict = {}   # (device, stream) -> workspace (pointer, size, tensor): streams must not share one
-
-
 class W4Weight:
     """A weight matrix [n][k] packed to 4 bits with bf16 group scales (ssd_w4_pack)."""
 
@@ -248,15 +245,16 @@ class W4Weight:
             os = self.n
         else:
             os = self._rows(out, (rows, self.n), dtype, "out")
-        stream = _stream(i)
-        work = _w4_work.get((i, stream))
-        if work is None or work[1] < self._work:
-            t = torch.empty(self._work, dtype=torch.uint8, device=self.device)
-            work = _w4_work[(i, stream)] = (t.data_ptr(), self._work, t)
+        # A call's own workspace, so that graphs, streams and threads share nothing.  bf16 rows that are operands
+        # as they lie need none (the rule of ssd_w4_matmul).
+        px, work = x.data_ptr(), None
+        if code or self.k % 128 or xs % 8 or px % 16:
+            work = torch.empty(self._work, dtype=torch.uint8, device=self.device)
         status = self.lib.ssd_w4_matmul(
-            self._packed, self.n, self.k, self.group, x.data_ptr(), code, rows, xs, out.data_ptr(), os,
+            self._packed, self.n, self.k, self.group, px, code, rows, xs, out.data_ptr(), os,
             None if residual is None else residual.data_ptr(),
-            0 if residual is None else self._rows(residual, (rows, self.n), dtype, "residual"), work[0], stream)
+            0 if residual is None else self._rows(residual, (rows, self.n), dtype, "residual"),
+            self._packed if work is None else work.data_ptr(), _stream(i))
         if status:
             _raise(status)
         return out

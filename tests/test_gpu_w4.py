@@ -146,3 +146,26 @@ def test_wrapper_refusals():
             f()
         assert e.value.status == 1, i
     assert w.matmul(x[:0]).shape == (0, 20)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_captured_product_shares_nothing_with_later_calls(dtype):
+    """A graph's replays after larger products on its stream: neither its values nor other tensors change."""
+    x, w = normal((5, 130), 1, dtype=DT[dtype]), normal((96, 130), 2, 0.05)
+    big_x, big_w = normal((16, 5000), 3, dtype=DT[dtype]), lib.W4Weight(normal((64, 5000), 4, 0.05))
+    p = lib.W4Weight(w, 32)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        p.matmul(x)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            y = p.matmul(x)
+        big = big_w.matmul(big_x)
+        others = [torch.full((1 << e,), 7, dtype=torch.uint8, device="cuda") for e in range(9, 21) for _ in range(8)]
+        for _ in range(3):
+            g.replay()
+            again = big_w.matmul(big_x)
+    s.synchronize()
+    check(y, x, p.dequantize())
+    assert torch.equal(big, again) and all((o == 7).all() for o in others)
