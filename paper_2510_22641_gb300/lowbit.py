@@ -60,13 +60,13 @@ class KV8Step:
     row_start [batch + 1], slot [rows] and length [batch] are views of the device buffer that
     KV8Cache.plan fills."""
 
-    def __init__(self, cache: KV8Cache, batch: int, rows: int, rows_per_request: int | None = None):
+    def __init__(self, cache: KV8Cache, batch: int, rows: int, rows_per_request: int | None = None, row_tile: int = 0):
         n = B.load().ssd_kv8_step_ints(batch, rows)
         if n < 0 or batch > cache.max_batch:
             _fail(f"step of {rows} rows of {batch} requests (the cache has {cache.max_batch} seats)")
         self.batch, self.rows, self.cache = batch, rows, cache
         self.data = torch.zeros(n, dtype=torch.int32, device=cache.device)
-        tile = 0
+        tile = row_tile
         if rows_per_request is not None:
             heads = rows_per_request * (cache.n_heads // cache.n_kv_heads)
             items = -(-heads // 32)
@@ -119,10 +119,11 @@ class KV8Cache:
         c.pool, c.work = self.pool.data_ptr(), self.work.data_ptr()
         self._index, self._state, self._scale = device.index, (1 + max_batch,), 1.0 / math.sqrt(head_dim)
 
-    def new_step(self, batch: int, rows: int, rows_per_request: int | None = None) -> KV8Step:
-        """A plan's buffer for `rows` new rows of `batch` requests.  rows_per_request: the usual number, if
-        it is not rows / batch (only the attention's speed depends on it)."""
-        return KV8Step(self, batch, rows, rows_per_request)
+    def new_step(self, batch: int, rows: int, rows_per_request: int | None = None, row_tile: int = 0) -> KV8Step:
+        """A plan's buffer for `rows` new rows of `batch` requests.  row_tile: query rows of a kv head the
+        attention takes at once (8, 16, 24 or 32; 0: chosen by the cache's size), or rows_per_request: as many
+        as that many rows have.  Only the attention's speed depends on it."""
+        return KV8Step(self, batch, rows, rows_per_request, row_tile)
 
     def plan(self, step: KV8Step, length: torch.Tensor, add: torch.Tensor, state: torch.Tensor | None = None,
              state_out: torch.Tensor | None = None) -> KV8Step:

@@ -349,6 +349,35 @@ def test_attention_is_right_for_any_row_tile(tile):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tile", [16, 24, 32])
+@pytest.mark.parametrize("case", CASES[2:10], ids=lambda c: f"d{c[0]}_h{c[1]}_{c[2]}_b{c[3]}_n{max(c[4])}_r{max(c[5])}")
+def test_attention_row_tiles(case, tile, dtype):
+    """Items of 16 to 32 query rows, which the size of the cache would choose only for large ones."""
+    dim, heads, kv, block, hist, add = case
+    wide = max(-(-(a + b) // block) for a, b in zip(hist, add))
+    f = Filled(block, heads, kv, dim, len(hist), wide, DT[dtype])
+    f.append(hist)
+    f.append(add, row_tile=tile)
+    q = rows((sum(add), heads, dim), 9, DT[dtype], 0.5) * 2
+    masks = [(0x9e3779b9 * (i + 1) >> 3 | 1 << 31) & 0xffffffff for i in range(sum(add))]
+    m = torch.tensor(np.array(masks, np.uint32).view(np.int32)).cuda()
+    check_attention(f, q, f.cache.attention(0, q, f.step), dim ** -0.5)
+    check_attention(f, q, f.cache.attention(0, q, f.step, row_mask=m), dim ** -0.5, masks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tile", [8, 16, 24, 32])
+def test_attention_of_many_short_contexts(tile, dtype):
+    """More segments than teams, each shorter than a team's usual span; some of one token, some empty."""
+    f = Filled(32, 32, 16, 64, 37, 3, DT[dtype])
+    f.append([i * 5 % 41 for i in range(37)])
+    f.append([i % 17 for i in range(37)], row_tile=tile)
+    q = rows((sum(f.add), 32, 64), 8, DT[dtype], 0.5)
+    check_attention(f, q, f.cache.attention(0, q, f.step), 0.125)
+    assert status(f.cache) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_attention_with_row_masks(dtype):
     """Trees of drafts: a row sees the prefix and some of the step's rows; rows of a request without a
     prefix may see nothing, and give zeros."""
