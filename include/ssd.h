@@ -511,7 +511,7 @@ typedef struct {
   int batch;     /* requests: seats 0 .. batch - 1 */
   int rows;      /* capacity: new rows of all requests */
   int row_tile;  /* 8, 16, 24 or 32: query rows x (n_heads / n_kv_heads) the attention takes at once; any
-                  * value is right, one near the usual product is fastest (0: from rows / batch) */
+                  * value is right (0: 8 where a layer of the cache fits L2, else rows / batch's product) */
   int32_t* data;
 } ssd_kv8_step;
 
@@ -552,7 +552,7 @@ SSD_API ssd_status ssd_kv8_read(const ssd_kv8* c, int layer, const int32_t* slot
 /* Attention of a step's rows over the cache (its own K/V rows appended before):
  *   o = sum_j softmax_j(scale * q . k_j) v_j
  * Query head h reads kv head h / (n_heads / n_kv_heads).  Row i of request b (position len[b] + i) sees
- * the keys before len[b] and, of the step's own rows j, those with bit j of row_mask[row] set -- or,
+ * the keys before len[b] and, of its request's rows j of the step, those with bit j of row_mask[row] set -- or,
  * with row_mask NULL, the rows j <= i.  A row that sees no key gives zeros, as do rows past the last
  * request's.  Keys without a block are not seen.
  *   q, o: device, type SSD_TYPE_*, element (row, head, i) at row * row_stride + head * head_stride + i;

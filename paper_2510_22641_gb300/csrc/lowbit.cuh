@@ -119,12 +119,6 @@ __device__ __forceinline__ float warp_max(float v) {
   for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
   return v;
 }
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-  return v;
-}
-
 // ------------------------------------------------------------------ the cache's workspace
 //
 // [64 ints: status word, plan ticket][attention tickets][attention partial states]
@@ -205,17 +199,19 @@ __host__ __device__ __forceinline__ StepView step_view(int32_t* d, int batch) {
   return v;
 }
 
-// Query rows (of one kv head) one attention item takes: as many as there usually are, in the fewest items
-// of at most 32.  Where every context fits 64 tiles, latency counts and not the tiles read again for each
-// item: the smallest for which each item still has a CTA (two requests of 300 tokens, 120 rows for one
-// kv head: items of 32 rows 14 us, of 8 rows 9 us).
+// Query rows (of one kv head) one attention item takes.  Items of 8 have the most warps per SM and the
+// fewest empty columns where requests differ, but more of them read the same tiles; so they are the choice
+// where the tiles come from L2: a layer's cache of at most 128 MB (96 rows for one kv head, 72 MB: items of
+// 24 rows 71 us, of 8 64; 28 rows, 16 MB: 33 and 21 us; 16 rows of a kv head and 186 MB: items of 16 55, of 8
+// 49; 24 rows, 147 MB: of 24 50, of 8 58).  Else as many as there usually are, in the fewest items of at
+// most 32 (24 rows, 900 MB: items of 24 111 us, of 8 182).
+constexpr int64_t kItemsOf8Bytes = 128ll << 20;
 inline int step_row_tile(const ssd_kv8* c, const ssd_kv8_step* s) {
   if (s->row_tile) return s->row_tile;
+  const int64_t all = static_cast<int64_t>(s->batch) * c->max_blocks, blocks = all < c->n_blocks ? all : c->n_blocks;
+  if (blocks * c->block_tokens * c->n_kv_heads * c->head_dim * 2 <= kItemsOf8Bytes) return 8;
   const int64_t r = static_cast<int64_t>((s->rows > 0 ? s->rows + s->batch - 1 : s->batch) / s->batch) *
                     (c->n_heads / c->n_kv_heads);
-  if (static_cast<int64_t>(c->max_blocks) * c->block_tokens <= 64 * kTileTokens)
-    for (int tile = 8; tile < 32; tile += 8)
-      if ((r + tile - 1) / tile * c->n_kv_heads * s->batch <= kAttnSms) return tile;
   const int64_t items = (r + 31) / 32;
   return static_cast<int>(((r + items - 1) / items + 7) / 8 * 8);
 }
