@@ -571,8 +571,8 @@ SSD_API ssd_status ssd_kv8_status(const ssd_kv8* c, int* bits, void* cuda_stream
 #define SSD_W4_MAX_ROWS 16
 
 /* A weight matrix [n][k] in 4 bits: per row and group of `group` (32, 64 or 128) columns a bf16 scale
- * s = amax / 7 (rounded to nearest even) and codes round(w * (1 / s)) in -8..7; k is padded to whole
- * 128-column chunks and n to 16 rows with zeros.  Packed as [16-row tile][128-column chunk]{codes, scales}
+ * s = amax / 7 (rounded to nearest even) and codes round(w * (1 / s)) in -8..7 (1 / s is taken as 0 where it is
+ * not finite: amax below about 2^-125); k is padded to whole 128-column chunks and n to 16 rows with zeros.  Packed as [16-row tile][128-column chunk]{codes, scales}
  * in the order the matrix instructions take them.  A group with a non-finite weight gives NaN. */
 SSD_API int64_t ssd_w4_bytes(int n, int k, int group);
 

@@ -26,20 +26,22 @@ __global__ void __launch_bounds__(256) ssd_w4_pack_kernel(const W4PackParams p) 
   for (int job = w; job < 16 * per; job += 8) {
     const int row = job / per, grp = job % per, n = tile * 16 + row;
     float x[4], amax = 0.0f;
-    bool nan = false;
+    bool bad = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int c = lane + 32 * i, col = chunk * kChunk + grp * p.group + c;
       x[i] = 0.0f;
       if (c < p.group && n < p.n && col < p.k)
         x[i] = to_f32(static_cast<const T*>(p.w)[static_cast<int64_t>(n) * p.row_stride + col]);
-      nan |= x[i] != x[i];
+      bad |= !(fabsf(x[i]) <= 3.402823466e38f);
       amax = fmaxf(amax, fabsf(x[i]));
     }
     amax = warp_max(amax);
-    if (__any_sync(~0u, nan)) amax = __int_as_float(0x7fc00000);
+    if (__any_sync(~0u, bad)) amax = __int_as_float(0x7fc00000);  // shows in every product of the row
     const __nv_bfloat16 sb = __float2bfloat16_rn(amax / 7.0f);
-    const float s = __bfloat162float(sb), inv = s > 0.0f ? 1.0f / s : 0.0f;
+    const float s = __bfloat162float(sb);
+    float inv = s > 0.0f ? 1.0f / s : 0.0f;
+    if (inv > 3.402823466e38f) inv = 0.0f;  // scales below 2^-128
     if (lane == 0) scales[row * per + grp] = sb;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

@@ -169,3 +169,25 @@ def test_a_captured_product_shares_nothing_with_later_calls(dtype):
     s.synchronize()
     check(y, x, p.dequantize())
     assert torch.equal(big, again) and all((o == 7).all() for o in others)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", ["inf", "-inf", "nan"])
+def test_a_group_with_a_non_finite_weight_is_nan(bad, dtype):
+    w = normal((20, 256), 1, 0.02, DT[dtype])
+    w[3, 70] = float(bad)
+    p = lib.W4Weight(w, 64)
+    d = p.dequantize()
+    assert torch.isnan(d[3, 64:128]).all() and torch.isfinite(d).sum() == d.numel() - 64
+    assert torch.isnan(p.matmul(normal((3, 256), 2, 1.0, DT[dtype]))[:, 3]).all()
+
+
+def test_pack_of_groups_whose_scale_has_no_finite_inverse():
+    """bf16 scales below 2^-128 (their inverse passes fp32): zeros, for the group's zeros too."""
+    w = torch.zeros(16, 128, device="cuda")
+    w[0, 3], w[1, ::2], w[2, 5] = 2.0 ** -129 * 7, -(2.0 ** -130) * 7, 2.0 ** -120 * 7
+    p = lib.W4Weight(w, 32)
+    want = torch.zeros_like(w)
+    want[2, 5] = 2.0 ** -120 * 7
+    assert torch.equal(p.dequantize(), want)
+    assert torch.isfinite(p.matmul(normal((2, 128), 1))).all()
