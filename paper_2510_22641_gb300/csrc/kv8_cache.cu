@@ -409,9 +409,10 @@ __device__ __forceinline__ uint32_t code8(float x, float inv) { return __float_a
 __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
-// The same for values that may be NaN (code 0) or infinite (the largest code).
-__device__ __forceinline__ float tame(float x, float scale) {
-  return x != x ? 0.0f : fminf(fmaxf(x, -127.0f * scale), 127.0f * scale);
+// The same for values that may be NaN (code 0) or infinite (the largest code).  The product is clamped, not the
+// value: 127 times the scale of the largest fp32 values rounds to infinity.
+__device__ __forceinline__ uint32_t code8_any(float x, float inv) {
+  return code8(x != x ? 0.0f : fminf(fmaxf(__fmul_rn(x, inv), -127.0f), 127.0f), 1.0f);
 }
 // The four codes of a word at a scale `ratio` times as large.
 __device__ __forceinline__ uint32_t rescale8(uint32_t word, float ratio) {
@@ -529,8 +530,7 @@ __global__ void __launch_bounds__(128) ssd_kv8_append_rows_kernel(const AppendPa
   for (int c = lane; c < n * D4; c += 32) {
     const float4 x = load4<VEC>(src + c / D4 * row_stride + c % D4 * 4);
     const int token = off + c / D4, d = c % D4 * 4;
-    const uint32_t q[4] = {code8(tame(x.x, s_new), inv), code8(tame(x.y, s_new), inv), code8(tame(x.z, s_new), inv),
-                           code8(tame(x.w, s_new), inv)};
+    const uint32_t q[4] = {code8_any(x.x, inv), code8_any(x.y, inv), code8_any(x.z, inv), code8_any(x.w, inv)};
     uint8_t* tile = blk + (token >> 4) * (32 * D);
     if (kv == 0) {
       *reinterpret_cast<uint32_t*>(tile + kv8_k_byte(token & 15, d, D)) = pack4(q[0], q[1], q[2], q[3]);
@@ -714,7 +714,7 @@ __global__ void __launch_bounds__(256, 2) ssd_kv8_append_kernel(const AppendPara
           y.template load<VEC>(rows + i * row_stride);
           word = 0;
 #pragma unroll
-          for (int e = 0; e < E; ++e) word |= (code8(tame(y[e], s_new), inv) & 255u) << (8 * e);
+          for (int e = 0; e < E; ++e) word |= (code8_any(y[e], inv) & 255u) << (8 * e);
         }
         if constexpr (E == 4) *reinterpret_cast<uint32_t*>(at) = word;
         else *reinterpret_cast<uint16_t*>(at) = static_cast<uint16_t>(word);
@@ -734,7 +734,7 @@ __global__ void __launch_bounds__(256, 2) ssd_kv8_append_kernel(const AppendPara
             y.template load<VEC>(rows + (4 * t + i) * row_stride);
             put |= 255u << (8 * i);
 #pragma unroll
-            for (int e = 0; e < E; ++e) word[e] |= (code8(tame(y[e], s_new), inv) & 255u) << (8 * i);
+            for (int e = 0; e < E; ++e) word[e] |= (code8_any(y[e], inv) & 255u) << (8 * i);
           }
 #pragma unroll
         for (int e = 0; e < E; ++e) {

@@ -244,6 +244,19 @@ def test_append_of_values_no_scale_fits():
     f.check_values()
 
 
+@pytest.mark.parametrize("n", [2, 20])
+def test_append_of_infinities_beside_the_largest_value(n):
+    """127 times the scale of the largest fp32 value rounds to infinity; infinities still get the codes 127 and
+    -127.  20 rows of one seat take the prompts' kernel, 2 the decode steps'."""
+    f = Filled(16, 1, 1, 64, 1, 2, torch.float32)
+    x = torch.ones(n, 1, 64, device="cuda")
+    x[0, 0, :3] = torch.tensor([torch.finfo(torch.float32).max, float("inf"), -float("inf")])
+    f.append([n], kv=[x, x.clone()])
+    f.check_values()
+    for got in f.cache.read(0, f.step.slot):
+        assert got[0, 0, 1] == got[0, 0, 0] == -got[0, 0, 2] == got.max()
+
+
 def test_append_and_read_skip_bad_slots():
     c = lib.KV8Cache(1, 1, 1, 64, 16, 3, 1, 3)
     step = c.new_step(1, 4)
