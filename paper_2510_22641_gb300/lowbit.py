@@ -68,9 +68,13 @@ class KV8Step:
         self.data = torch.zeros(n, dtype=torch.int32, device=cache.device)
         tile = row_tile
         if rows_per_request is not None:
+            if rows_per_request < 1:
+                _fail(f"rows_per_request {rows_per_request}")
             heads = rows_per_request * (cache.n_heads // cache.n_kv_heads)
             items = -(-heads // 32)
             tile = (-(-heads // items) + 7) // 8 * 8
+        if tile not in (0, 8, 16, 24, 32):
+            _fail(f"row_tile 0, 8, 16, 24 or 32 expected, got {row_tile}")
         at = B.SSD_KV8_STEP_HEAD + batch + 1
         self.row_start = self.data[at:at + batch + 1]
         self.length = self.data[at + batch + 1:at + 2 * batch + 1]
@@ -144,6 +148,8 @@ class KV8Cache:
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, step: KV8Step) -> None:
         """ssd_kv8_append: quantise the step's new rows k, v [rows][n_kv_heads][head_dim] into the cache."""
         i = self._index
+        if step.cache is not self:
+            _fail("the step was made for another cache")
         ks, vs = _rows3(k, step._kv, i, "k"), _rows3(v, step._kv, i, "v")
         dtype = k.dtype
         if v.dtype is not dtype:

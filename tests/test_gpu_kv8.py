@@ -546,3 +546,17 @@ def test_wrapper_refusals():
         with pytest.raises(lib.SSDError) as e:
             f()
         assert e.value.status == 1, i
+
+
+def test_steps_refused_by_the_wrapper():
+    """A step of a cache of another shape (its rows are fewer bytes than this cache would read), tiles and
+    row counts that no kernel has."""
+    c, other = lib.KV8Cache(1, 8, 8, 64, 16, 8, 2, 4), lib.KV8Cache(1, 2, 2, 64, 16, 8, 2, 4)
+    step = other.new_step(1, 3)
+    x = torch.zeros(3, 2, 64, device="cuda")
+    for i, f in enumerate([lambda: c.append(0, x, x, step), lambda: c.new_step(1, 3, row_tile=12),
+                           lambda: c.new_step(1, 3, row_tile=-8), lambda: c.new_step(1, 3, rows_per_request=0)]):
+        with pytest.raises(lib.SSDError) as e:
+            f()
+        assert e.value.status == 1, i
+    other.append(0, x, x, step)
