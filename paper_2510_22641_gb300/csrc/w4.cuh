@@ -50,7 +50,7 @@ __host__ __device__ constexpr int w4_bit(int row, int col) {
 // lanes read back the bytes they copied, the scales are shared within the warp.
 //
 // Measured (device time, of the copy rate): 32000 x 4096, one bf16 row 16.8 us, 59 %; 16 rows 23.9 us, 42 %;
-// one fp32 row 18.0 us, 55 %; 8 rows 22.5 us, 44 %; 16 rows 35.2 us, 28 %; 4096 x 4096, one bf16 row 5.0 us
+// one fp32 row 18.0 us, 55 %; 8 rows 22.5 us, 44 %; 16 rows 35.2 us, 28 %; 4096 x 4096, one bf16 row 4.4 us
 // (launch, one round of loads, the sum).  137 to 174 instructions a record, half of them unpacking, against
 // the 180 issue slots that a record's bytes leave at the copy rate; 16 fp32 rows wait for their products
 // with 8 warps an SM.
