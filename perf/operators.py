@@ -277,7 +277,7 @@ def _quantize4(w, group):
     """4-bit codes and bf16 group scales of w [n][k], k padded to whole groups with zeros."""
     n, k = w.shape
     w = torch.nn.functional.pad(w.float(), (0, -k % group)).view(n, -1, group)
-    s = (w.abs().amax(2) / w.new_tensor(7.0)).to(torch.bfloat16).float()
+    s = (w.abs().amax(2) / 7).to(torch.bfloat16).float()
     inv = torch.where(s > 0, 1 / s, torch.zeros_like(s))
     return torch.round(w * inv[:, :, None]).clamp(-8, 7).to(torch.int8).view(n, -1), s
 
@@ -355,7 +355,7 @@ def _append(codes, scales, x, slots, counts):
     touched = torch.zeros(n_blocks, dtype=torch.bool, device=x.device).index_fill_(0, block, True)
     opened = torch.zeros(n_blocks, device=x.device).index_add_(0, block, (slots % bs == 0).float()) > 0
     old = torch.where(opened[:, None], torch.zeros_like(scales), scales)
-    new = torch.where(touched[:, None], torch.maximum(old, (amax / amax.new_tensor(127.0)).clamp(min=TINY_SCALE)), scales)
+    new = torch.where(touched[:, None], torch.maximum(old, (amax / 127).clamp(min=TINY_SCALE)), scales)
     # only a request's first new row can fall into a block that holds earlier tokens
     head = block[(torch.cumsum(counts, 0) - counts).clamp(max=len(block) - 1)]
     ratio = old[head] / new[head]
