@@ -588,8 +588,9 @@ SSD_API ssd_status ssd_w4_unpack(const void* packed, int n, int k, int group, fl
  *   residual: device [rows][res_row_stride] of the same type, or NULL; may be y itself
  *   work: device, ssd_w4_work_bytes(), 16-byte aligned, of this call alone until it has run.  Neither read
  *     nor written for bf16 rows with k and x_row_stride multiples of 128 and 8 and x 16-byte aligned.
- * y must not overlap x.  Sums of bf16 rows run over (128 + u) x with u in 0..15 before 136 x is taken off:
- * finite rows above about 2^113 can overflow to NaN, and an infinity gives NaN. */
+ * y must not overlap x.  bf16 rows enter the products as they are; fp32 rows as pairs of fp16, each
+ * element to 2^-22 of itself or 2^-39 of the largest magnitude among its 128 columns, whichever is more
+ * (rows below about 2^-100 lose further bits to the end of fp32's range).  NaN and infinities in a row show in that row alone. */
 SSD_API int64_t ssd_w4_work_bytes(int n, int k);
 SSD_API ssd_status ssd_w4_matmul(const void* packed, int n, int k, int group, const void* x, int type, int rows,
                                  int64_t x_row_stride, void* y, int64_t y_row_stride, const void* residual,

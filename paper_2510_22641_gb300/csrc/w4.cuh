@@ -31,13 +31,13 @@ __host__ __device__ constexpr int w4_bit(int row, int col) {
 // ------------------------------------------------------------------ matmul
 //
 // y^T = W x^T by m16n8k16 products: 16 weight rows by 8 activation rows, 16 columns at a time.
-//   bf16 rows are operands as they are, and codes become operands by shifts and masks alone: u = code + 8
-//     goes into the mantissa of 128, 128 + u is exact in bf16, and one more product with the constant 136
-//     gives what has to be taken off, sum (128 + u) x - sum 136 x = sum code x (the cancellation costs 5
-//     of 24 bits, the output has 8);
+//   bf16 rows are operands as they are: u = code + 8 goes into the mantissa of 128, and one subtraction per
+//     pair gives the codes.  (Products with 128 + u itself, less 136 times the row's sum, would save the
+//     subtractions, but their rounding goes with the largest activation, seen by the weights or not: 3e-3
+//     of the result beside one of 1e4, 0.4 beside 1e6.)
 //   fp32 rows are scaled per row and chunk by a power of two to 2^14 .. 2^15 and split into a high and a
-//     low half (22 bits); u goes into the mantissa of the half 1024, and one subtraction (or fused
-//     multiply) per pair gives the codes themselves, with no cancellation.  (u read as a subnormal half
+//     low half (22 bits, and to 2^-39 of the chunk's largest); u goes into the mantissa of the half 1024,
+//     and one subtraction (or fused multiply) per pair gives the codes.  (u read as a subnormal half
 //     would need no arithmetic, but the matrix unit aligns its sums by the exponents of the operands, so
 //     a subnormal operand costs its leading zeros: 10 bits, measured 1e-5 of the result.)
 // Each group's sum is multiplied by its scale in fp32 and added to the fp32 sums.
@@ -49,7 +49,7 @@ __host__ __device__ constexpr int w4_bit(int row, int col) {
 // A warp streams its records (16 rows x 128 columns, 1 KB + scales) with cp.async into a ring of its own;
 // lanes read back the bytes they copied, the scales are shared within the warp.
 //
-// Measured (device time, of the copy rate): 32000 x 4096, one bf16 row 16.8 us, 59 %; 16 rows 23.9 us, 42 %;
+// Measured (device time, of the copy rate): 32000 x 4096, one bf16 row 17.3 us, 57 %; 16 rows 23.4 us, 42 %;
 // one fp32 row 18.0 us, 55 %; 8 rows 22.5 us, 44 %; 16 rows 35.2 us, 28 %; 4096 x 4096, one bf16 row 4.4 us
 // (launch, one round of loads, the sum).  137 to 174 instructions a record, half of them unpacking, against
 // the 180 issue slots that a record's bytes leave at the copy rate; 16 fp32 rows wait for their products
@@ -108,6 +108,11 @@ __device__ __forceinline__ uint32_t half2_sub(uint32_t a, uint32_t b) {
   asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+__device__ __forceinline__ uint32_t bf2_sub(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 __device__ __forceinline__ uint32_t half2_fma(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t r;
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
@@ -124,10 +129,10 @@ __device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t b
 template <bool BF16>
 __device__ __forceinline__ void w4_operand(uint32_t w, uint32_t (&a)[4]) {
   if constexpr (BF16) {
-    a[0] = and_or(w, 0x000f000fu, 0x43004300u);
-    a[1] = and_or(w >> 4, 0x000f000fu, 0x43004300u);
-    a[2] = and_or(w >> 8, 0x000f000fu, 0x43004300u);
-    a[3] = and_or(w >> 12, 0x000f000fu, 0x43004300u);
+    a[0] = bf2_sub(and_or(w, 0x000f000fu, 0x43004300u), 0x43084308u);  // 128 + u - 136
+    a[1] = bf2_sub(and_or(w >> 4, 0x000f000fu, 0x43004300u), 0x43084308u);
+    a[2] = bf2_sub(and_or(w >> 8, 0x000f000fu, 0x43004300u), 0x43084308u);
+    a[3] = bf2_sub(and_or(w >> 12, 0x000f000fu, 0x43004300u), 0x43084308u);
   } else {
     const uint32_t h = w >> 8;
     a[0] = half2_sub(and_or(w, 0x000f000fu, 0x64006400u), 0x64086408u);               // 1024 + u - 1032
@@ -227,23 +232,6 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<kW4Parts<T, PAIR>, NB, MT>::
       } else {
         load_x(cur, chunk);
       }
-      // what the constant offset of the codes adds, per group
-      float off[4][NB][2];
-      if constexpr (BF16) {
-        const uint32_t a[4] = {0x43084308u, 0x43084308u, 0x43084308u, 0x43084308u};  // 136
-        float s[NB][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            if (i % (4 / per) == 0) s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.0f;
-            w4_mma<BF16>(s[nb], a, cur.x[nb][0][i].x, cur.x[nb][0][i].y);
-            w4_mma<BF16>(s[nb], a, cur.x[nb][0][i].z, cur.x[nb][0][i].w);
-            off[i][nb][0] = s[nb][0];
-            off[i][nb][1] = s[nb][1];
-          }
-        }
-      }
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         if (mt >= cnt) break;
@@ -289,10 +277,10 @@ __global__ void __launch_bounds__(kW4Threads, W4Geo<kW4Parts<T, PAIR>, NB, MT>::
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] += c[1][nb][e];
               if constexpr (BF16) {
-                y[mt][nb][0] += (v[0] - off[i][nb][0]) * s0;
-                y[mt][nb][1] += (v[1] - off[i][nb][1]) * s0;
-                y[mt][nb][2] += (v[2] - off[i][nb][0]) * s1;
-                y[mt][nb][3] += (v[3] - off[i][nb][1]) * s1;
+                y[mt][nb][0] += v[0] * s0;
+                y[mt][nb][1] += v[1] * s0;
+                y[mt][nb][2] += v[2] * s1;
+                y[mt][nb][3] += v[3] * s1;
               } else {
                 y[mt][nb][0] += v[0] * (s0 * cur.scale[nb].x);
                 y[mt][nb][1] += v[1] * (s0 * cur.scale[nb].y);

@@ -191,3 +191,29 @@ def test_pack_of_groups_whose_scale_has_no_finite_inverse():
     want[2, 5] = 2.0 ** -120 * 7
     assert torch.equal(p.dequantize(), want)
     assert torch.isfinite(p.matmul(normal((2, 128), 1))).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [1, 5, 16])
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("size", [1e4, 1e6])
+def test_matmul_beside_an_outlier_that_the_weights_do_not_see(size, group, rows, dtype):
+    """An activation that is much larger than the others, at a column whose codes are 0, adds nothing and costs
+    the others nothing: the bound is that of sum |x w|, without it.  fp32 rows are held to 2^-39 of a chunk's
+    largest magnitude."""
+    w = normal((200, 384), 1, 0.02)
+    w[:, 70], w[:, 301] = 0, 0
+    p = lib.W4Weight(w, group)
+    x = normal((rows, 384), 2, 1.0)
+    x[:, 70], x[:, 301] = size, -size
+    x = x.to(DT[dtype])
+    y, d = p.matmul(x), p.dequantize().double()
+    assert (d[:, 70] == 0).all() and (d[:, 301] == 0).all()
+    want, total = x.double() @ d.T, x.double().abs() @ d.abs().T
+    bound = (384 / 8 + 64) * 2.0 ** -24 * total
+    if dtype == "fp32":
+        bound = bound + 2.0 ** -39 * size * d.abs().sum(1)
+    else:
+        bound = bound + 2.0 ** -8 * want.abs()
+    err = (y.double() - want).abs()
+    assert (err <= bound).all(), f"{(err > bound).sum().item()} of {err.numel()}, worst {(err / bound).max().item()}"
