@@ -558,8 +558,9 @@ SSD_API ssd_status ssd_kv8_read(const ssd_kv8* c, int layer, const int32_t* slot
  *   q, o: device, type SSD_TYPE_*, element (row, head, i) at row * row_stride + head * head_stride + i;
  *         o must not overlap q
  *   row_mask: device uint32 [rows] or NULL (with it a request may have at most 32 rows)
- * Scores, softmax statistics and sums are fp32; for bf16 rows the probabilities enter the products as
- * fp16, for fp32 rows q and the probabilities as pairs of fp16. */
+ * Scores, softmax statistics and sums are fp32.  bf16 rows of q enter the products as they are, fp32 rows as
+ * pairs of fp16 (each element to 2^-22 of itself or 2^-39 of its row's largest).  The weights, probability
+ * times V scale, enter as fp16 (bf16 rows) or as pairs of it. */
 SSD_API ssd_status ssd_kv8_attention(const ssd_kv8* c, int layer, const ssd_kv8_step* step, const void* q, void* o,
                                      int type, int64_t q_row_stride, int64_t q_head_stride, int64_t o_row_stride,
                                      int64_t o_head_stride, float scale, const uint32_t* row_mask, void* cuda_stream);

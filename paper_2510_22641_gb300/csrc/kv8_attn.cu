@@ -4,9 +4,10 @@
 // S^T = K Q^T and O^T = V^T P^T, 16 keys at a time, with m16n8k16 products: the keys (then the
 // dimensions) are the 16 matrix rows, the query rows the 8 columns, so one row costs no more than
 // eight need.  Codes are exact in fp16: a byte c + 128 becomes the half 1024 + (c + 128) by a byte
-// permute, less 1152.  Queries are scaled by a power of two per row into [1, 2) and held as one half
-// (bf16 rows: exact) or a high and a low half (fp32 rows, 22 bits).  The K scale, the row's power of
-// two and the softmax scale multiply the fp32 scores.  Softmax is online, in fp32: p = 2^(s - m) with a
+// permute, less 1152.  Queries are scaled by a power of two per row, the largest into [2^14, 2^15), and held
+// as one half (bf16 rows: exact down to 2^-31 of the largest) or a high and a low half (fp32 rows: 22 bits,
+// or 2^-39 of the largest).  The K scale, the row's power of two and the softmax scale multiply the fp32
+// scores.  Softmax is online, in fp32: p = 2^(s - m) with a
 // reference m per row that is raised to the running maximum only when a p passes 2^8, and the sum l.  The
 // V scale vs of a tile goes into the weights w = 2^7 p vs / B, which are rounded to one half (two for fp32
 // rows); B is a power of two per row, raised with m to at least every p vs, so that neither tiny nor huge
@@ -282,8 +283,8 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
       amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
       uint32_t ex = __float_as_uint(amax) & 0x7f800000u;
       if (ex == 0x7f800000u) ex = 127u << 23;  // an infinite query: its row comes out NaN or infinite
-      if (ex == 0) ex = 1u << 23;
-      const float inv = __uint_as_float((254u << 23) - ex);
+      ex = max(ex, 15u << 23);                 // so that 2^(14 - e) is a normal number
+      const float inv = __uint_as_float((268u << 23) - ex);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
 #pragma unroll
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[nb][e] *= rs[nb][e & 1] * sc.x;
+        for (int e = 0; e < 4; ++e) s[nb][e] *= rs[nb][e & 1] * (sc.x * 0x1p-14f);
       // masks: only where a tile reaches past the cached tokens, or does not exist
       if ((tile + 1) * 16 > len || sc.x < 0.0f) {
 #pragma unroll

@@ -560,3 +560,19 @@ def test_steps_refused_by_the_wrapper():
             f()
         assert e.value.status == 1, i
     other.append(0, x, x, step)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tile", [8, 16])
+def test_attention_of_queries_with_an_outlier_that_no_key_sees(tile, dtype):
+    """One dimension of the queries is a million times the others, where all keys are 0: it adds nothing to the
+    scores and costs the other dimensions nothing."""
+    f = Filled(32, 4, 2, 64, 2, 4, DT[dtype])
+    for add in ([90, 20], [5, 2]):
+        kv = [rows((sum(add), 2, 64), 50 + i + sum(add), DT[dtype], 0.3) for i in range(2)]
+        kv[0][:, :, 9] = 0
+        f.append(add, kv=kv, row_tile=tile)
+    q = rows((7, 4, 64), 3, torch.float32, 0.2)
+    q[:, :, 9] = 1e6
+    q = q.to(DT[dtype])
+    check_attention(f, q, f.cache.attention(0, q, f.step), 64 ** -0.5)
