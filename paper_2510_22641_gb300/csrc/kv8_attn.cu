@@ -7,11 +7,11 @@
 // permute, less 1152.  Queries are scaled by a power of two per row, the largest into [2^14, 2^15), and held
 // as one half (bf16 rows: exact down to 2^-31 of the largest) or a high and a low half (fp32 rows: 22 bits,
 // or 2^-39 of the largest).  The K scale, the row's power of two and the softmax scale multiply the fp32
-// scores.  Softmax is online, in fp32: p = 2^(s - m) with a
-// reference m per row that is raised to the running maximum only when a p passes 2^8, and the sum l.  The
-// V scale vs of a tile goes into the weights w = 2^7 p vs / B, which are rounded to one half (two for fp32
-// rows); B is a power of two per row, raised with m to at least every p vs, so that neither tiny nor huge
-// V blocks lose bits; O is kept in units of B / 2^7.
+// scores.  Softmax is online, in fp32: p = 2^(s - m) with a reference m per row that is raised, in whole
+// steps, to the running maximum only when a p passes 2^8, and the sum l.  The V scale vs of a tile goes into
+// the weights w = 2^7 p vs / B, which are rounded to one half (two for fp32 rows); B is a power of two per
+// row, raised with m to at least every p vs, so that neither tiny nor huge V blocks lose bits; O is kept in
+// units of B / 2^7.
 //
 // Bound: bytes.  A cached token costs 2 D bytes and 4 D rows flops, below the tensor rate up to about
 // 16 rows; so the design is a stream of the cache at full width.  The tile layout (lowbit.cuh) lets
@@ -428,8 +428,9 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
             float top = fmaxf(s[nb][e], s[nb][e + 2]);
 #pragma unroll
             for (int k = 4; k <= 16; k <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
-            const float m_new = fmaxf(m[nb][e], top);
-            const float alpha = ex2(m[nb][e] - m_new);
+            // whole steps: alpha is a power of two, so that rows raised often do not round their unit up each time
+            const float m_new = fmaxf(m[nb][e], ceilf(top)), step = m_new - m[nb][e];
+            const float alpha = step > 126.0f ? 0.0f : __uint_as_float((127u - static_cast<unsigned>(step)) << 23);
             const float need = fmaxf(unit[nb][e] * alpha, ex2(top - m_new) * sc.y);
             const uint32_t bits = max((__float_as_uint(need) + 0x7fffffu) & 0x7f800000u, 8u << 23);
             const float f = (alpha * unit[nb][e]) * __uint_as_float((254u << 23) - bits);

@@ -576,3 +576,47 @@ def test_attention_of_queries_with_an_outlier_that_no_key_sees(tile, dtype):
     q[:, :, 9] = 1e6
     q = q.to(DT[dtype])
     check_attention(f, q, f.cache.attention(0, q, f.step), 64 ** -0.5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attention_where_scores_rise_slowly_after_large_values(dtype):
+    """The scores of one query head rise steeply from tile to tile, those of its neighbours slowly, and the first
+    tile's values are 2^40 times the others': at the end it weighs little in every row, and the later values
+    need their bits.  Enough segments that a warp takes a whole one (60 tiles)."""
+    batch, kv, group, dim, block, tiles = 61, 40, 8, 64, 16, 60
+    n = tiles * block
+    c = lib.KV8Cache(1, kv * group, kv, dim, block, batch * (tiles + 1), batch, tiles + 1)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k = torch.zeros(n, kv, dim, device="cuda")
+    k[:, :, 0] = (torch.arange(n, device="cuda") // block)[:, None]
+    step = c.new_step(batch, batch * n)
+    c.plan(step, ints([0] * batch), ints([n] * batch))
+    v = torch.randn(batch, n, kv, dim, device="cuda", generator=g)
+    v[:, :block] *= 2.0 ** 40
+    c.append(0, k.to(DT[dtype]).repeat(batch, 1, 1), v.view(batch * n, kv, dim).to(DT[dtype]), step)
+    one = c.new_step(batch, batch)
+    c.plan(one, ints([n] * batch), ints([1] * batch))
+    last = torch.zeros(batch, kv, dim, device="cuda", dtype=DT[dtype])
+    c.append(0, last, last, one)
+    q = torch.zeros(batch, kv, group, dim, device="cuda")
+    rise = torch.full((group,), 0.9, device="cuda")
+    rise[0] = 9
+    q[..., 0] = rise * float(np.log(2.0))
+    q = q.to(DT[dtype])
+    o = c.attention(0, q.view(batch, kv * group, dim), one, scale=1.0).view(batch, kv, group, dim)
+    slots = torch.cat([step.slot.view(batch, n), one.slot[:, None]], 1)
+    for b in (0, 30, 60):
+        kk, vv = (x.double() for x in c.read(0, slots[b].contiguous()))
+        s = torch.einsum("hgd,nhd->hgn", q[b].double(), kk)
+        p = s.softmax(2)
+        want, weight = torch.einsum("hgn,nhd->hgd", p, vv), torch.einsum("hgn,nhd->hgd", p, vv.abs())
+        # as in check_attention
+        size = s.abs().amax(2)[:, :, None]
+        bound = (2.0 ** -18 * (1 + size) + n * 2.0 ** -26) * weight
+        scale = c.scales[0, slots[b].long() // block, :, 1].double()
+        floor = (p * scale.T[:, None]).amax(2)[:, :, None] * (vv.abs() / scale[:, :, None]).sum(0)[:, None]
+        bound = bound + 2.0 ** -24 * floor
+        if dtype == "bf16":
+            bound = bound + 2.0 ** -10 * weight + 2.0 ** -8 * want.abs()
+        err = (o[b].double() - want).abs()
+        assert (err <= bound).all(), f"{(err > bound).sum().item()} of {err.numel()}, worst {(err / bound).max().item()}"
