@@ -469,7 +469,8 @@ enum { SSD_TYPE_BF16 = 0, SSD_TYPE_FP32 = 1 };
 /* Bits of the cache's device status word, which ssd_kv8_status reads and clears. */
 enum {
   SSD_KV8_NO_BLOCKS = 1,   /* the free stack ran out: rows without a block have slot -1 */
-  SSD_KV8_LENGTH = 2,      /* len / add / held out of range, or more rows than the step holds */
+  SSD_KV8_LENGTH = 2,      /* len / add / held out of range, more rows than the step holds, or more than 32
+                            * rows of a request under a row mask */
   SSD_KV8_SLOT = 4,        /* a slot or block id outside the cache was skipped */
   SSD_KV8_NON_FINITE = 8   /* a NaN (held as 0) or an infinity (held as the largest code) was appended */
 };
@@ -557,7 +558,8 @@ SSD_API ssd_status ssd_kv8_read(const ssd_kv8* c, int layer, const int32_t* slot
  * request's.  Keys without a block are not seen.
  *   q, o: device, type SSD_TYPE_*, element (row, head, i) at row * row_stride + head * head_stride + i;
  *         o must not overlap q
- *   row_mask: device uint32 [rows] or NULL (with it a request may have at most 32 rows)
+ *   row_mask: device uint32 [rows] or NULL (with it a request may have at most 32 rows: a mask has no bits for
+ *         the others, whose keys are not seen, and the status word says so)
  * Scores, softmax statistics and sums are fp32.  bf16 rows of q enter the products as they are, fp32 rows as
  * pairs of fp16 (each element to 2^-22 of itself or 2^-39 of its row's largest).  The weights, probability
  * times V scale, enter as fp16 (bf16 rows) or as pairs of it. */

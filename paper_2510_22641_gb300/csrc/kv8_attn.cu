@@ -247,6 +247,8 @@ __global__ void __launch_bounds__(Geo<D, NB>::kThreads, Geo<D, NB>::kCtas) ssd_k
 
   for (;;) {
     const int head = c_piece.head, rg = c_piece.rg;
+    // a mask has bits for 32 rows of the step; others are seen by none, which the caller is told
+    if (p.row_mask && rows_b > 32 && tt == 0) atomicOr(reinterpret_cast<int*>(p.tickets) - kKv8WorkHead, SSD_KV8_LENGTH);
     const int r_valid = static_cast<int>(min(static_cast<int64_t>(rows_b) * p.group - static_cast<int64_t>(rg) * RT,
                                              static_cast<int64_t>(RT)));
     // row r of the segment -> (step row of the request, query head of the kv head)

@@ -620,3 +620,20 @@ def test_attention_where_scores_rise_slowly_after_large_values(dtype):
             bound = bound + 2.0 ** -10 * weight + 2.0 ** -8 * want.abs()
         err = (o[b].double() - want).abs()
         assert (err <= bound).all(), f"{(err > bound).sum().item()} of {err.numel()}, worst {(err / bound).max().item()}"
+
+
+def test_attention_flags_requests_of_more_rows_than_a_mask_has_bits():
+    f = Filled(16, 2, 2, 64, 2, 5, torch.float32)
+    f.append([4, 20])
+    f.append([33, 3])
+    q = rows((36, 2, 64), 4, torch.float32)
+    want = f.cache.attention(0, q, f.step)
+    assert status(f.cache) == 0   # without masks any number of rows is right
+    mask = ints([-1] * 36)
+    got = f.cache.attention(0, q, f.step, row_mask=mask)
+    assert status(f.cache) == 2
+    assert torch.isfinite(got).all() and torch.equal(got[35], want[35])   # the request of three rows is as it was
+    f.append([32, 32])
+    q = rows((64, 2, 64), 5, torch.float32)
+    f.cache.attention(0, q, f.step, row_mask=ints([-1] * 64))
+    assert status(f.cache) == 0
