@@ -16,14 +16,23 @@ from . import _binding as B
 
 _TYPES = {torch.bfloat16: B.SSD_TYPE_BF16, torch.float32: B.SSD_TYPE_FP32}
 _stream = torch._C._cuda_getCurrentRawStream   # of a device index; the public wrapper makes an object per call
+_current = torch._C._cuda_getDevice            # (a tensor's device exists already, so CUDA is initialised)
 
 
 def _fail(msg: str):
     raise B.SSDError(1, msg)
 
 
-def _raise(status: int):
-    raise B.SSDError(status, B.load().ssd_op_last_error().decode())
+def _call(index: int, entry, *args):
+    """Makes a library call on device `index`'s current stream.  The library launches on the current device, so
+    another one is entered first."""
+    if _current() == index:
+        status = entry(*args, _stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = entry(*args, _stream(index))
+    if status:
+        raise B.SSDError(status, B.load().ssd_op_last_error().decode())
 
 
 # The checks below run on every call of a decode loop: they compare whole shapes and device indices.
@@ -138,11 +147,9 @@ class KV8Cache:
             _fail("the step was made for another cache")
         state = self.state if state is None else state
         state_in = _int32(state, self._state, i, "state")
-        status = self.lib.ssd_kv8_plan(
-            self._ref, step._ref, _int32(length, step._batch, i, "length"), _int32(add, step._batch, i, "add"), state_in,
-            state_in if state_out is None else _int32(state_out, self._state, i, "state_out"), _stream(i))
-        if status:
-            _raise(status)
+        _call(i, self.lib.ssd_kv8_plan, self._ref, step._ref, _int32(length, step._batch, i, "length"),
+              _int32(add, step._batch, i, "add"), state_in,
+              state_in if state_out is None else _int32(state_out, self._state, i, "state_out"))
         return step
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, step: KV8Step) -> None:
@@ -154,10 +161,8 @@ class KV8Cache:
         dtype = k.dtype
         if v.dtype is not dtype:
             _fail(f"k and v: one type expected, got {dtype} and {v.dtype}")
-        status = self.lib.ssd_kv8_append(self._ref, layer, k.data_ptr(), v.data_ptr(), _type(dtype, "k"), step.rows, ks[0],
-                                         ks[1], vs[0], vs[1], step._slot, _stream(i))
-        if status:
-            _raise(status)
+        _call(i, self.lib.ssd_kv8_append, self._ref, layer, k.data_ptr(), v.data_ptr(), _type(dtype, "k"), step.rows,
+              ks[0], ks[1], vs[0], vs[1], step._slot)
 
     def read(self, layer: int, slots: torch.Tensor, dtype: torch.dtype = torch.float32):
         """ssd_kv8_read: the (k, v) values held at int32 `slots`, each [n][n_kv_heads][head_dim]."""
@@ -166,9 +171,7 @@ class KV8Cache:
         shape = (n, self.n_kv_heads, self.head_dim)
         k = torch.empty(shape, dtype=dtype, device=self.device)
         v = torch.empty(shape, dtype=dtype, device=self.device)
-        status = self.lib.ssd_kv8_read(self._ref, layer, at, n, k.data_ptr(), v.data_ptr(), code, _stream(i))
-        if status:
-            _raise(status)
+        _call(i, self.lib.ssd_kv8_read, self._ref, layer, at, n, k.data_ptr(), v.data_ptr(), code)
         return k, v
 
     def attention(self, layer: int, q: torch.Tensor, step: KV8Step, out: torch.Tensor | None = None,
@@ -187,19 +190,14 @@ class KV8Cache:
             os = _rows3(out, step._q, i, "out")
             if out.dtype is not dtype:
                 _fail(f"q and out: one type expected, got {dtype} and {out.dtype}")
-        status = self.lib.ssd_kv8_attention(
-            self._ref, layer, step._ref, q.data_ptr(), out.data_ptr(), _type(dtype, "q"), qs[0], qs[1], os[0], os[1],
-            self._scale if scale is None else scale,
-            None if row_mask is None else _int32(row_mask, (step.rows,), i, "row_mask"), _stream(i))
-        if status:
-            _raise(status)
+        _call(i, self.lib.ssd_kv8_attention, self._ref, layer, step._ref, q.data_ptr(), out.data_ptr(), _type(dtype, "q"),
+              qs[0], qs[1], os[0], os[1], self._scale if scale is None else scale,
+              None if row_mask is None else _int32(row_mask, (step.rows,), i, "row_mask"))
         return out
 
     def check(self) -> None:
         """Wait for the stream and raise SSDError if a call met bad lengths, slots or values (ssd_kv8_status)."""
-        status = self.lib.ssd_kv8_status(self._ref, None, _stream(self._index))
-        if status:
-            _raise(status)
+        _call(self._index, self.lib.ssd_kv8_status, self._ref, None)
 
 
 class W4Weight:
@@ -218,17 +216,13 @@ class W4Weight:
         self._index = weight.get_device()
         self.packed = torch.empty(size, dtype=torch.uint8, device=weight.device)
         self._packed = self.packed.data_ptr()
-        status = self.lib.ssd_w4_pack(weight.data_ptr(), _type(weight.dtype, "weight"), self.n, self.k, weight.stride(0),
-                                      group, self._packed, _stream(self._index))
-        if status:
-            _raise(status)
+        _call(self._index, self.lib.ssd_w4_pack, weight.data_ptr(), _type(weight.dtype, "weight"), self.n, self.k,
+              weight.stride(0), group, self._packed)
 
     def dequantize(self) -> torch.Tensor:
         """The fp32 values [n][k] the packed codes stand for."""
         out = torch.empty((self.n, self.k), dtype=torch.float32, device=self.device)
-        status = self.lib.ssd_w4_unpack(self._packed, self.n, self.k, self.group, out.data_ptr(), _stream(self._index))
-        if status:
-            _raise(status)
+        _call(self._index, self.lib.ssd_w4_unpack, self._packed, self.n, self.k, self.group, out.data_ptr())
         return out
 
     def _rows(self, t: torch.Tensor, shape: tuple, dtype: torch.dtype, what: str) -> int:
@@ -257,11 +251,8 @@ class W4Weight:
         px, work = x.data_ptr(), None
         if code or self.k % 128 or xs % 8 or px % 16:
             work = torch.empty(self._work, dtype=torch.uint8, device=self.device)
-        status = self.lib.ssd_w4_matmul(
-            self._packed, self.n, self.k, self.group, px, code, rows, xs, out.data_ptr(), os,
-            None if residual is None else residual.data_ptr(),
-            0 if residual is None else self._rows(residual, (rows, self.n), dtype, "residual"),
-            self._packed if work is None else work.data_ptr(), _stream(i))
-        if status:
-            _raise(status)
+        _call(i, self.lib.ssd_w4_matmul, self._packed, self.n, self.k, self.group, px, code, rows, xs, out.data_ptr(), os,
+              None if residual is None else residual.data_ptr(),
+              0 if residual is None else self._rows(residual, (rows, self.n), dtype, "residual"),
+              self._packed if work is None else work.data_ptr())
         return out

@@ -1,8 +1,11 @@
 """Low-bit operators without a GPU: struct layouts, sizes and the refusals that come before any device call."""
+import contextlib
 import ctypes
 import os
+import types
 
 import pytest
+import torch
 
 import paper_2510_22641_gb300 as lib
 from paper_2510_22641_gb300 import _binding as B
@@ -138,3 +141,96 @@ def test_header_compiles_as_c(tmp_path):
     src.write_text('#include "ssd.h"\nint main(void) { return SSD_W4_MAX_ROWS == 16 ? 0 : 1; }\n')
     inc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
     assert os.system(f"gcc -Wall -Werror -I{inc} {src} -o {tmp_path / 'h'} && {tmp_path / 'h'}") == 0
+
+
+class _FakeTensor:
+    """Enough of a contiguous tensor on GPU 1 for the wrappers' checks; its address is never followed."""
+    is_cuda = True
+
+    def __init__(self, shape, dtype):
+        self.shape, self.dtype, self.device = torch.Size(shape), dtype, torch.device("cuda", 1)
+
+    def get_device(self):
+        return 1
+
+    def numel(self):
+        return self.shape.numel()
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self, i=None):
+        s = [self.shape[j + 1:].numel() for j in range(len(self.shape))]
+        return tuple(s) if i is None else s[i]
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return id(self) % (1 << 30) * 4096
+
+    def __getitem__(self, i):
+        return _FakeTensor((len(range(*i.indices(self.shape[0]))),), self.dtype)
+
+    def __setitem__(self, i, v):
+        pass
+
+
+class _FakeTorch:
+    """torch with fake allocations, and GPU 0 current."""
+
+    def __init__(self):
+        self.current = 0
+        self.cuda = types.SimpleNamespace(current_device=lambda: self.current, device=self.enter)
+
+    def __getattr__(self, name):
+        return getattr(torch, name)
+
+    def empty(self, shape, *_, dtype, device):
+        assert torch.device(device) == torch.device("cuda", 1)
+        return _FakeTensor((shape,) if isinstance(shape, int) else shape, dtype)
+
+    zeros = full = empty
+
+    def arange(self, a, b, c, dtype, device):
+        return self.empty(len(range(a, b, c)), dtype=dtype, device=device)
+
+    @contextlib.contextmanager
+    def enter(self, i):
+        before, self.current = self.current, i
+        yield
+        self.current = before
+
+
+def test_calls_on_another_device_than_the_current_one_enter_it(l, monkeypatch):
+    """Kernels are launched on the current device, and a default stream is the same null handle on each."""
+    from paper_2510_22641_gb300 import lowbit
+    fake, calls = _FakeTorch(), []
+
+    class Lib:
+        def __getattr__(self, name):
+            if name.endswith(("_bytes", "_ints")):
+                return getattr(l, name)
+            return lambda *a: calls.append((name, fake.current)) or 0
+
+    monkeypatch.setattr(lowbit, "torch", fake)
+    monkeypatch.setattr(lowbit, "_stream", lambda i: 0)
+    monkeypatch.setattr(lowbit, "_current", lambda: fake.current, raising=False)
+    monkeypatch.setattr(lowbit.B, "load", Lib)
+    bf16, i32 = torch.bfloat16, torch.int32
+    c = lowbit.KV8Cache(1, 4, 2, 64, 16, 8, 2, 4, device="cuda:1")
+    step = c.new_step(2, 3)
+    kv, q = _FakeTensor((3, 2, 64), bf16), _FakeTensor((3, 4, 64), bf16)
+    c.plan(step, _FakeTensor((2,), i32), _FakeTensor((2,), i32))
+    c.append(0, kv, kv, step)
+    c.read(0, _FakeTensor((5,), i32))
+    c.attention(0, q, step)
+    c.check()
+    w = lowbit.W4Weight(_FakeTensor((32, 256), bf16))
+    w.dequantize()
+    w.matmul(_FakeTensor((3, 256), bf16))
+    w.matmul(_FakeTensor((3, 256), torch.float32))
+    assert [n for n, _ in calls] == ["ssd_kv8_plan", "ssd_kv8_append", "ssd_kv8_read", "ssd_kv8_attention",
+                                     "ssd_kv8_status", "ssd_w4_pack", "ssd_w4_unpack", "ssd_w4_matmul", "ssd_w4_matmul"]
+    assert [d for _, d in calls] == [1] * len(calls)
+    assert fake.current == 0
