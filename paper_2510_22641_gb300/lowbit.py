@@ -117,6 +117,8 @@ class KV8Cache:
             _fail(f"KV8Cache: unsupported shape ({n_layers=}, {n_heads=}, {n_kv_heads=}, {head_dim=}, {block_tokens=}, "
                   f"{n_blocks=}, {max_batch=}, {max_blocks=})")
         device = torch.device(device)
+        if device.type != "cuda":
+            _fail(f"KV8Cache: a CUDA device expected, got {device}")
         if device.index is None:
             device = torch.device("cuda", torch.cuda.current_device())
         self.device = device

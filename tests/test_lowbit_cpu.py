@@ -234,3 +234,11 @@ def test_calls_on_another_device_than_the_current_one_enter_it(l, monkeypatch):
                                      "ssd_kv8_status", "ssd_w4_pack", "ssd_w4_unpack", "ssd_w4_matmul", "ssd_w4_matmul"]
     assert [d for _, d in calls] == [1] * len(calls)
     assert fake.current == 0
+
+
+@pytest.mark.parametrize("device", ["cpu", "meta"])
+def test_a_cache_on_no_gpu_is_refused(l, device, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)   # a GPU that it must not be moved to
+    with pytest.raises(lib.SSDError) as e:
+        lib.KV8Cache(1, 4, 2, 64, 16, 8, 2, 4, device=device)
+    assert e.value.status == INVALID
