@@ -588,7 +588,8 @@ SSD_API ssd_status ssd_w4_unpack(const void* packed, int n, int k, int group, fl
 
 /* y = x W^T (+ residual), rows <= SSD_W4_MAX_ROWS, fp32 sums, each group's products scaled in fp32.
  *   x: device, type SSD_TYPE_*, [rows][x_row_stride];  y: same type, [rows][y_row_stride]
- *   residual: device [rows][res_row_stride] of the same type, or NULL; may be y itself
+ *   residual: device [rows][res_row_stride] of the same type, or NULL; may be y itself (same rows), else must
+ *     not overlap it
  *   work: device, ssd_w4_work_bytes(), 16-byte aligned, of this call alone until it has run.  Neither read
  *     nor written for bf16 rows with k and x_row_stride multiples of 128 and 8 and x 16-byte aligned.
  * y must not overlap x.  bf16 rows enter the products as they are; fp32 rows as pairs of fp16, each

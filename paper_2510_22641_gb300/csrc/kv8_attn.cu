@@ -712,6 +712,9 @@ ssd_status ssd_kv8_attention(const ssd_kv8* c, int layer, const ssd_kv8_step* st
   const int size = type == SSD_TYPE_FP32 ? 4 : 2;
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(o)) % size)
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_attention: q and o must be aligned to their elements");
+  const OpRows qr{q, step->rows, c->n_heads, q_row_stride, q_head_stride, c->head_dim},
+      outr{o, step->rows, c->n_heads, o_row_stride, o_head_stride, c->head_dim};
+  if (op_overlap(qr, outr, size)) return op_fail(SSD_ERR_INVALID_ARG, "ssd_kv8_attention: o overlaps q");
   Kv8AttnParams p;
   p.q = q;
   p.o = o;

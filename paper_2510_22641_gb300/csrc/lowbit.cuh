@@ -45,6 +45,55 @@ ssd_status op_launch(const char* what, void (*kernel)(P...), dim3 grid, int thre
 // The status of a launch that has just been made.
 ssd_status op_launched(const char* what);
 
+// ------------------------------------------------------------------ operands that share memory
+
+// Elements p + r * row + h * head + [0, width) of a buffer, r < rows, h < heads.
+struct OpRows {
+  const void* p;
+  int64_t rows, heads, row, head, width;
+};
+// Whether two of them, of elements of `size` bytes, share an element.  Almost always the address ranges are apart;
+// else rows that lie between each other (slices of one buffer) are told from rows that overlap.
+inline bool op_overlap(OpRows a, OpRows b, int size) {
+  using Int = __int128;
+  auto span = [](const OpRows& x, Int& lo, Int& hi) {  // elements from x.p on
+    const Int r = static_cast<Int>(x.rows - 1) * x.row, h = static_cast<Int>(x.heads - 1) * x.head;
+    lo = (r < 0 ? r : 0) + (h < 0 ? h : 0);
+    hi = (r > 0 ? r : 0) + (h > 0 ? h : 0) + x.width;
+  };
+  Int alo, ahi, blo, bhi;
+  span(a, alo, ahi);
+  span(b, blo, bhi);
+  const Int delta = (static_cast<Int>(reinterpret_cast<uintptr_t>(b.p)) - reinterpret_cast<uintptr_t>(a.p)) / size;
+  if (delta + bhi <= alo || ahi <= delta + blo) return false;
+  for (OpRows* x : {&a, &b})
+    if (x->head == x->width) x->width *= x->heads, x->heads = 1, x->head = 0;  // one piece per row
+  // whether -b.width < c + r * s < a.width for a whole r in [lo, hi]
+  auto meets = [&](Int c, Int s, Int lo, Int hi) -> bool {
+    if (s < 0) {
+      s = -s;
+      const Int t = lo;
+      lo = -hi, hi = -t;
+    }
+    if (s == 0) return lo <= hi && -b.width < c && c < a.width;
+    auto floor_div = [](Int x, Int y) -> Int { return x / y - (x % y < 0 ? 1 : 0); };  // y > 0
+    const Int first = floor_div(-b.width - c, s) + 1, last = -floor_div(c - a.width, s) - 1;
+    return (first > lo ? first : lo) <= (last < hi ? last : hi);
+  };
+  if (a.row == b.row && a.head == b.head) {  // differences of rows and heads
+    for (int64_t h = 1 - a.heads; h < b.heads; ++h)
+      if (meets(delta + static_cast<Int>(h) * a.head, a.row, 1 - a.rows, b.rows - 1)) return true;
+    return false;
+  }
+  for (int64_t r = 0; r < a.rows; ++r)
+    for (int64_t h = 0; h < a.heads; ++h)
+      for (int64_t g = 0; g < b.heads; ++g)
+        if (meets(delta + static_cast<Int>(g) * b.head - static_cast<Int>(h) * a.head - static_cast<Int>(r) * a.row, b.row,
+                  0, b.rows - 1))
+          return true;
+  return false;
+}
+
 // ------------------------------------------------------------------ cache layout
 //
 // A tile is 16 tokens of one block and kv head: 16 * D bytes of K, then 16 * D of V, a code c

@@ -197,6 +197,12 @@ ssd_status ssd_w4_matmul(const void* packed, int n, int k, int group, const void
   const int size = type == SSD_TYPE_FP32 ? 4 : 2;
   if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y) | reinterpret_cast<uintptr_t>(residual)) % size)
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_w4_matmul: rows must be aligned to their elements");
+  const OpRows xr{x, rows, 1, x_row_stride, 0, k}, yr{y, rows, 1, y_row_stride, 0, n},
+      rr{residual, rows, 1, res_row_stride, 0, n};
+  if (op_overlap(xr, yr, size)) return op_fail(SSD_ERR_INVALID_ARG, "ssd_w4_matmul: y overlaps x");
+  const bool in_place = residual == y && (rows == 1 || res_row_stride == y_row_stride);
+  if (residual && !in_place && op_overlap(rr, yr, size))
+    return op_fail(SSD_ERR_INVALID_ARG, "ssd_w4_matmul: y overlaps the residual and is not the same rows");
   const WorkLayout lay = work_layout(k);
   uint8_t* wk = static_cast<uint8_t*>(work);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);

@@ -637,3 +637,24 @@ def test_attention_flags_requests_of_more_rows_than_a_mask_has_bits():
     q = rows((64, 2, 64), 5, torch.float32)
     f.cache.attention(0, q, f.step, row_mask=ints([-1] * 64))
     assert status(f.cache) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attention_into_the_buffer_of_its_queries(dtype):
+    """Heads, dimensions or rows beside the queries are fine; theirs are refused."""
+    f = Filled(32, 4, 2, 64, 2, 3, DT[dtype])
+    f.append([50, 9])
+    f.append([3, 4])
+    for q_of, o_of in ((lambda b: b[:, :4, :64], lambda b: b[:, 4:, :64]), (lambda b: b[:, ::2, 64:], lambda b: b[:, 1::2, 64:]),
+                       (lambda b: b[:, :4, :64], lambda b: b[:, :4, 64:])):
+        buf = rows((7, 8, 128), 3, DT[dtype])
+        q = q_of(buf).clone()
+        o = f.cache.attention(0, q_of(buf), f.step, out=o_of(buf))
+        check_attention(f, q, o, 64 ** -0.5)
+        assert torch.equal(q_of(buf), q)
+    keep = buf.clone()
+    for o in (buf[:, :4, :64], buf[:, 1:5, :64], buf[:, :4, 1:65]):
+        with pytest.raises(lib.SSDError) as e:
+            f.cache.attention(0, buf[:, :4, :64], f.step, out=o)
+        assert e.value.status == 1 and "overlaps" in str(e.value)
+    assert torch.equal(buf, keep)

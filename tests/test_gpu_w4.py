@@ -217,3 +217,24 @@ def test_matmul_beside_an_outlier_that_the_weights_do_not_see(size, group, rows,
         bound = bound + 2.0 ** -8 * want.abs()
     err = (y.double() - want).abs()
     assert (err <= bound).all(), f"{(err > bound).sum().item()} of {err.numel()}, worst {(err / bound).max().item()}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_matmul_into_the_buffer_of_its_rows(dtype):
+    """Columns beside x and the residual are fine; columns of theirs are refused."""
+    w = lib.W4Weight(normal((128, 128), 1, 0.05), 64)
+    buf = normal((5, 3 * 128), 2, 1.0, DT[dtype])
+    x, out, res = buf[:, :128], buf[:, 128:256], buf[:, 256:]
+    before = buf.clone()
+    w.matmul(x, out=out, residual=res)
+    check(out, before[:, :128], w.dequantize(), before[:, 256:])
+    assert torch.equal(x, before[:, :128]) and torch.equal(res, before[:, 256:])
+    keep = buf.clone()
+    for f in (lambda: w.matmul(x, out=x), lambda: w.matmul(x, out=buf[:, 127:255]), lambda: w.matmul(x[:3], out=x[2:]),
+              lambda: w.matmul(x, out=out, residual=buf[:, 129:257])):
+        with pytest.raises(lib.SSDError) as e:
+            f()
+        assert e.value.status == 1 and "overlaps" in str(e.value)
+    assert torch.equal(buf, keep)
+    w.matmul(x[:2], out=buf[2:4, :128])   # other rows of the same columns
+    check(buf[2:4, :128], keep[:2, :128], w.dequantize())

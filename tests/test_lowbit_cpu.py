@@ -242,3 +242,30 @@ def test_a_cache_on_no_gpu_is_refused(l, device, monkeypatch):
     with pytest.raises(lib.SSDError) as e:
         lib.KV8Cache(1, 4, 2, 64, 16, 8, 2, 4, device=device)
     assert e.value.status == INVALID
+
+
+def test_outputs_over_inputs_are_refused(l):
+    """Some CTAs would read what others have written.  Slices of one buffer that lie between each other are no
+    overlap (the GPU tests run them)."""
+    c, s = cache(), step()   # 4 rows of 8 heads of 128 elements
+    r, t = ctypes.byref(c), ctypes.byref(s)
+    base = 1 << 20
+    for size, type in ((2, 0), (4, 1)):
+        whole = (1024, 128)
+        for at, strides in ((0, whole), (127, whole), (-1023, whole), (4 * 1024 - 1, whole), (0, (2048, 128)),
+                            (0, (128, 512)), (1000, (1024, 130))):
+            got = l.ssd_kv8_attention(r, 0, t, base, base + at * size, type, *whole, *strides, 1.0, None, None)
+            assert got == INVALID and b"overlaps" in l.ssd_op_last_error(), (at, strides)
+        # every second head of q, and the heads between them moved by one element
+        assert l.ssd_kv8_attention(r, 0, t, base, base + 129 * size, type, 2048, 256, 2048, 256, 1.0, None, None) == INVALID
+
+        def matmul(y, y_row, x_row=64, residual=None, res_row=0):
+            return l.ssd_w4_matmul(256, 64, 64, 32, base, type, 4, x_row, base + y * size, y_row,
+                                   None if residual is None else base + residual * size, res_row, 256, None)
+
+        for y, y_row in ((0, 64), (63, 64), (-63, 64), (255, 64), (0, 100)):
+            assert matmul(y, y_row) == INVALID and b"overlaps x" in l.ssd_op_last_error(), (y, y_row)
+        assert matmul(65, 128, x_row=128) == INVALID   # columns 65.. of the rows whose columns ..63 are x: row 1's
+        for residual, res_row in ((4097, 64), (4096 - 64, 64), (4096, 65)):
+            assert matmul(4096, 64, residual=residual, res_row=res_row) == INVALID
+            assert b"residual" in l.ssd_op_last_error()
