@@ -658,3 +658,20 @@ def test_attention_into_the_buffer_of_its_queries(dtype):
             f.cache.attention(0, buf[:, :4, :64], f.step, out=o)
         assert e.value.status == 1 and "overlaps" in str(e.value)
     assert torch.equal(buf, keep)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+def test_append_of_prompts_that_go_on_in_a_block(block, dim, dtype):
+    """The prompts' kernel (one seat, more than 16 rows a call) where the first rows go to a block that holds
+    older ones: in the middle of a tile or on a tile's edge, with scales that grow or stay."""
+    f = Filled(block, 3, 3, dim, 1, 5 + 260 // block, DT[dtype])
+    for add, size in ((block + 5, 1.0), (40, 30.0), (17, 0.01), (block + 19, 100.0), (33, 100.0)):
+        kv = [rows((add, 3, dim), f.seed + i + add, torch.float32) * size for i in range(2)]
+        kv[0][:, 1] *= 1e-3
+        f.append([add], kv=[x.to(DT[dtype]) for x in kv])
+        f.check_values()
+        if add == 17:   # rejected rows: the next call starts at a tile's edge
+            f.length[0] = f.length[0] // 16 * 16
+    assert status(f.cache) == 0
