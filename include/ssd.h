@@ -540,7 +540,13 @@ SSD_API ssd_status ssd_kv8_plan(const ssd_kv8* c, const ssd_kv8_step* step, cons
  * Per block, kv head and K / V: s' = max(s, amax / 127, 2^-100) with amax over the block's finite new
  * values and s the block's scale, or 0 when a row goes to the block's first token.  If s' > s, the
  * block's older codes become round(c * (s / s')).  New codes are round(x * (1 / s')) in -127..127, in
- * fp32, ties to even. */
+ * fp32, ties to even.
+ * So what a token is held as depends on the rows that its block got later, rejected drafts among them (a
+ * smaller len takes their rows back, not their part in the scale), and on how many rows a call brought: a
+ * decode with drafts and one without hold the same tokens within the bound below, not as the same codes,
+ * and may part where two logits are that close.  A finite value appended at scale s_0 and rounded again at
+ * scales s_1 < .. < s_r is off by at most (1/2 + 2^-14) (s_0 + .. + s_r), at most (r + 1) (1/2 + 2^-14)
+ * times the block's scale. */
 SSD_API ssd_status ssd_kv8_append(const ssd_kv8* c, int layer, const void* k, const void* v, int type, int rows,
                                   int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride,
                                   int64_t v_head_stride, const int32_t* slot, void* cuda_stream);

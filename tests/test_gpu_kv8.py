@@ -675,3 +675,31 @@ def test_append_of_prompts_that_go_on_in_a_block(block, dim, dtype):
         if add == 17:   # rejected rows: the next call starts at a tile's edge
             f.length[0] = f.length[0] // 16 * 16
     assert status(f.cache) == 0
+
+
+@pytest.mark.parametrize("few", [True, False])
+def test_values_rounded_again_stay_within_their_bound(few):
+    """A value appended at scale s_0 and rounded again at each of r growths is off by at most half of each of the
+    scales it was rounded at, so by (r + 1) / 2 of the block's scale: 1 / 2 for exact products, 2^-14 more a
+    rounding for fp32 ones (codes up to 127, a few roundings to 24 bits each)."""
+    block, n = 128, 8 if few else 18   # few: the decode steps' kernel
+    f = Filled(block, 2, 2, 64, 1, 1, torch.float32)
+    at, scales = [], []
+    for i in range(7):
+        f.append([n], kv=[rows((n, 2, 64), 7 + i + j, torch.float32) * 1.3 ** i for j in range(2)])
+        at.append(f.kv)
+        scales.append([r.scales[f.step.slot[0].item() // block].astype(np.float64) for r in f.ref])
+    got = f.cache.read(0, ints(f.slots_of(0)))
+    most = 0
+    for j in range(2):
+        for i in range(7):
+            total, r = scales[i][j].copy(), 0
+            for t in range(i + 1, 7):
+                grown = scales[t][j] > scales[t - 1][j]
+                total += np.where(grown, scales[t][j], 0)
+                r = r + grown
+            most = max(most, np.max(r))
+            assert (total <= (r + 1) * scales[6][j]).all()
+            err = (got[j][i * n:(i + 1) * n].double() - at[i][j].double()).abs().amax((0, 2)).cpu().numpy()
+            assert (err <= (0.5 + 2.0 ** -14) * total).all()
+    assert most >= 2
