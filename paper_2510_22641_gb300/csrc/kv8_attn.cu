@@ -13,13 +13,14 @@
 // row, raised with m to at least every p vs, so that neither tiny nor huge V blocks lose bits; O is kept in
 // units of B / 2^7.
 //
-// Bound: bytes.  A cached token costs 2 D bytes and 4 D rows flops, below the tensor rate up to about
-// 16 rows; so the design is a stream of the cache at full width.  The tile layout (lowbit.cuh) lets
-// each lane copy the 16-byte pieces that it alone reads, with cp.async into its warp's own ring of three
-// tiles or more: no barrier between the copies and their use.  Measured: 64 requests of up to 8191 tokens,
-// 32 / 8 heads, two bf16 rows 110 us, 6.1 TB/s; 16 of 1024, 40 heads, seven fp32 rows 32 us (3.5 TB/s:
-// 12 tiles a warp, then the merge); two of 131072, six rows, 24 query rows a kv head 106 us (4.3 TB/s:
-// 8 warps an SM, the accumulators take the registers); one row over 640 tokens 9.7 us (latency).
+// Bound: bytes.  A cached token of a kv head costs 2 D bytes and 4 D flops per query row (times grouped heads),
+// below these products' rate up to about 16 rows; so the design is a stream of the cache at full width.  The
+// tile layout (lowbit.cuh) lets each lane copy the 16-byte pieces that it alone reads, with cp.async into its
+// warp's own ring of three tiles or more: no barrier between the copies and their use.  Measured: 64 requests
+// of up to 8191 tokens, 32 / 8 heads, two bf16 rows 112 us, 6.0 TB/s; 16 of 1024, 40 heads, seven fp32 rows 32 us (3.5 TB/s:
+// 12 tiles a warp, then the merge); two of 131072, six rows, 24 query rows a kv head 106 us (4.3 TB/s: the
+// accumulators leave 8 warps an SM, which wait for dependent results: issue 45 %, DRAM 51 %, tensor pipe 38 %);
+// one row over 640 tokens 9.7 us (latency).
 //
 // Work is the flat list of 16-token tiles of all (request, kv head, row group) segments, cut by the plan
 // into equal spans, one per team of W warps, a CTA or less.  A team's warps take a segment's tiles in turn

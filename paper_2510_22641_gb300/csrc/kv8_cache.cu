@@ -598,7 +598,7 @@ __device__ __forceinline__ int list_runs(Runs& runs, const int32_t* slot, int be
 // ones, or the scale has grown, it is read first.
 //
 // Prompts; bound: bytes.  A CTA of 8 warps takes 8 / (block / 16) jobs at a time and every `takers`-th of
-// its window's blocks, so that rows that stand for none cost nothing.  29,000 rows of 8 prompts, 8 heads,
+// its window's blocks, so that rows that stand for none cost nothing.  43,565 rows of 8 prompts, 8 heads,
 // bf16: 74 us, 41 % of the DRAM rate (16 warps an SM: a tile's values take 64 registers).
 template <typename T, int D, bool VEC>
 __global__ void __launch_bounds__(256, 2) ssd_kv8_append_kernel(const AppendParams p) {
@@ -919,7 +919,8 @@ ssd_status ssd_kv8_append(const ssd_kv8* c, int layer, const void* k, const void
   p.v_head = v_head_stride;
   p.slot = slot;
   p.rows = rows;
-  // as many CTAs per window as blocks usually begin in it: every block_tokens rows, and with each request
+  // as many CTAs per window as blocks may begin in it: every block_tokens rows, and with each request (the call
+  // does not know how many there are: at most one a seat)
   const int in_window = rows < kWindow ? rows : kWindow;
   p.takers = static_cast<int>(in_window / c->block_tokens + static_cast<int64_t>(c->max_batch) * in_window / rows + 1);
   p.shift = log2_of(c->block_tokens);
@@ -931,9 +932,12 @@ ssd_status ssd_kv8_append(const ssd_kv8* c, int layer, const void* k, const void
   p.status = static_cast<int32_t*>(c->work);
   const bool vec = aligned4(k, size, k_row_stride, k_head_stride) && aligned4(v, size, v_row_stride, v_head_stride);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  // A warp per row and head where rows of a block are few (at most the 16 rows of a decode step for every
-  // seat); a warp per 16 tokens of a block else.  62 rows of 16 requests, 40 heads, blocks of 32: 4.9 and 22 us;
-  // a prompt of 640 rows, 32 heads, blocks of 64: 42 and 7.0 us.
+  // A warp per row and head where rows of a block are few; a warp per 16 tokens of a block else.  The call knows
+  // its rows but not its requests, so the rule takes the seats for them: at most the 16 rows of a decode step
+  // for each.  Where every seat takes part that is right: 62 rows of 16 requests, 40 heads, blocks of 32 take 4.9
+  // and 22 us, a prompt of 640 rows in a cache of one seat, 32 heads, blocks of 64, 42 and 7.1 us.  A prompt of
+  // up to 16 rows a seat in a cache of many gets the slow one: those 640 rows take 9.1 us with 16 seats, 42 us
+  // with 64 or more.
   const bool few = rows <= SSD_MAX_ROWS * c->max_batch;
   const int per_cta = 128 / c->block_tokens;  // jobs
   const dim3 grid = few ? dim3(rows, (c->n_kv_heads + 1) / 2)

@@ -250,10 +250,13 @@ __host__ __device__ __forceinline__ StepView step_view(int32_t* d, int batch) {
 
 // Query rows (of one kv head) one attention item takes.  Items of 8 have the most warps per SM and the
 // fewest empty columns where requests differ, but more of them read the same tiles; so they are the choice
-// where the tiles come from L2: a layer's cache of at most 128 MB (96 rows for one kv head, 72 MB: items of
-// 24 rows 71 us, of 8 64; 28 rows, 16 MB: 33 and 21 us; 16 rows of a kv head and 186 MB: items of 16 55, of 8
-// 49; 24 rows, 147 MB: of 24 50, of 8 58).  Else as many as there usually are, in the fewest items of at
-// most 32 (24 rows, 900 MB: items of 24 111 us, of 8 182).
+// where the tiles come from L2: a layer's cache of at most 128 MB, about L2's size (12 rows of a kv head, 75 MB:
+// items of 8 rows 29 us, of 16 34; 16 rows, 89 MB: 31 and 44 us; 32 rows, 132 MB: 52 and 51).  Else as many as
+// there usually are, in the fewest items of at most 32 (24 rows, 147 MB: of 24 50 us, of 8 58; 900 MB: 111 and
+// 182).  Measured in caches as large as their content.  The host knows the capacity only, so a large pool that
+// holds short contexts gets the larger items where 8 would be faster (256 requests of 300 tokens, 16 rows:
+// 85 us, of 8 54).  Where the content is just above L2 either may be (64 requests of 2000 tokens, 16 rows,
+// 186 MB: of 16 55 us, of 8 49).
 constexpr int64_t kItemsOf8Bytes = 128ll << 20;
 inline int step_row_tile(const ssd_kv8* c, const ssd_kv8_step* s) {
   if (s->row_tile) return s->row_tile;

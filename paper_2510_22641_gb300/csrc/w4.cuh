@@ -37,9 +37,10 @@ __host__ __device__ constexpr int w4_bit(int row, int col) {
 //     of the result beside one of 1e4, 0.4 beside 1e6.)
 //   fp32 rows are scaled per row and chunk by a power of two to 2^14 .. 2^15 and split into a high and a
 //     low half (22 bits, and to 2^-39 of the chunk's largest); u goes into the mantissa of the half 1024,
-//     and one subtraction (or fused multiply) per pair gives the codes.  (u read as a subnormal half
-//     would need no arithmetic, but the matrix unit aligns its sums by the exponents of the operands, so
-//     a subnormal operand costs its leading zeros: 10 bits, measured 1e-5 of the result.)
+//     and one subtraction (or fused multiply) per pair gives the codes.  Integers put into a mantissa so are
+//     a published way to unpack them (Kim et al., "Who Says Elephants Can't Run", 2022).  (u read as a
+//     subnormal half would need no arithmetic, but the matrix unit aligns its sums by the exponents of the
+//     operands, so a subnormal operand costs its leading zeros: 10 bits, measured 1e-5 of the result.)
 // Each group's sum is multiplied by its scale in fp32 and added to the fp32 sums.
 //
 // Bound: bytes, n k / 2 of codes.  The row tiles are dealt out evenly, once, to the teams of W warps
@@ -50,10 +51,10 @@ __host__ __device__ constexpr int w4_bit(int row, int col) {
 // lanes read back the bytes they copied, the scales are shared within the warp.
 //
 // Measured (device time, of the copy rate): 32000 x 4096, one bf16 row 17.3 us, 57 %; 16 rows 23.4 us, 42 %;
-// one fp32 row 18.0 us, 55 %; 8 rows 22.5 us, 44 %; 16 rows 35.2 us, 28 %; 4096 x 4096, one bf16 row 4.4 us
-// (launch, one round of loads, the sum).  137 to 174 instructions a record, half of them unpacking, against
-// the 180 issue slots that a record's bytes leave at the copy rate; 16 fp32 rows wait for their products
-// with 8 warps an SM.
+// one fp32 row 18.0 us, 55 %; 8 rows 22.4 us, 44 %; 16 rows 35.1 us, 28 %; 4096 x 4096, one bf16 row 4.6 us
+// (launch, one round of loads, the sum).  162 to 195 instructions a record, about half of them unpacking,
+// against the 180 issue slots that a record's bytes leave at the copy rate.  Neither is used up (issue 51 to
+// 59 %, DRAM 37 to 48 %): 16 warps an SM (8 for 16 fp32 rows) wait for fixed latencies and the logic pipe.
 
 constexpr int kW4Warps = 8;
 constexpr int kW4Threads = 32 * kW4Warps;
@@ -76,12 +77,12 @@ struct W4Params {
 template <int PARTS, int NB, int MT>
 struct W4Geo {
   // per SM: two, but for 16 fp32 rows, whose operands take the registers (32000 x 4096: one bf16 row with
-  // one CTA 20.5 us, two 16.8; 16 bf16 rows 30.0 and 23.9; 8 fp32 rows 27.7 and 22.5)
+  // one CTA 21.1 us, two 17.2; 16 bf16 rows 28.7 and 23.4; 8 fp32 rows 26.1 and 22.4)
   static constexpr int kCtas = PARTS * NB <= 2 ? 2 : 1;
   static constexpr int kStages = kCtas == 1 ? 18 : NB == 1 ? 9 : 8;  // records
   // whether the next chunk's activations are fetched ahead: where one CTA has the registers and few tiles
-  // cover the wait (16 fp32 rows, 4096 x 4096: ahead 9.2 us, not ahead 9.6; 16 bf16 rows, 32000 x 4096, with
-  // spills: 30.8 and 23.9)
+  // cover the wait (16 fp32 rows, 4096 x 4096: ahead 9.2 us, not ahead 9.6; 8 fp32 rows, 4096 x 4096, with
+  // spills: 7.9 and 7.4; 16 bf16 rows, 32000 x 4096, with spills: 30.5 and 23.4)
   static constexpr bool kAhead = PARTS * NB == 4 && MT <= 4;
   static constexpr int kRing = kStages * kW4MaxRec;    // per warp
   static constexpr int kPart = MT > 4 ? MT / 2 : NB == 2 && MT > 2 ? 2 : MT;  // tiles merged at a time

@@ -1,6 +1,6 @@
 """Python face of the low-bit operators (include/ssd.h): a paged 8-bit K/V cache and 4-bit weights.
 
-The classes own torch buffers and forward every call to the library on the current CUDA stream.  No
+The classes own torch buffers and forward every call to the library on their device's current stream.  No
 computation happens here.  Calls of one KV8Cache share its workspace, so calls from several streams
 must be ordered by the caller.  Everything but KV8Cache.check runs asynchronously and may be captured
 into a CUDA graph after a first call outside of it.
