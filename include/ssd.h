@@ -460,8 +460,8 @@ SSD_API ssd_status ssd_probe_bounded_wait(ssd_ctx* ctx, int64_t limit_ns);
  * Calls that share an ssd_kv8's or a matmul's workspace must be ordered (one stream, or events).
  * On failure ssd_op_last_error() holds a message for the calling thread. */
 
-/* Activation types. */
-enum { SSD_TYPE_BF16 = 0, SSD_TYPE_FP32 = 1 };
+/* Activation types (SSD_TYPE_F4: rows packed by ssd_f4_pack, where a call says that it takes them). */
+enum { SSD_TYPE_BF16 = 0, SSD_TYPE_FP32 = 1, SSD_TYPE_F4 = 2 };
 
 #define SSD_KV8_MAX_BATCH 1024  /* seats of one block table */
 #define SSD_KV8_STEP_HEAD 38928  /* ints before seg_start in a step's buffer */
@@ -605,6 +605,110 @@ SSD_API int64_t ssd_w4_work_bytes(int n, int k);
 SSD_API ssd_status ssd_w4_matmul(const void* packed, int n, int k, int group, const void* x, int type, int rows,
                                  int64_t x_row_stride, void* y, int64_t y_row_stride, const void* residual,
                                  int64_t res_row_stride, void* work, void* cuda_stream);
+
+/* ---- 4-bit floats: rows packed on both sides of a product, any number of rows ----
+ * The form of weights that prompts and verification passes of many rows multiply on the matrix units as they are
+ * held; the activations are packed on the way. */
+
+/* Rows [rows][k] in 4-bit floats, a scale per 16 columns and one per row:
+ *   rho = 2^e, the smallest power of two >= 2^-100 with max |x| <= 2688 rho over the row (2688 = 6 * 448);
+ *   y = x / rho;  per 16 columns s = max |y| / 6 rounded to e4m3;  codes y / s rounded to e2m1 (0 where s = 0),
+ * each quotient an fp32 quotient, rounded to nearest even, a code at most 6.  The value is c * s * rho.  k is padded
+ * with zeros.  A row with a NaN or an infinity stands for NaN in every column, the others are not touched by it.
+ * Rows below about 2^-90 keep fewer bits.  Packed as [128-row tile][256-column chunk]{codes, scales} in the order
+ * the matrix instructions take them, then rho [rows].  ssd_f4_bytes: -1 for a shape that is not supported
+ * (rows or k < 1, rows > 2^23, k > 2^20). */
+SSD_API int64_t ssd_f4_bytes(int rows, int k);
+
+/* Pack x: device, type SSD_TYPE_*, [rows][x_row_stride], aligned to its elements; packed: device, ssd_f4_bytes() of
+ * them, 16-byte aligned.  x and packed must not overlap. */
+SSD_API ssd_status ssd_f4_pack(const void* x, int type, int rows, int k, int64_t x_row_stride, void* packed,
+                               void* cuda_stream);
+
+/* The values of packed rows: out device [rows][k], type SSD_TYPE_* (c * s * rho rounded to it; exact but for rho near
+ * the ends of its range). */
+SSD_API ssd_status ssd_f4_unpack(const void* packed, int rows, int k, void* out, int type, void* cuda_stream);
+
+/* y = x W^T (+ residual) of packed w [n][k], fp32 sums of the codes' exact products, each row's scaled in fp32.
+ *   x: device, x_type SSD_TYPE_BF16 / FP32: [rows][x_row_stride], packed into work first (ssd_f4_bytes(rows, k),
+ *     16-byte aligned, of this call alone until it has run); SSD_TYPE_F4: rows packed by ssd_f4_pack
+ *     (x_row_stride and work are not looked at)
+ *   y: device, type SSD_TYPE_BF16 / FP32, [rows][y_row_stride];  residual: device [rows][res_row_stride] of the same
+ *     type, or NULL; may be y itself (same rows), else must not overlap it.  y must not overlap x, w or work. */
+SSD_API ssd_status ssd_f4_matmul(const void* w, int n, int k, const void* x, int x_type, int rows,
+                                 int64_t x_row_stride, void* y, int type, int64_t y_row_stride, const void* residual,
+                                 int64_t res_row_stride, void* work, void* cuda_stream);
+
+/* ---- Rotary positions, with the norms of query and key heads in the same pass ---- */
+
+#define SSD_ROTARY_MAX_AXES 4
+#define SSD_ROTARY_MAX_DIM 256
+
+/* How heads turn: of the first `turn` elements pair i (elements i and i + turn / 2, or 2 i and 2 i + 1 with
+ * interleaved != 0) is rotated by position[axis[i]] * step[i] turns, step a 64-bit fraction of a turn per position, so
+ * that angles are exact to pos * 2^-54 of a radian at any position.  The other elements pass through.
+ * ssd_rotary_init fills it; callers with other frequencies may write step and axis themselves. */
+typedef struct {
+  int head_dim;     /* elements of a head, even, 2 .. SSD_ROTARY_MAX_DIM */
+  int turn;         /* elements that turn, even, 0 .. head_dim */
+  int interleaved;  /* 0: pairs (i, i + turn / 2), 1: pairs (2 i, 2 i + 1) */
+  int axes;         /* positions per row, 1 .. SSD_ROTARY_MAX_AXES */
+  float eps;        /* of the norms */
+  uint8_t axis[SSD_ROTARY_MAX_DIM / 2];
+  uint64_t step[SSD_ROTARY_MAX_DIM / 2];
+} ssd_rotary;
+
+/* Frequencies theta^(-2 i / turn) radians a position; section [axes] (host): the pairs of each axis in order, which
+ * add up to turn / 2 (NULL with one axis).  theta >= 1. */
+SSD_API ssd_status ssd_rotary_init(ssd_rotary* r, int head_dim, int turn, int interleaved, int axes,
+                                   const int* section, double theta, float eps);
+
+/* The heads of one operand: x and y device, element (row, head, i) at row * row_stride + head * head_stride + i;
+ * y may be x itself (with the same strides), else must not overlap any x.  gain: device [head_dim] of gain_type or
+ * NULL; with it every head is x / sqrt(mean x^2 + eps) * gain before it turns. */
+typedef struct {
+  const void* x;
+  void* y;
+  int heads;
+  int64_t x_row, x_head, y_row, y_head;
+  const void* gain;
+  int gain_type;
+} ssd_heads;
+
+/* Norm and rotate `rows` rows of n operands (1 or 2: queries, keys), all of type SSD_TYPE_*.
+ *   pos: device int32, position of (row, axis) at row * pos_row + axis * pos_axis
+ * Sums, sines and products are fp32, rounded once to the type. */
+SSD_API ssd_status ssd_rotary_apply(const ssd_rotary* r, const ssd_heads* operand, int n, int type, int rows,
+                                    const int32_t* pos, int64_t pos_row, int64_t pos_axis, void* cuda_stream);
+
+/* ---- Sampling from logits with given random numbers ---- */
+
+#define SSD_SAMPLE_MAX_VOCAB 262144
+
+/* Settings of a call: the value, or device pointers with one per row (NULL: the value for all). */
+typedef struct {
+  float temperature, top_p, min_p;
+  int top_k;
+  const float* temperature_rows;
+  const float* top_p_rows;
+  const float* min_p_rows;
+  const int32_t* top_k_rows;
+} ssd_sampling;
+
+/* One token per row.  With z = logit / temperature, tokens ranked by logit, equal ones by index (lower first):
+ *   kept are the first top_k (all where top_k < 1); of these those whose mass of better-ranked ones is below
+ *   top_p * mass of all of these (all where top_p >= 1); of these those with exp(z - max z) >= min_p; and the first
+ *   in any case.  The token is the first kept one in vocabulary order whose running mass of kept ones exceeds
+ *   u * the kept mass (the last with mass, should u be 1 or more).
+ * temperature <= 0 takes the first-ranked token.  A NaN logit counts as -infinity; rows that have no more than that
+ * give token -1 and prob 0.  Where the largest logit is +infinity, those that are share the mass.  NaN settings act as
+ * temperature 0, top_p 1, min_p 0, u 0.
+ *   logits: device, type SSD_TYPE_*, [rows][row_stride];  u: device fp32 [rows], in [0, 1)
+ *   token: device int32 [rows];  prob: device fp32 [rows], the token's share of the kept mass, or NULL
+ * Masses are exp(z - max z) to about 2^-33 of themselves or 2^-44, held as integers, so the result does not depend on
+ * the order of any sum.  vocab at most SSD_SAMPLE_MAX_VOCAB. */
+SSD_API ssd_status ssd_sample(const void* logits, int type, int rows, int vocab, int64_t row_stride, const float* u,
+                              const ssd_sampling* how, int32_t* token, float* prob, void* cuda_stream);
 
 /* The calling thread's last failure of a low-bit operator ("" if none). */
 SSD_API const char* ssd_op_last_error(void);

@@ -28,6 +28,7 @@ SSD_FAULT_ALLOC = 1
 SSD_FAULT_LAUNCH = 2
 SSD_TYPE_BF16 = 0
 SSD_TYPE_FP32 = 1
+SSD_TYPE_F4 = 2
 SSD_KV8_MAX_BATCH = 1024
 SSD_KV8_STEP_HEAD = 38928
 SSD_KV8_NO_BLOCKS = 1
@@ -35,6 +36,9 @@ SSD_KV8_LENGTH = 2
 SSD_KV8_SLOT = 4
 SSD_KV8_NON_FINITE = 8
 SSD_W4_MAX_ROWS = 16
+SSD_ROTARY_MAX_AXES = 4
+SSD_ROTARY_MAX_DIM = 256
+SSD_SAMPLE_MAX_VOCAB = 262144
 
 STATUS = {0: "SSD_OK", 1: "SSD_ERR_INVALID_ARG", 2: "SSD_ERR_OOM", 3: "SSD_ERR_CUDA", 4: "SSD_ERR_CAPACITY",
           5: "SSD_ERR_STATE", 6: "SSD_ERR_TIMEOUT", 7: "SSD_ERR_DEVICE", 8: "SSD_ERR_UNSUPPORTED"}
@@ -48,7 +52,8 @@ EXPORTED = ("ssd_create", "ssd_destroy", "ssd_prefill", "ssd_draft", "ssd_verify
             "ssd_lm_head_static", "ssd_profile_projection", "ssd_set_fault_injection", "ssd_probe_bounded_wait",
             "ssd_kv8_data_bytes", "ssd_kv8_work_bytes", "ssd_kv8_step_ints", "ssd_kv8_plan", "ssd_kv8_append",
             "ssd_kv8_read", "ssd_kv8_attention", "ssd_kv8_status", "ssd_w4_bytes", "ssd_w4_work_bytes", "ssd_w4_pack",
-            "ssd_w4_unpack", "ssd_w4_matmul", "ssd_op_last_error",
+            "ssd_w4_unpack", "ssd_w4_matmul", "ssd_f4_bytes", "ssd_f4_pack", "ssd_f4_unpack", "ssd_f4_matmul",
+            "ssd_rotary_init", "ssd_rotary_apply", "ssd_sample", "ssd_op_last_error",
             "ssd_status_string", "ssd_last_error")
 
 
@@ -103,6 +108,22 @@ class SSDKv8Step(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int), ("rows", ctypes.c_int), ("row_tile", ctypes.c_int), ("data", ctypes.c_void_p)]
 
 
+class SSDRotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("head_dim", "turn", "interleaved", "axes")] + [("eps", ctypes.c_float)] + \
+               [("axis", ctypes.c_uint8 * (SSD_ROTARY_MAX_DIM // 2)), ("step", ctypes.c_uint64 * (SSD_ROTARY_MAX_DIM // 2))]
+
+
+class SSDHeads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("heads", ctypes.c_int)] + \
+               [(n, ctypes.c_int64) for n in ("x_row", "x_head", "y_row", "y_head")] + \
+               [("gain", ctypes.c_void_p), ("gain_type", ctypes.c_int)]
+
+
+class SSDSampling(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in ("temperature", "top_p", "min_p")] + [("top_k", ctypes.c_int)] + \
+               [(n, ctypes.c_void_p) for n in ("temperature_rows", "top_p_rows", "min_p_rows", "top_k_rows")]
+
+
 _lib = None
 
 
@@ -151,6 +172,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "ssd_w4_pack": [vp, i32, i32, i32, i64, i32, vp, vp],
         "ssd_w4_unpack": [vp, i32, i32, i32, vp, vp],
         "ssd_w4_matmul": [vp, i32, i32, i32, vp, i32, i32, i64, vp, i64, vp, i64, vp, vp],
+        "ssd_f4_pack": [vp, i32, i32, i32, i64, vp, vp],
+        "ssd_f4_unpack": [vp, i32, i32, vp, i32, vp],
+        "ssd_f4_matmul": [vp, i32, i32, vp, i32, i32, i64, vp, i32, i64, vp, i64, vp, vp],
+        "ssd_rotary_init": [vp, i32, i32, i32, i32, vp, ctypes.c_double, ctypes.c_float],
+        "ssd_rotary_apply": [vp, vp, i32, i32, i32, vp, i64, i64, vp],
+        "ssd_sample": [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -163,7 +190,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.ssd_rel_bucket.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int]
     lib.ssd_rel_bucket.restype = ctypes.c_int
     for name, args in {"ssd_kv8_data_bytes": [vp], "ssd_kv8_work_bytes": [vp], "ssd_kv8_step_ints": [i32, i32],
-                       "ssd_w4_bytes": [i32, i32, i32], "ssd_w4_work_bytes": [i32, i32]}.items():
+                       "ssd_w4_bytes": [i32, i32, i32], "ssd_w4_work_bytes": [i32, i32],
+                       "ssd_f4_bytes": [i32, i32]}.items():
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = i64
     lib.ssd_op_last_error.argtypes = []

@@ -18,7 +18,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libssd.so")
 SOURCES = ["engine.cu", "gemv_qkv.cu", "gemv_gate.cu", "gemv_silu.cu", "gemv_resid.cu", "gemv_head.cu", "gemv_xattn.cu", "gemv_mid.cu", "attention.cu",
            "static_head.cu", "prefill.cu", "kv8_cache.cu", "kv8_attn.cu", "w4.cu", "w4_bf16_8.cu", "w4_bf16_16.cu",
-           "w4_fp32_4.cu", "w4_fp32_8.cu", "w4_fp32_16.cu"]
+           "w4_fp32_4.cu", "w4_fp32_8.cu", "w4_fp32_16.cu", "f4.cu", "f4_matmul.cu", "rotary.cu", "sample.cu"]
 FLAGS = ["-gencode", "arch=compute_103a,code=sm_103a", "-O3", "-lineinfo", "-std=c++17",
          "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
 

@@ -94,6 +94,19 @@ inline bool op_overlap(OpRows a, OpRows b, int size) {
   return false;
 }
 
+// Whether an output's rows and heads lie apart: the wider stride steps over all that the narrower one spans.
+inline bool op_apart(OpRows a) {
+  auto size = [](int64_t v) -> __int128 { return v < 0 ? -static_cast<__int128>(v) : v; };
+  __int128 s = size(a.row), t = size(a.head);
+  int64_t n = a.rows, m = a.heads;
+  if (m < 2 || (n >= 2 && s < t)) {
+    const __int128 u = s;
+    const int64_t v = n;
+    s = t, n = m, t = u, m = v;
+  }
+  return (m < 2 || t >= a.width) && (n < 2 || s >= t * (m - 1) + a.width);
+}
+
 // ------------------------------------------------------------------ cache layout
 //
 // A tile is 16 tokens of one block and kv head: 16 * D bytes of K, then 16 * D of V, a code c
