@@ -1,15 +1,16 @@
 // Products of rows and weights that are both packed to 4-bit floats.
 #include "f4.cuh"
 
-#include <cuda_fp8.h>
+#include "tcgen05.cuh"
 
 namespace ssd {
 namespace {
 
 struct F4MatmulParams {
   const uint8_t *w, *x;
-  const float *w_rho, *x_rho;
-  int n, k, rows, chunks;
+  const uint32_t *w_rho, *x_rho;
+  int n, rows, chunks;
+  int early;  // the launch before writes x alone: w may be read ahead of it
   void* y;
   const void* residual;
   int64_t y_row, r_row;
@@ -19,50 +20,215 @@ struct F4MatmulParams {
 // unless the result does.  A NaN stays one.
 __device__ __forceinline__ float f4_scaled(float sum, uint32_t rho_x, uint32_t rho_w) {
   const uint32_t e = (rho_x >> 23) + (rho_w >> 23), half = e >> 1;
-  if (rho_x >= 0x7f800000u || rho_w >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
-  return sum * __uint_as_float(half << 23) * __uint_as_float((e - half) << 23);
+  const float v = sum * __uint_as_float(half << 23) * __uint_as_float((e - half) << 23);
+  return max(rho_x, rho_w) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : v;
 }
 
-// 64 x rows by 64 weight rows a CTA, 4 x 4 a thread, 64 columns at a time from shared memory.
 template <typename T>
-__global__ void __launch_bounds__(256) ssd_f4_matmul_kernel(const F4MatmulParams p) {
-  pdl_wait();
-  pdl_trigger();
-  __shared__ float xs[64][65], ws[64][65];
-  const int n0 = blockIdx.x * 64, m0 = blockIdx.y * 64, tn = threadIdx.x & 15, tm = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < p.chunks * kF4Cols; k0 += 64) {
-    for (int i = threadIdx.x; i < 2 * 64 * 64; i += 256) {
-      const bool of_w = i >= 4096;
-      const int r = (i >> 6 & 63) + (of_w ? n0 : m0), c = k0 + (i & 63);
-      float v = 0.0f;
-      if (r < (of_w ? p.n : p.rows)) {
-        const uint8_t* at = (of_w ? p.w : p.x) + (static_cast<int64_t>(r / kF4Rows) * p.chunks + c / kF4Cols) * kF4Record;
-        const uint32_t code = at[f4_code_byte(r % kF4Rows, c % kF4Cols)] >> (4 * (c & 1)) & 15u;
-        const float mag = (code & 7u) < 2 ? 0.5f * (code & 7u) : __uint_as_float(((code & 7u) + 252u) << 22);
-        const __nv_fp8_storage_t s = at[f4_scale_byte(r % kF4Rows, c % kF4Cols)];
-        v = (code & 8u ? -mag : mag) * __half2float(__half(__nv_cvt_fp8_to_halfraw(s, __NV_E4M3)));
-      }
-      (of_w ? ws : xs)[i >> 6 & 63][i & 63] = v;
-    }
-    __syncthreads();
-    for (int c = 0; c < 64; ++c)
-#pragma unroll
-      for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) acc[a][b] = fmaf(xs[tm + 16 * a][c], ws[tn + 16 * b][c], acc[a][b]);
-    __syncthreads();
+__device__ __forceinline__ void f4_store(const F4MatmulParams& p, int m, int n, float v) {
+  if (p.residual) v += to_f32(static_cast<const T*>(p.residual)[m * p.r_row + n]);
+  static_cast<T*>(p.y)[m * p.y_row + n] = from_f32<T>(v);
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr, uint32_t rank) {
+  uint32_t a;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+
+// A tile is 128 weight rows (the matrix rows, so that few x rows are few columns) by up to BN x rows.
+template <int BN>
+struct F4Tile {
+  static constexpr int kRecords = (BN + kF4Rows - 1) / kF4Rows;  // of x
+  static constexpr int kStages = BN > 128 ? 4 : BN > 64 ? 5 : 4;
+  static constexpr int kCodes = BN * kF4Cols / 2, kScales = kF4Record - kF4CodeBytes;
+  static constexpr int kStage = kF4Record + kCodes + kRecords * kScales;
+  // tensor memory columns: the sums, then each stage's scales (16 of w, 16 of each x record)
+  static constexpr int kSums = BN < 32 ? 32 : BN, kScaleCols = 16 + 16 * kRecords;
+  static constexpr int kCols = kSums + kStages * kScaleCols <= 256 ? 256 : 512;
+  static constexpr int kSmem = 1024 + kStages * kStage + 256 + BN * 4;
+  static_assert(kSums + kStages * kScaleCols <= kCols && kCols <= 512, "tensor memory");
+  static_assert(BN * kF4Rows * 4 <= kStages * kStage, "partial sums take the stages' place");
+};
+
+// Warp 0 copies records to shared memory, warp 1 issues the products, warps 2..5 read the sums.  The CTAs of a
+// cluster split the columns and add up in rank order through shared memory.
+template <int BN, typename T>
+__global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams p) {
+  using S = F4Tile<BN>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);
+  uint64_t* empty = full + S::kStages;
+  uint64_t* done = empty + S::kStages;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  uint32_t* rho = reinterpret_cast<uint32_t*>(full) + 64;
+  float* part = reinterpret_cast<float*>(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n0 = blockIdx.x * kF4Rows, m0 = blockIdx.y * BN, cols = min(BN, p.rows - m0), nn = (cols + 15) / 16 * 16;
+  const int split = gridDim.z, rank = blockIdx.z;
+  const int c0 = static_cast<int>(static_cast<int64_t>(p.chunks) * rank / split);
+  const int c1 = static_cast<int>(static_cast<int64_t>(p.chunks) * (rank + 1) / split);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
+    mbar_init(done, 1);
+    fence_mbar_init();
   }
-#pragma unroll
-  for (int a = 0; a < 4; ++a)
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int m = m0 + tm + 16 * a, n = n0 + tn + 16 * b;
-      if (m >= p.rows || n >= p.n) continue;
-      float v = f4_scaled(acc[a][b], __float_as_uint(p.x_rho[m]), __float_as_uint(p.w_rho[n]));
-      if (p.residual) v += to_f32(static_cast<const T*>(p.residual)[m * p.r_row + n]);
-      static_cast<T*>(p.y)[m * p.y_row + n] = from_f32<T>(v);
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                 "r"(S::kCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  bool ok = true;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint8_t* w = p.w + static_cast<int64_t>(blockIdx.x) * p.chunks * kF4Record;
+      const uint8_t* x = p.x + static_cast<int64_t>(m0 / kF4Rows) * p.chunks * kF4Record;
+      const int records = (nn + kF4Rows - 1) / kF4Rows, last = nn - (records - 1) * kF4Rows;
+      const uint32_t x_bytes = nn * 128 + records * S::kScales;
+      auto load_w = [&](int c) {
+        const int s = (c - c0) % S::kStages;
+        mbar_arrive_expect_tx(&full[s], kF4Record + x_bytes);
+        bulk_load(smem + s * S::kStage, w + static_cast<int64_t>(c) * kF4Record, kF4Record, &full[s]);
+      };
+      auto load_x = [&](int c) {
+        const int s = (c - c0) % S::kStages;
+        uint8_t* at = smem + s * S::kStage + kF4Record;
+        for (int r = 0; r < records; ++r) {
+          const uint8_t* rec = x + (static_cast<int64_t>(r) * p.chunks + c) * kF4Record;
+          bulk_load(at + r * kF4CodeBytes, rec, (r + 1 < records ? kF4Rows : last) * 128, &full[s]);
+          bulk_load(at + S::kCodes + r * S::kScales, rec + kF4CodeBytes, S::kScales, &full[s]);
+        }
+      };
+      if (!p.early) pdl_wait();
+      const int ahead = min(c1, c0 + S::kStages);
+      for (int c = c0; c < ahead; ++c) load_w(c);
+      if (p.early) pdl_wait();
+      for (int c = c0; c < ahead; ++c) load_x(c);
+      int c = ahead;
+      for (; c < c1; ++c) {
+        const int i = c - c0;
+        if (!mbar_wait(&empty[i % S::kStages], (i / S::kStages - 1) & 1)) break;
+        load_w(c);
+        load_x(c);
+      }
+      if (c < c1) drain_ring(full, S::kStages, c - c0);
     }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = umma_idesc_f4(kF4Rows, nn);
+      for (int c = c0; c < c1; ++c) {
+        const int i = c - c0, s = i % S::kStages;
+        if (!mbar_wait(&full[s], (i / S::kStages) & 1)) {
+          ok = false;
+          break;
+        }
+        tmem_fence_after();
+        const uint32_t at = smem_u32(smem + s * S::kStage), sa = tmem + S::kSums + s * S::kScaleCols, sb = sa + 16;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          tmem_copy_scales(sa + 4 * kk, umma_desc_scales(at + kF4CodeBytes + 512 * kk));
+#pragma unroll
+          for (int r = 0; r < S::kRecords; ++r)
+            tmem_copy_scales(sb + 4 * (S::kRecords * kk + r),
+                             umma_desc_scales(at + kF4Record + S::kCodes + r * S::kScales + 512 * kk));
+        }
+        const uint64_t a = umma_desc_sw128(at), b = umma_desc_sw128(at + kF4Record);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)  // 64 columns are 32 bytes of the 128-byte rows
+          umma_f4(tmem, a + 2 * kk, b + 2 * kk, idesc, sa + 4 * kk, sb + 4 * S::kRecords * kk, i > 0 || kk > 0);
+        umma_commit(&empty[s]);
+      }
+      if (ok) umma_commit(done);
+    }
+  } else {
+    const int q = warp & 3, n = n0 + q * 32 + lane;
+    pdl_wait();
+    for (int i = threadIdx.x - 64; i < cols; i += 128) rho[i] = p.x_rho[m0 + i];
+    const uint32_t rho_w = n < p.n ? p.w_rho[n] : 0u;
+    named_bar_sync(1, 128);
+    ok = mbar_wait(done, 0);
+    tmem_fence_after();
+    for (int c = 0; c < nn; c += 16) {
+      float v[16];
+      tmem_ld16(tmem + (static_cast<uint32_t>(q * 32) << 16) + c, v);
+      if (!ok)
+        for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(0x7fc00000u);
+      if (split > 1) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) part[(c + j) * kF4Rows + q * 32 + lane] = v[j];
+      } else if (n < p.n) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (c + j < cols) f4_store<T>(p, m0 + c + j, n, f4_scaled(v[j], rho[c + j], rho_w));
+      }
+    }
+  }
+  pdl_trigger();
+  tmem_fence_before();
+  __syncthreads();
+  if (split > 1) {
+    cluster_barrier();
+    const int i0 = cols * rank / split, i1 = cols * (rank + 1) / split, n = n0 + (threadIdx.x & 127);
+    if (threadIdx.x < 128 && n < p.n) {
+      const uint32_t rho_w = p.w_rho[n];
+      for (int i = i0; i < i1; ++i) {
+        float v = 0.0f;
+        const uint32_t at = smem_u32(&part[i * kF4Rows + threadIdx.x]);
+        for (int r = 0; r < split; ++r) v += ld_cluster(at, r);
+        f4_store<T>(p, m0 + i, n, f4_scaled(v, rho[i], rho_w));
+      }
+    }
+    __syncwarp();
+    cluster_barrier();  // the others still read this CTA's sums
+  }
+  if (warp == 1) {
+    tmem_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kCols) : "memory");
+  }
+}
+
+template <int BN, typename T>
+ssd_status f4_launch(const F4MatmulParams& p, int split, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  constexpr int smem = F4Tile<BN>::kSmem;
+  if (ssd_status e = op_smem(ssd_f4_matmul_kernel<BN, T>, smem, ready, "ssd_f4_matmul")) return e;
+  const dim3 grid((p.n + kF4Rows - 1) / kF4Rows, (p.rows + BN - 1) / BN, split);
+  return op_launch_cluster("ssd_f4_matmul", ssd_f4_matmul_kernel<BN, T>, grid, 192, smem, dim3(1, 1, split), s, p);
+}
+
+template <typename T>
+ssd_status f4_dispatch(const F4MatmulParams& p, cudaStream_t s) {
+  const int bn = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : p.rows <= 128 ? 128 : 256;
+  const int64_t tiles = static_cast<int64_t>((p.n + kF4Rows - 1) / kF4Rows) * ((p.rows + bn - 1) / bn);
+  const int64_t slots = 152 * (bn <= 64 ? 2 : 1);
+  int split = 1;
+  while (split < 8 && tiles * split * 2 <= slots && split * 2 <= p.chunks) split *= 2;
+  switch (bn) {
+    case 16: return f4_launch<16, T>(p, split, s);
+    case 32: return f4_launch<32, T>(p, split, s);
+    case 64: return f4_launch<64, T>(p, split, s);
+    case 128: return f4_launch<128, T>(p, split, s);
+    default: return f4_launch<256, T>(p, split, s);
+  }
 }
 
 }  // namespace
@@ -107,14 +273,11 @@ ssd_status ssd_f4_matmul(const void* w, int n, int k, const void* x, int x_type,
   F4MatmulParams p{};
   p.w = static_cast<const uint8_t*>(w);
   p.x = static_cast<const uint8_t*>(xp);
-  p.w_rho = reinterpret_cast<const float*>(p.w + f4_scales_at(n, k));
-  p.x_rho = reinterpret_cast<const float*>(p.x + f4_scales_at(rows, k));
-  p.n = n, p.k = k, p.rows = rows, p.chunks = f4_chunks(k);
+  p.w_rho = reinterpret_cast<const uint32_t*>(p.w + f4_scales_at(n, k));
+  p.x_rho = reinterpret_cast<const uint32_t*>(p.x + f4_scales_at(rows, k));
+  p.n = n, p.rows = rows, p.chunks = f4_chunks(k), p.early = !packed;
   p.y = y, p.residual = residual, p.y_row = y_row_stride, p.r_row = res_row_stride;
-  const dim3 grid((n + 63) / 64, (rows + 63) / 64);
-  if (grid.y > 65535) return op_fail(SSD_ERR_INVALID_ARG, "ssd_f4_matmul: %d rows", rows);
-  return type == SSD_TYPE_FP32 ? op_launch("ssd_f4_matmul", ssd_f4_matmul_kernel<float>, grid, 256, 0, s, p)
-                               : op_launch("ssd_f4_matmul", ssd_f4_matmul_kernel<__nv_bfloat16>, grid, 256, 0, s, p);
+  return type == SSD_TYPE_FP32 ? f4_dispatch<float>(p, s) : f4_dispatch<__nv_bfloat16>(p, s);
 }
 
 }  // extern "C"

@@ -28,19 +28,28 @@ ssd_status op_smem(K* kernel, int bytes, std::atomic<uint64_t>& ready, const cha
 // Launch that may begin while the launch before it drains: every kernel launched so waits for that one
 // (griddepcontrol.wait) before it touches memory, and lets the next begin early.
 template <typename... P, typename... A>
-ssd_status op_launch(const char* what, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t s, A... args) {
+ssd_status op_launch_cluster(const char* what, void (*kernel)(P...), dim3 grid, int threads, int smem, dim3 cluster,
+                             cudaStream_t s, A... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cudaLaunchAttribute at[1];
+  cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster.x;
+  at[1].val.clusterDim.y = cluster.y;
+  at[1].val.clusterDim.z = cluster.z;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster.x * cluster.y * cluster.z > 1 ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
   return e == cudaSuccess ? SSD_OK : op_fail(SSD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+template <typename... P, typename... A>
+ssd_status op_launch(const char* what, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t s, A... args) {
+  return op_launch_cluster(what, kernel, grid, threads, smem, dim3(1), s, args...);
 }
 // The status of a launch that has just been made.
 ssd_status op_launched(const char* what);
