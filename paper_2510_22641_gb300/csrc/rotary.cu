@@ -19,6 +19,8 @@ struct RotaryParams {
   const int32_t* pos;
   int64_t pos_row, pos_axis;
   int rows, heads;  // heads of both operands
+  int norms;        // whether any operand has a gain
+  int slots, span, spans;  // lanes per head, heads per warp, warps per row
 };
 
 // Cosine and sine of pos * step turns.  step is a 64-bit fraction of a turn, so the product's low 64 bits are the
@@ -35,9 +37,15 @@ __device__ __forceinline__ void turn_of(int pos, uint64_t step, float& c, float&
   if (quarter & 2) s = -s;
 }
 
-// Any head size, pairing and stride: a warp per (row, head), pair p = lane + 32 j of a lane, scalar accesses.
+// One product rounded, the other not, in every kernel alike: a call's bits do not depend on its alignment.
+__device__ __forceinline__ void turn_pair(float u, float v, float c, float s, float& a, float& b) {
+  a = __fmaf_rn(u, c, -__fmul_rn(v, s));
+  b = __fmaf_rn(v, c, __fmul_rn(u, s));
+}
+
+// What the units below do not divide: a warp per (row, head), pair p = lane + 32 j of a lane, scalar accesses.
 template <typename T>
-__global__ void __launch_bounds__(256) ssd_rotary_kernel(const RotaryParams p) {
+__global__ void __launch_bounds__(256) ssd_rotary_any_kernel(const RotaryParams p) {
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31;
@@ -84,12 +92,146 @@ __global__ void __launch_bounds__(256) ssd_rotary_kernel(const RotaryParams p) {
       float c, s;
       turn_of(p.pos[row * p.pos_row + p.r.axis[i] * p.pos_axis], p.r.step[i], c, s);
       const float u = a[j], v = b[j];
-      a[j] = u * c - v * s;
-      b[j] = v * c + u * s;
+      turn_pair(u, v, c, s, a[j], b[j]);
     }
     y[at[j]] = from_f32<T>(a[j]);
     y[with[j]] = from_f32<T>(b[j]);
   }
+}
+
+// What bounds this operator is one pass over the heads' bytes, so sines and cosines are made once per row and held in
+// registers while a warp goes over heads.
+//
+// A head is cut into units of V neighbouring elements (16 bytes or less); `slots` lanes hold a head, each a pair of
+// units: the two halves of a rotated pair (pairs apart), or two neighbouring units (pairs next to each other, elements
+// that do not turn).  A warp takes 32 / slots heads at a time, `span` heads in all, of one row.
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Unit {
+  T v[V];
+};
+
+template <typename T, int V, bool APART>
+__global__ void __launch_bounds__(256) ssd_rotary_kernel(const RotaryParams p) {
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  const int64_t job = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  const int64_t row = job / p.spans;
+  if (row >= p.rows) return;
+  const int slots = p.slots, slot = lane % slots, in_warp = 32 / slots;
+  int head = static_cast<int>(job % p.spans) * p.span;
+  const int end = min(head + p.span, p.heads);
+  const bool idle = lane >= in_warp * slots;
+  const int half = p.r.turn / 2;
+  // elements of the two units, and the first pair that turns with them
+  int at, with, pair;
+  if (APART) {
+    const bool turns = slot * V < half;
+    at = turns ? slot * V : p.r.turn + 2 * (slot * V - half);
+    with = turns ? at + half : at + V;
+    pair = turns ? slot * V : half;
+  } else {
+    at = slot * 2 * V, with = at + V, pair = slot * V;
+  }
+  float c[V], s[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    c[j] = 1.0f, s[j] = 0.0f;
+    if (pair + j < half) turn_of(p.pos[row * p.pos_row + p.r.axis[pair + j] * p.pos_axis], p.r.step[pair + j], c[j], s[j]);
+  }
+  float g[2][2 * V];
+#pragma unroll
+  for (int o = 0; o < 2; ++o) {
+    const RotaryOperand& op = p.op[o];
+#pragma unroll
+    for (int j = 0; j < 2 * V; ++j) {
+      const int i = j < V ? at + j : with + j - V;
+      g[o][j] = !op.gain ? 1.0f : op.gain_fp32 ? static_cast<const float*>(op.gain)[i]
+                                               : to_f32(static_cast<const __nv_bfloat16*>(op.gain)[i]);
+    }
+  }
+  for (head += lane / slots; head - lane / slots < end; head += in_warp) {
+    const bool on = !idle && head < end, second = head >= p.op[0].heads;
+    const RotaryOperand& o = p.op[second];
+    const int h = second ? head - p.op[0].heads : head;
+    const T* x = static_cast<const T*>(o.x) + row * o.x_row + h * o.x_head;
+    T* y = static_cast<T*>(o.y) + row * o.y_row + h * o.y_head;
+    Unit<T, V> ua = {}, ub = {};
+    if (on) {
+      ua = *reinterpret_cast<const Unit<T, V>*>(x + at);
+      ub = *reinterpret_cast<const Unit<T, V>*>(x + with);
+    }
+    float e[2 * V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) e[j] = to_f32(ua.v[j]), e[V + j] = to_f32(ub.v[j]);
+    if (p.norms) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 2 * V; ++j) sum += e[j] * e[j];
+      // the sum over a head's lanes, a number that need not be a power of two
+      for (int d = 1; d < slots; d <<= 1) {
+        const float t = __shfl_down_sync(~0u, sum, d);
+        if (slot + d < slots) sum += t;
+      }
+      sum = __shfl_sync(~0u, sum, lane - slot);
+      if (o.gain) {
+        const float inv = 1.0f / sqrtf(sum / p.r.head_dim + p.r.eps);
+#pragma unroll
+        for (int j = 0; j < 2 * V; ++j) e[j] *= inv * (second ? g[1][j] : g[0][j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int a = APART ? j : 2 * j, b = APART ? V + j : 2 * j + 1;
+      const float u = e[a], v = e[b];
+      if (pair + j < half) {
+        turn_pair(u, v, c[j], s[j], e[a], e[b]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) ua.v[j] = from_f32<T>(e[j]), ub.v[j] = from_f32<T>(e[V + j]);
+    if (on) {
+      *reinterpret_cast<Unit<T, V>*>(y + at) = ua;
+      *reinterpret_cast<Unit<T, V>*>(y + with) = ub;
+    }
+  }
+}
+
+template <typename T, int V>
+ssd_status rotary_launch(RotaryParams& p, cudaStream_t s) {
+  p.slots = (p.r.head_dim / 2 + V - 1) / V;
+  // A warp takes as many heads of a row as leave every SM its 48 warps or more: the row's sines are made anew by every
+  // warp that works on it.
+  const int in_warp = 32 / p.slots, turns = (p.heads + in_warp - 1) / in_warp;
+  const int64_t all = static_cast<int64_t>(p.rows) * turns, most = all / (152 * 48);
+  const int each = most < 1 ? 1 : most < turns ? static_cast<int>(most) : turns;
+  const int parts = (turns + each - 1) / each;
+  p.span = (turns + parts - 1) / parts * in_warp;
+  p.spans = (p.heads + p.span - 1) / p.span;
+  const int64_t ctas = (static_cast<int64_t>(p.rows) * p.spans + 7) / 8;
+  if (ctas > 0x7fffffff) return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: %d rows of %d heads", p.rows, p.heads);
+  const dim3 grid(static_cast<unsigned>(ctas));
+  return p.r.interleaved ? op_launch("ssd_rotary_apply", ssd_rotary_kernel<T, V, false>, grid, 256, 0, s, p)
+                         : op_launch("ssd_rotary_apply", ssd_rotary_kernel<T, V, true>, grid, 256, 0, s, p);
+}
+
+// The widest unit that divides the pairs, the turning ones and every stride, and to which every head is aligned.
+template <typename T>
+ssd_status rotary_dispatch(RotaryParams& p, int n, cudaStream_t s) {
+  uint64_t bits = static_cast<uint64_t>(p.r.head_dim / 2) | (p.r.turn / 2);
+  for (int i = 0; i < n; ++i) {
+    const RotaryOperand& o = p.op[i];
+    bits |= (reinterpret_cast<uintptr_t>(o.x) | reinterpret_cast<uintptr_t>(o.y)) / sizeof(T);
+    if (p.rows > 1) bits |= o.x_row | o.y_row;
+    if (o.heads > 1) bits |= o.x_head | o.y_head;
+  }
+  if (sizeof(T) == 2 && bits % 8 == 0) return rotary_launch<T, 16 / sizeof(T)>(p, s);
+  if (bits % 4 == 0) return rotary_launch<T, 4>(p, s);
+  if (bits % 2 == 0 && p.r.head_dim <= 128) return rotary_launch<T, 2>(p, s);
+  if (p.r.head_dim <= 64) return rotary_launch<T, 1>(p, s);
+  const int64_t ctas = (static_cast<int64_t>(p.rows) * p.heads + 7) / 8;
+  if (ctas > 0x7fffffff) return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: %d rows of %d heads", p.rows, p.heads);
+  return op_launch("ssd_rotary_apply", ssd_rotary_any_kernel<T>, dim3(static_cast<unsigned>(ctas)), 256, 0, s, p);
 }
 
 }  // namespace
@@ -151,6 +293,7 @@ ssd_status ssd_rotary_apply(const ssd_rotary* r, const ssd_heads* operand, int n
       return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: unaligned gain");
     p.op[i] = {h.x, h.y, h.gain, h.x_row, h.x_head, h.y_row, h.y_head, h.heads, h.gain_type == SSD_TYPE_FP32};
     p.heads += h.heads;
+    p.norms |= h.gain != nullptr;
   }
   for (int i = 0; i < n; ++i) {
     const ssd_heads& a = operand[i];
@@ -164,12 +307,8 @@ ssd_status ssd_rotary_apply(const ssd_rotary* r, const ssd_heads* operand, int n
         return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: an output overlaps another operand");
     }
   }
-  const int64_t ctas = (static_cast<int64_t>(rows) * p.heads + 7) / 8;
-  if (ctas > 0x7fffffff) return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: %d rows of %d heads", rows, p.heads);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  const dim3 grid(static_cast<unsigned>(ctas));
-  return type == SSD_TYPE_FP32 ? op_launch("ssd_rotary_apply", ssd_rotary_kernel<float>, grid, 256, 0, s, p)
-                               : op_launch("ssd_rotary_apply", ssd_rotary_kernel<__nv_bfloat16>, grid, 256, 0, s, p);
+  return type == SSD_TYPE_FP32 ? rotary_dispatch<float>(p, n, s) : rotary_dispatch<__nv_bfloat16>(p, n, s);
 }
 
 }  // extern "C"
