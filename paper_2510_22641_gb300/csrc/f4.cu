@@ -10,34 +10,54 @@ namespace {
 struct F4PackParams {
   const void* x;
   int64_t x_row;
-  int rows, k, chunks;
+  int rows, k, chunks, warps;
   uint8_t* out;
   float* rho;
 };
 
-// Eight neighbouring columns from `col` on, zeros past k.
-template <bool VEC>
-__device__ __forceinline__ void load8(const float* p, int col, int k, float* v) {
-  if (VEC && col + 8 <= k) {
-    const float4 a = *reinterpret_cast<const float4*>(p + col), b = *reinterpret_cast<const float4*>(p + col + 4);
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-  } else {
+// Eight neighbouring columns as they lie in memory: fp32 numbers, or pairs of bf16.
+template <typename T>
+struct Raw8 {
+  uint32_t w[2 * sizeof(T)];
+
+  // From `col` on, zeros past k.  VEC: 16-byte aligned.
+  template <bool VEC>
+  __device__ __forceinline__ void load(const T* p, int col, int k) {
+    if (VEC && col + 8 <= k) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = col + i < k ? p[col + i] : 0.0f;
-  }
-}
-template <bool VEC>
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, int col, int k, float* v) {
-  if (VEC && col + 8 <= k) {
-    const uint4 w = *reinterpret_cast<const uint4*>(p + col);
-    const float2 a = bf16x2_to_float2(w.x), b = bf16x2_to_float2(w.y), c = bf16x2_to_float2(w.z),
-                 d = bf16x2_to_float2(w.w);
-    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y, v[4] = c.x, v[5] = c.y, v[6] = d.x, v[7] = d.y;
-  } else {
+      for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i)
+        reinterpret_cast<uint4*>(w)[i] = reinterpret_cast<const uint4*>(p + col)[i];
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = col + i < k ? to_f32(p[col + i]) : 0.0f;
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          w[i] = col + i < k ? __float_as_uint(p[col + i]) : 0u;
+        } else {
+          const uint32_t v = col + i < k ? __bfloat16_as_ushort(p[col + i]) : 0u;
+          w[i / 2] = i & 1 ? w[i / 2] | v << 16 : v;
+        }
+      }
+    }
   }
-}
+  // The largest magnitude's bits as those of a float: a NaN is above infinity, infinity above the rest.
+  __device__ __forceinline__ uint32_t amax() const {
+    if constexpr (sizeof(T) == 4) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
+      return m;
+    } else {
+      uint32_t m = 0;  // of the even and the odd columns
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+      return max(m << 16, m & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ float2 pair(int i) const {
+    if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    return bf16x2_to_float2(w[i]);
+  }
+};
 
 __device__ __forceinline__ float e4m3_value(uint32_t byte) {
   return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(byte), __NV_E4M3)));
@@ -49,85 +69,188 @@ __device__ __forceinline__ int f4_row_exponent(uint32_t amax) {
   return max(static_cast<int>(amax >> 23) - 127 - 11 + ((amax & 0x7fffffu) > 0x280000u ? 1 : 0), -100);
 }
 
-// One row's 16-column group, half of it (8 columns) in this lane and half in lane ^ 1, scaled by the row's 2^-e:
-// the scale's byte and the 8 codes.  Quotients are correctly rounded by one step of Markstein's (IBM J. R&D 34, 1990)
-// from a correctly rounded reciprocal; s has four bits, so its reciprocal is never the theorem's exception.
-__device__ __forceinline__ void f4_encode(float* y, uint32_t& scale, uint32_t& codes) {
-  float m = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(y[i]));
-  m = fmaxf(m, __shfl_xor_sync(~0u, m, 1));
-  scale = __nv_cvt_float_to_fp8(m / 6.0f, __NV_SATFINITE, __NV_E4M3);
-  const float s = e4m3_value(scale), r = s > 0.0f ? __frcp_rn(s) : 0.0f;
+// One row's 16-column group, half of it (8 columns) in this lane and half in lane ^ 1, times the row's down = 2^-e: the
+// scale's byte and the 8 codes.  A quotient is fma(y, h, y * l) of its divisor's reciprocal h + l, exact to 2^-47, and
+// so correctly rounded: numerators have 24 bits and divisors (6, s) at most 4, so no quotient lies nearer than 2^-30 to
+// the middle of two fp32 numbers.
+template <typename T>
+__device__ __forceinline__ void f4_encode(const Raw8<T>& x, float down, uint32_t& scale, uint32_t& codes) {
+  uint32_t bits = x.amax();
+  bits = max(bits, __shfl_xor_sync(~0u, bits, 1));
+  constexpr float kSixth = 1.0f / 6.0f, kSixthLow = static_cast<float>(1.0 / 6.0 - static_cast<double>(kSixth));
+  const float m = __uint_as_float(bits) * down;
+  scale = __nv_cvt_float_to_fp8(fmaf(m, kSixth, m * kSixthLow), __NV_SATFINITE, __NV_E4M3);
+  const float s = e4m3_value(scale), h = scale ? __frcp_rn(s) : 0.0f, l = fmaf(-s, h, 1.0f) * h;
   codes = 0;
 #pragma unroll
-  for (int i = 0; i < 8; i += 2) {
-    float2 q;
-    q.x = y[i] * r;
-    q.y = y[i + 1] * r;
-    q.x = fmaf(fmaf(-q.x, s, y[i]), r, q.x);
-    q.y = fmaf(fmaf(-q.y, s, y[i + 1]), r, q.y);
-    codes |= static_cast<uint32_t>(__nv_cvt_float2_to_fp4x2(q, __NV_E2M1, cudaRoundNearest)) << (4 * i);
+  for (int i = 0; i < 4; ++i) {
+    float2 y = x.pair(i);
+    y.x *= down, y.y *= down;
+    y.x = fmaf(y.x, h, y.x * l);
+    y.y = fmaf(y.y, h, y.y * l);
+    codes |= static_cast<uint32_t>(__nv_cvt_float2_to_fp4x2(y, __NV_E2M1, cudaRoundNearest)) << (8 * i);
   }
 }
 
-// One CTA per row, a warp per 256 columns at a time: 8 columns a lane, two lanes a group.  Two passes over the row.
-template <typename T, bool VEC>
+struct F4Row {  // what a row's largest magnitude says
+  bool bad;
+  float down;
+  __device__ __forceinline__ F4Row(uint32_t amax) {
+    bad = amax >= 0x7f800000u;
+    down = __uint_as_float(static_cast<uint32_t>(127 - (bad ? 0 : f4_row_exponent(amax))) << 23);
+  }
+  __device__ __forceinline__ float rho() const {
+    return __uint_as_float(bad ? 0x7fc00000u : (254u << 23) - __float_as_uint(down));
+  }
+};
+
+// Writes 8 columns' codes, and a group's scale as one of four in a word.
+template <typename T>
+__device__ __forceinline__ void f4_put(const Raw8<T>& x, const F4Row& f, uint8_t* at, int r) {
+  const int lane = threadIdx.x & 31;
+  uint32_t scale, codes;
+  f4_encode(x, f.down, scale, codes);
+  if (f.bad) scale = codes = 0;
+  *reinterpret_cast<uint32_t*>(at + f4_code_byte(r, lane * 8)) = codes;
+  scale <<= 8 * (lane >> 1 & 3);
+  scale |= __shfl_xor_sync(~0u, scale, 2);
+  scale |= __shfl_xor_sync(~0u, scale, 4);
+  if ((lane & 7) == 0) *reinterpret_cast<uint32_t*>(at + f4_scale_byte(r, lane * 8)) = scale;
+}
+
+// A row is held in registers between its maximum and its codes, by p.warps warps (1, 2, 4 or 8) of up to J chunks of
+// 256 columns each, 8 columns a lane; the CTA has 8 warps.  The row is read once.
+template <typename T, bool VEC, int J>
 __global__ void __launch_bounds__(256) ssd_f4_pack_kernel(const F4PackParams p) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ uint32_t part[8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = warp % p.warps;
+  const int row = blockIdx.x * (8 / p.warps) + warp / p.warps;
+  const bool on = row < p.rows;
+  const T* src = static_cast<const T*>(p.x) + (on ? row : 0) * p.x_row;
+  Raw8<T> x[J];
+  uint32_t amax = 0;
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+    if (c0 + j * p.warps < p.chunks) x[j].template load<VEC>(src, (c0 + j * p.warps) * kF4Cols + lane * 8, p.k);
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+    if (c0 + j * p.warps < p.chunks) amax = max(amax, x[j].amax());
+  amax = __reduce_max_sync(~0u, amax);
+  if (p.warps > 1) {
+    if (lane == 0) part[warp] = amax;
+    __syncthreads();
+    for (int i = 0; i < p.warps; ++i) amax = max(amax, part[warp - c0 + i]);
+  }
+  if (!on) return;
+  const F4Row f(amax);
+  if (c0 == 0 && lane == 0) p.rho[row] = f.rho();
+  uint8_t* rec = p.out + static_cast<int64_t>(row / kF4Rows) * p.chunks * kF4Record;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int c = c0 + j * p.warps;
+    if (c < p.chunks) f4_put(x[j], f, rec + static_cast<int64_t>(c) * kF4Record, row % kF4Rows);
+  }
+}
+
+// Rows of more than 16384 columns are read twice, by 8 warps.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) ssd_f4_pack_long_kernel(const F4PackParams p) {
   pdl_wait();
   pdl_trigger();
   __shared__ uint32_t part[8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x;
   const T* src = static_cast<const T*>(p.x) + row * p.x_row;
-  uint32_t amax = 0;  // as bits: a NaN is above infinity, infinity above the rest
-  float v[8];
+  uint32_t amax = 0;
+  Raw8<T> x;
   for (int c = warp; c < p.chunks; c += 8) {
-    load8<VEC>(src, c * kF4Cols + lane * 8, p.k, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7fffffffu);
+    x.template load<VEC>(src, c * kF4Cols + lane * 8, p.k);
+    amax = max(amax, x.amax());
   }
   amax = __reduce_max_sync(~0u, amax);
   if (lane == 0) part[warp] = amax;
   __syncthreads();
   for (int i = 0; i < 8; ++i) amax = max(amax, part[i]);
-  const bool bad = amax >= 0x7f800000u;
-  const int e = bad ? 0 : f4_row_exponent(amax);
-  const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-  if (threadIdx.x == 0) p.rho[row] = __uint_as_float(bad ? 0x7fc00000u : static_cast<uint32_t>(127 + e) << 23);
-  const int r = row % kF4Rows;
+  const F4Row f(amax);
+  if (threadIdx.x == 0) p.rho[row] = f.rho();
   uint8_t* rec = p.out + static_cast<int64_t>(row / kF4Rows) * p.chunks * kF4Record;
   for (int c = warp; c < p.chunks; c += 8) {
-    load8<VEC>(src, c * kF4Cols + lane * 8, p.k, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = bad ? 0.0f : v[i] * down;
-    uint32_t scale, codes;
-    f4_encode(v, scale, codes);
-    uint8_t* at = rec + static_cast<int64_t>(c) * kF4Record;
-    *reinterpret_cast<uint32_t*>(at + f4_code_byte(r, lane * 8)) = codes;
-    // four groups' scales are one word
-    scale <<= 8 * (lane >> 1 & 3);
-    scale |= __shfl_xor_sync(~0u, scale, 2);
-    scale |= __shfl_xor_sync(~0u, scale, 4);
-    if ((lane & 7) == 0) *reinterpret_cast<uint32_t*>(at + f4_scale_byte(r, lane * 8)) = scale;
+    x.template load<VEC>(src, c * kF4Cols + lane * 8, p.k);
+    f4_put(x, f, rec + static_cast<int64_t>(c) * kF4Record, row % kF4Rows);
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) ssd_f4_unpack_kernel(const uint8_t* packed, int k, int chunks, const float* rho, int first,
-                                                            T* out) {
+// A CTA per record: 8 columns of a row a lane.  Products of code and scale have 6 bits and are exact in fp16.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) ssd_f4_unpack_kernel(const uint8_t* packed, int rows, int k, int chunks,
+                                                            const float* rho, T* out) {
   pdl_wait();
   pdl_trigger();
-  const int row = first + blockIdx.y, r = row % kF4Rows;
-  const float scale = rho[row];
-  const uint8_t* rec = packed + static_cast<int64_t>(row / kF4Rows) * chunks * kF4Record;
-  for (int col = blockIdx.x * 256 + threadIdx.x; col < k; col += gridDim.x * 256) {
-    const uint8_t* at = rec + static_cast<int64_t>(col / kF4Cols) * kF4Record;
-    const int c = col % kF4Cols;
-    const uint32_t code = at[f4_code_byte(r, c)] >> (4 * (c & 1)) & 15u;
-    const float mag = (code & 7u) < 2 ? 0.5f * (code & 7u) : __uint_as_float(((code & 7u) + 252u) << 22);
-    const float v = (code & 8u ? -mag : mag) * e4m3_value(at[f4_scale_byte(r, c)]) * scale;
-    out[static_cast<int64_t>(row) * k + col] = from_f32<T>(v);
+  const int lane = threadIdx.x & 31, chunk = blockIdx.x, tile = blockIdx.y, col = chunk * kF4Cols + lane * 8;
+  const uint8_t* at = packed + (static_cast<int64_t>(tile) * chunks + chunk) * kF4Record;
+  const int end = min(rows - tile * kF4Rows, kF4Rows);
+  if (col >= k) return;
+#pragma unroll 4
+  for (int r = threadIdx.x >> 5; r < end; r += 8) {
+    const int64_t row = static_cast<int64_t>(tile) * kF4Rows + r;
+    const uint32_t codes = *reinterpret_cast<const uint32_t*>(at + f4_code_byte(r, lane * 8));
+    const __half2 s = __half2half2(
+        __half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(at[f4_scale_byte(r, lane * 8)]), __NV_E4M3)));
+    const float f = rho[row];
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 c(__nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(codes >> (8 * i)), __NV_E2M1));
+      const float2 t = __half22float2(__hmul2(c, s));
+      v[2 * i] = t.x * f, v[2 * i + 1] = t.y * f;
+    }
+    T* y = out + row * k + col;
+    if (VEC && col + 8 <= k) {
+      if constexpr (sizeof(T) == 4) {
+        reinterpret_cast<float4*>(y)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(y)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+        __nv_bfloat162 h[4];
+        for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<uint4*>(y) = *reinterpret_cast<const uint4*>(h);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + i < k) y[i] = from_f32<T>(v[i]);
+    }
   }
+}
+
+template <typename T, bool VEC>
+ssd_status f4_pack_dispatch(const char* what, F4PackParams& p, cudaStream_t s) {
+  // one warp a row as long as it holds the row in two chunks a lane; eight from 8 chunks on
+  p.warps = p.chunks <= 2 ? 1 : p.chunks <= 4 ? 2 : p.chunks <= 8 ? 4 : 8;
+  const int each = 8 / p.warps;
+  const dim3 grid((p.rows + each - 1) / each);
+  if (p.chunks <= 16) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 2>, grid, 256, 0, s, p);
+  if (p.chunks <= 32) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 4>, grid, 256, 0, s, p);
+  if (p.chunks <= 64) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 8>, grid, 256, 0, s, p);
+  return op_launch(what, ssd_f4_pack_long_kernel<T, VEC>, grid, 256, 0, s, p);
+}
+
+template <typename T>
+ssd_status f4_unpack_dispatch(const uint8_t* in, int rows, int k, T* out, cudaStream_t s) {
+  const int chunks = f4_chunks(k);
+  const float* rho = reinterpret_cast<const float*>(in + f4_scales_at(rows, k));
+  const bool vec = reinterpret_cast<uintptr_t>(out) % 16 == 0 && k % (16 / sizeof(T)) == 0;
+  for (int first = 0; first < rows; first += 65535 * kF4Rows) {  // what a grid's second dimension takes
+    const int n = rows - first < 65535 * kF4Rows ? rows - first : 65535 * kF4Rows;
+    const dim3 grid(chunks, (n + kF4Rows - 1) / kF4Rows);
+    const uint8_t* at = in + static_cast<int64_t>(first / kF4Rows) * chunks * kF4Record;
+    T* y = out + static_cast<int64_t>(first) * k;
+    const ssd_status e =
+        vec ? op_launch("ssd_f4_unpack", ssd_f4_unpack_kernel<T, true>, grid, 256, 0, s, at, n, k, chunks, rho + first, y)
+            : op_launch("ssd_f4_unpack", ssd_f4_unpack_kernel<T, false>, grid, 256, 0, s, at, n, k, chunks, rho + first, y);
+    if (e) return e;
+  }
+  return SSD_OK;
 }
 
 }  // namespace
@@ -140,16 +263,13 @@ ssd_status f4_check_shape(int rows, int k) {
 
 ssd_status f4_pack_rows(const char* what, const void* x, int type, int rows, int k, int64_t x_row, void* packed,
                         cudaStream_t s) {
-  F4PackParams p{x, x_row, rows, k, f4_chunks(k), static_cast<uint8_t*>(packed), nullptr};
+  F4PackParams p{x, x_row, rows, k, f4_chunks(k), 0, static_cast<uint8_t*>(packed), nullptr};
   p.rho = reinterpret_cast<float*>(p.out + f4_scales_at(rows, k));
   const int size = type == SSD_TYPE_FP32 ? 4 : 2;
-  const bool vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && x_row % (16 / size) == 0;
-  const dim3 grid(rows);
+  const bool vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (rows == 1 || x_row % (16 / size) == 0);
   if (type == SSD_TYPE_FP32)
-    return vec ? op_launch(what, ssd_f4_pack_kernel<float, true>, grid, 256, 0, s, p)
-               : op_launch(what, ssd_f4_pack_kernel<float, false>, grid, 256, 0, s, p);
-  return vec ? op_launch(what, ssd_f4_pack_kernel<__nv_bfloat16, true>, grid, 256, 0, s, p)
-             : op_launch(what, ssd_f4_pack_kernel<__nv_bfloat16, false>, grid, 256, 0, s, p);
+    return vec ? f4_pack_dispatch<float, true>(what, p, s) : f4_pack_dispatch<float, false>(what, p, s);
+  return vec ? f4_pack_dispatch<__nv_bfloat16, true>(what, p, s) : f4_pack_dispatch<__nv_bfloat16, false>(what, p, s);
 }
 
 }  // namespace ssd
@@ -181,21 +301,10 @@ ssd_status ssd_f4_unpack(const void* packed, int rows, int k, void* out, int typ
   const int size = type == SSD_TYPE_FP32 ? 4 : 2;
   if (!out || !packed || reinterpret_cast<uintptr_t>(packed) % 16 || reinterpret_cast<uintptr_t>(out) % size)
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_f4_unpack: null or unaligned buffer");
-  const int chunks = f4_chunks(k);
   const uint8_t* in = static_cast<const uint8_t*>(packed);
-  const float* rho = reinterpret_cast<const float*>(in + f4_scales_at(rows, k));
-  for (int first = 0; first < rows; first += 65535) {
-    const dim3 grid((k + 255) / 256, rows - first < 65535 ? rows - first : 65535);
-    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    const ssd_status e =
-        type == SSD_TYPE_FP32
-            ? op_launch("ssd_f4_unpack", ssd_f4_unpack_kernel<float>, grid, 256, 0, s, in, k, chunks, rho, first,
-                        static_cast<float*>(out))
-            : op_launch("ssd_f4_unpack", ssd_f4_unpack_kernel<__nv_bfloat16>, grid, 256, 0, s, in, k, chunks, rho, first,
-                        static_cast<__nv_bfloat16*>(out));
-    if (e) return e;
-  }
-  return SSD_OK;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return type == SSD_TYPE_FP32 ? f4_unpack_dispatch(in, rows, k, static_cast<float*>(out), s)
+                               : f4_unpack_dispatch(in, rows, k, static_cast<__nv_bfloat16*>(out), s);
 }
 
 }  // extern "C"

@@ -13,14 +13,16 @@ struct RotaryOperand {
   int64_t x_row, x_head, y_row, y_head;
   int heads, gain_fp32;
 };
+constexpr int kRotaryWarps = 48;  // per SM
 struct RotaryParams {
   ssd_rotary r;
   RotaryOperand op[2];
   const int32_t* pos;
   int64_t pos_row, pos_axis;
   int rows, heads;  // heads of both operands
+  float per_element;  // 1 / head_dim
   int norms;        // whether any operand has a gain
-  int slots, span, spans;  // lanes per head, heads per warp, warps per row
+  int slots, turns[2], warps;  // lanes per head; of each operand a warp's turns of 32 / slots heads; warps of a row in a CTA
 };
 
 // Cosine and sine of pos * step turns.  step is a 64-bit fraction of a turn, so the product's low 64 bits are the
@@ -29,8 +31,11 @@ __device__ __forceinline__ void turn_of(int pos, uint64_t step, float& c, float&
   const int32_t t = static_cast<int32_t>((static_cast<uint64_t>(static_cast<int64_t>(pos)) * step) >> 32);
   const int32_t quarter = static_cast<int32_t>((static_cast<uint32_t>(t) + (1u << 29)) >> 30);
   const int32_t rest = static_cast<int32_t>(static_cast<uint32_t>(t) - (static_cast<uint32_t>(quarter) << 30));
-  float a, b;
-  sincospif(static_cast<float>(rest) * 0x1p-31f, &b, &a);
+  // Taylor series at |x| <= pi / 4: what is left out is below 2^-29 and 2^-33
+  const float x = static_cast<float>(rest) * 1.46291807926715968e-9f, q = x * x;  // 2 pi / 2^32
+  const float b = fmaf(x * q, fmaf(q, fmaf(q, fmaf(q, 1.0f / 362880.0f, -1.0f / 5040.0f), 1.0f / 120.0f), -1.0f / 6.0f), x);
+  const float a =
+      fmaf(q, fmaf(q, fmaf(q, fmaf(q, fmaf(q, -1.0f / 3628800.0f, 1.0f / 40320.0f), -1.0f / 720.0f), 1.0f / 24.0f), -0.5f), 1.0f);
   c = quarter & 1 ? b : a;
   s = quarter & 1 ? a : b;
   if (quarter == 1 || quarter == 2) c = -c;
@@ -74,7 +79,7 @@ __global__ void __launch_bounds__(256) ssd_rotary_any_kernel(const RotaryParams 
   if (o.gain) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-    const float inv = 1.0f / sqrtf(sum / p.r.head_dim + p.r.eps);
+    const float inv = rsqrtf(fmaf(sum, p.per_element, p.r.eps));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (lane + 32 * j >= pairs) continue;
@@ -99,120 +104,169 @@ __global__ void __launch_bounds__(256) ssd_rotary_any_kernel(const RotaryParams 
   }
 }
 
-// What bounds this operator is one pass over the heads' bytes, so sines and cosines are made once per row and held in
-// registers while a warp goes over heads.
+// What bounds this operator is one pass over the heads' bytes, so sines and cosines are made once per row (and CTA) in
+// shared memory, and a warp holds its lanes' in registers while it goes over the row's heads.
 //
 // A head is cut into units of V neighbouring elements (16 bytes or less); `slots` lanes hold a head, each a pair of
 // units: the two halves of a rotated pair (pairs apart), or two neighbouring units (pairs next to each other, elements
-// that do not turn).  A warp takes 32 / slots heads at a time, `span` heads in all, of one row.
+// that do not turn).  A warp takes 32 / slots heads of an operand at a time.
 template <typename T, int V>
 struct alignas(sizeof(T) * V) Unit {
   T v[V];
+  __device__ __forceinline__ void unpack(float* e) const {
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+#pragma unroll
+      for (int j = 0; j < V; j += 2) {
+        const float2 f = bf16x2_to_float2(reinterpret_cast<const uint32_t*>(v)[j / 2]);
+        e[j] = f.x, e[j + 1] = f.y;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) e[j] = to_f32(v[j]);
+    }
+  }
+  __device__ __forceinline__ void pack(const float* e) {
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+#pragma unroll
+      for (int j = 0; j < V; j += 2)
+        reinterpret_cast<__nv_bfloat162*>(v)[j / 2] = __floats2bfloat162_rn(e[j], e[j + 1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = from_f32<T>(e[j]);
+    }
+  }
 };
 
-template <typename T, int V, bool APART>
-__global__ void __launch_bounds__(256) ssd_rotary_kernel(const RotaryParams p) {
+// The CTA's 8 warps work on 8 / p.warps rows, p.warps on each; gridDim.y CTAs share a row's heads.
+template <typename T, int V, bool APART, bool NORM>
+__global__ void __launch_bounds__(256) ssd_rotary_kernel(const __grid_constant__ RotaryParams p) {
+  __shared__ float2 turn[8 * SSD_ROTARY_MAX_DIM / 2];
+  __shared__ float gain[NORM ? 2 * SSD_ROTARY_MAX_DIM : 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_row = warp % p.warps;
+  const int half = p.r.turn / 2, row = blockIdx.x * (8 / p.warps) + warp / p.warps;
+  const bool on = row < p.rows;
+  float2* const cs = turn + warp / p.warps * half;
+  // lanes read different entries: through a pointer, as the constant path takes one address at a time
+  const uint64_t* step = p.r.step;
+  const uint8_t* axis = p.r.axis;
+  asm volatile("" : "+l"(step), "+l"(axis));
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const int64_t job = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  const int64_t row = job / p.spans;
-  if (row >= p.rows) return;
-  const int slots = p.slots, slot = lane % slots, in_warp = 32 / slots;
-  int head = static_cast<int>(job % p.spans) * p.span;
-  const int end = min(head + p.span, p.heads);
-  const bool idle = lane >= in_warp * slots;
-  const int half = p.r.turn / 2;
-  // elements of the two units, and the first pair that turns with them
-  int at, with, pair;
+  if (on)
+    for (int j = in_row * 32 + lane; j < half; j += p.warps * 32) {
+      float c, s;
+      turn_of(p.pos[row * p.pos_row + axis[j] * p.pos_axis], step[j], c, s);
+      cs[j] = make_float2(c, s);
+    }
+  if (NORM)
+    for (int i = threadIdx.x; i < 2 * p.r.head_dim; i += 256) {
+      const RotaryOperand& o = p.op[i >= p.r.head_dim];
+      const int j = i >= p.r.head_dim ? i - p.r.head_dim : i;
+      gain[i] = !o.gain ? 1.0f : o.gain_fp32 ? static_cast<const float*>(o.gain)[j]
+                                             : to_f32(static_cast<const __nv_bfloat16*>(o.gain)[j]);
+    }
+  __syncthreads();
+  if (!on) return;
+  const int slots = p.slots, in_warp = 32 / slots, mine = lane / slots, slot = lane - mine * slots;
+  // elements of the two units, and whether they turn
+  const bool turns = slot * V < half;
+  int at = slot * 2 * V, with = at + V;
   if (APART) {
-    const bool turns = slot * V < half;
     at = turns ? slot * V : p.r.turn + 2 * (slot * V - half);
     with = turns ? at + half : at + V;
-    pair = turns ? slot * V : half;
-  } else {
-    at = slot * 2 * V, with = at + V, pair = slot * V;
   }
-  float c[V], s[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    c[j] = 1.0f, s[j] = 0.0f;
-    if (pair + j < half) turn_of(p.pos[row * p.pos_row + p.r.axis[pair + j] * p.pos_axis], p.r.step[pair + j], c[j], s[j]);
-  }
-  float g[2][2 * V];
-#pragma unroll
-  for (int o = 0; o < 2; ++o) {
-    const RotaryOperand& op = p.op[o];
-#pragma unroll
-    for (int j = 0; j < 2 * V; ++j) {
-      const int i = j < V ? at + j : with + j - V;
-      g[o][j] = !op.gain ? 1.0f : op.gain_fp32 ? static_cast<const float*>(op.gain)[i]
-                                               : to_f32(static_cast<const __nv_bfloat16*>(op.gain)[i]);
+  const bool pow2 = (slots & (slots - 1)) == 0;
+  int t = blockIdx.y * p.warps + in_row;
+  const int stride = gridDim.y * p.warps;
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i) {
+    const RotaryOperand& o = p.op[i];
+    const int turns_of = p.turns[i];  // heads of this operand, in_warp at a time
+    if (t >= turns_of) {
+      t -= turns_of;
+      continue;
     }
-  }
-  for (head += lane / slots; head - lane / slots < end; head += in_warp) {
-    const bool on = !idle && head < end, second = head >= p.op[0].heads;
-    const RotaryOperand& o = p.op[second];
-    const int h = second ? head - p.op[0].heads : head;
-    const T* x = static_cast<const T*>(o.x) + row * o.x_row + h * o.x_head;
-    T* y = static_cast<T*>(o.y) + row * o.y_row + h * o.y_head;
-    Unit<T, V> ua = {}, ub = {};
-    if (on) {
-      ua = *reinterpret_cast<const Unit<T, V>*>(x + at);
-      ub = *reinterpret_cast<const Unit<T, V>*>(x + with);
-    }
-    float e[2 * V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) e[j] = to_f32(ua.v[j]), e[V + j] = to_f32(ub.v[j]);
-    if (p.norms) {
-      float sum = 0.0f;
-#pragma unroll
-      for (int j = 0; j < 2 * V; ++j) sum += e[j] * e[j];
-      // the sum over a head's lanes, a number that need not be a power of two
-      for (int d = 1; d < slots; d <<= 1) {
-        const float t = __shfl_down_sync(~0u, sum, d);
-        if (slot + d < slots) sum += t;
-      }
-      sum = __shfl_sync(~0u, sum, lane - slot);
-      if (o.gain) {
-        const float inv = 1.0f / sqrtf(sum / p.r.head_dim + p.r.eps);
-#pragma unroll
-        for (int j = 0; j < 2 * V; ++j) e[j] *= inv * (second ? g[1][j] : g[0][j]);
-      }
-    }
+    const bool normed = NORM && o.gain;
+    // a pair (u, v) becomes (u c - v s, v c + u s), with the gains of its elements in the factors
+    float uc[V], vs[V], vc[V], us[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int a = APART ? j : 2 * j, b = APART ? V + j : 2 * j + 1;
-      const float u = e[a], v = e[b];
-      if (pair + j < half) {
-        turn_pair(u, v, c[j], s[j], e[a], e[b]);
-      }
+      const float2 f = turns ? cs[slot * V + j] : make_float2(1.0f, 0.0f);
+      const int iu = APART ? at + j : at + 2 * j, iv = APART ? with + j : iu + 1;
+      const float gu = NORM ? gain[i * p.r.head_dim + iu] : 1.0f, gv = NORM ? gain[i * p.r.head_dim + iv] : 1.0f;
+      uc[j] = gu * f.x, vs[j] = gv * f.y, vc[j] = gv * f.x, us[j] = gu * f.y;
     }
+    const T* x = static_cast<const T*>(o.x) + row * o.x_row + (t * in_warp + mine) * o.x_head;
+    T* y = static_cast<T*>(o.y) + row * o.y_row + (t * in_warp + mine) * o.y_head;
+    const int64_t x_step = stride * in_warp * o.x_head, y_step = stride * in_warp * o.y_head;
+    Unit<T, V> ua = {}, ub = {};
+    auto load = [&](int t, const T* x) {
+      if (mine < in_warp && t * in_warp + mine < o.heads)
+        ua = *reinterpret_cast<const Unit<T, V>*>(x + at), ub = *reinterpret_cast<const Unit<T, V>*>(x + with);
+    };
+    load(t, x);
+#pragma unroll 1
+    for (; t < turns_of; t += stride) {
+      const bool keep = mine < in_warp && t * in_warp + mine < o.heads;
+      float e[2 * V];
+      ua.unpack(e), ub.unpack(e + V);
+      x += x_step;
+      if (t + stride < turns_of) load(t + stride, x);
+      float inv = 1.0f;
+      if (normed) {
+        float sum = 0.0f, more = 0.0f;
 #pragma unroll
-    for (int j = 0; j < V; ++j) ua.v[j] = from_f32<T>(e[j]), ub.v[j] = from_f32<T>(e[V + j]);
-    if (on) {
-      *reinterpret_cast<Unit<T, V>*>(y + at) = ua;
-      *reinterpret_cast<Unit<T, V>*>(y + with) = ub;
+        for (int j = 0; j < V; ++j) sum = fmaf(e[j], e[j], sum), more = fmaf(e[V + j], e[V + j], more);
+        sum += more;
+        if (pow2) {
+          for (int d = 1; d < slots; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
+        } else {  // sums of the lanes above within the head, then the first lane's
+          for (int d = 1; d < slots; d <<= 1) {
+            const float v = __shfl_down_sync(~0u, sum, d);
+            if (slot + d < slots) sum += v;
+          }
+          sum = __shfl_sync(~0u, sum, lane - slot);
+        }
+        inv = rsqrtf(fmaf(sum, p.per_element, p.r.eps));
+      }
+      float r[2 * V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int k = APART ? j : 2 * j, l = APART ? V + j : 2 * j + 1;
+        r[k] = e[k] * uc[j], r[l] = e[l] * vc[j];
+        if (turns && (APART || slot * V + j < half)) {
+          r[k] = __fmaf_rn(e[k], uc[j], -__fmul_rn(e[l], vs[j]));
+          r[l] = __fmaf_rn(e[l], vc[j], __fmul_rn(e[k], us[j]));
+        }
+        if (NORM) r[k] *= inv, r[l] *= inv;
+      }
+      Unit<T, V> ra, rb;
+      ra.pack(r), rb.pack(r + V);
+      if (keep) *reinterpret_cast<Unit<T, V>*>(y + at) = ra, *reinterpret_cast<Unit<T, V>*>(y + with) = rb;
+      y += y_step;
     }
+    t -= turns_of;
   }
 }
 
 template <typename T, int V>
-ssd_status rotary_launch(RotaryParams& p, cudaStream_t s) {
-  p.slots = (p.r.head_dim / 2 + V - 1) / V;
-  // A warp takes as many heads of a row as leave every SM its 48 warps or more: the row's sines are made anew by every
-  // warp that works on it.
-  const int in_warp = 32 / p.slots, turns = (p.heads + in_warp - 1) / in_warp;
-  const int64_t all = static_cast<int64_t>(p.rows) * turns, most = all / (152 * 48);
-  const int each = most < 1 ? 1 : most < turns ? static_cast<int>(most) : turns;
-  const int parts = (turns + each - 1) / each;
-  p.span = (turns + parts - 1) / parts * in_warp;
-  p.spans = (p.heads + p.span - 1) / p.span;
-  const int64_t ctas = (static_cast<int64_t>(p.rows) * p.spans + 7) / 8;
-  if (ctas > 0x7fffffff) return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: %d rows of %d heads", p.rows, p.heads);
-  const dim3 grid(static_cast<unsigned>(ctas));
-  return p.r.interleaved ? op_launch("ssd_rotary_apply", ssd_rotary_kernel<T, V, false>, grid, 256, 0, s, p)
-                         : op_launch("ssd_rotary_apply", ssd_rotary_kernel<T, V, true>, grid, 256, 0, s, p);
+ssd_status rotary_launch(RotaryParams& p, int n, cudaStream_t s) {
+  p.slots = p.r.head_dim / 2 / V;
+  const int in_warp = 32 / p.slots;
+  for (int i = 0; i < n; ++i) p.turns[i] = (p.op[i].heads + in_warp - 1) / in_warp;
+  const int turns = p.turns[0] + p.turns[1];
+  // Warps of a row: as few (the row's sines are used most often) as leave every SM kRotaryWarps of them.
+  const int64_t want = 152 * kRotaryWarps;
+  int split = 1;
+  while (split < turns && static_cast<int64_t>(p.rows) * split < want) split *= 2;
+  p.warps = split < 8 ? split : 8;
+  const int each = 8 / p.warps;
+  const dim3 grid((p.rows + each - 1) / each, split / p.warps);
+  if (p.norms)
+    return p.r.interleaved ? op_launch("ssd_rotary_apply", ssd_rotary_kernel<T, V, false, true>, grid, 256, 0, s, p)
+                           : op_launch("ssd_rotary_apply", ssd_rotary_kernel<T, V, true, true>, grid, 256, 0, s, p);
+  return p.r.interleaved ? op_launch("ssd_rotary_apply", ssd_rotary_kernel<T, V, false, false>, grid, 256, 0, s, p)
+                         : op_launch("ssd_rotary_apply", ssd_rotary_kernel<T, V, true, false>, grid, 256, 0, s, p);
 }
 
 // The widest unit that divides the pairs, the turning ones and every stride, and to which every head is aligned.
@@ -225,10 +279,10 @@ ssd_status rotary_dispatch(RotaryParams& p, int n, cudaStream_t s) {
     if (p.rows > 1) bits |= o.x_row | o.y_row;
     if (o.heads > 1) bits |= o.x_head | o.y_head;
   }
-  if (sizeof(T) == 2 && bits % 8 == 0) return rotary_launch<T, 16 / sizeof(T)>(p, s);
-  if (bits % 4 == 0) return rotary_launch<T, 4>(p, s);
-  if (bits % 2 == 0 && p.r.head_dim <= 128) return rotary_launch<T, 2>(p, s);
-  if (p.r.head_dim <= 64) return rotary_launch<T, 1>(p, s);
+  if (sizeof(T) == 2 && bits % 8 == 0) return rotary_launch<T, 16 / sizeof(T)>(p, n, s);
+  if (bits % 4 == 0) return rotary_launch<T, 4>(p, n, s);
+  if (bits % 2 == 0 && p.r.head_dim <= 128) return rotary_launch<T, 2>(p, n, s);
+  if (p.r.head_dim <= 64) return rotary_launch<T, 1>(p, n, s);
   const int64_t ctas = (static_cast<int64_t>(p.rows) * p.heads + 7) / 8;
   if (ctas > 0x7fffffff) return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: %d rows of %d heads", p.rows, p.heads);
   return op_launch("ssd_rotary_apply", ssd_rotary_any_kernel<T>, dim3(static_cast<unsigned>(ctas)), 256, 0, s, p);
@@ -282,6 +336,7 @@ ssd_status ssd_rotary_apply(const ssd_rotary* r, const ssd_heads* operand, int n
   const int size = type == SSD_TYPE_FP32 ? 4 : 2;
   RotaryParams p = {};
   p.r = *r, p.pos = pos, p.pos_row = pos_row, p.pos_axis = pos_axis, p.rows = rows;
+  p.per_element = 1.0f / r->head_dim;
   for (int i = 0; i < n; ++i) {
     const ssd_heads& h = operand[i];
     if (h.heads < 1 || h.heads > 1 << 14) return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: %d heads", h.heads);
