@@ -68,9 +68,12 @@ __device__ __forceinline__ float key_value(uint32_t key) {  // the inverse of or
 }
 constexpr uint32_t kKeyNone = 0x007fffffu, kKeyInf = 0xff800000u;  // orderable(-inf), orderable(inf)
 
-// floor(a * b / 2^64) of b = 2^64 * f, f in [0, 1); up: the ceiling.
+// floor(a * f) of f in [0, 1), f's digits below 2^-64 cut off; up: the ceiling.  In integers: a 64-bit float operation
+// costs an SM of this GPU 16 cycles a warp.
 __device__ __forceinline__ uint64_t times_fraction(uint64_t a, float f, bool up) {
-  const uint64_t b = static_cast<uint64_t>(static_cast<double>(f) * 0x1p64);
+  const int e = static_cast<int>(__float_as_uint(f) >> 23);  // f = digits * 2^(e - 150)
+  const uint64_t digits = (__float_as_uint(f) & 0x7fffffu) | 0x800000u;
+  const uint64_t b = e >= 86 ? digits << (e - 86) : e > 86 - 24 ? digits >> (86 - e) : 0;
   return __umul64hi(a, b) + (up && a * b != 0 ? 1 : 0);
 }
 
@@ -91,17 +94,24 @@ struct SampleParams {
 // mass each; the bin in which the rule's count or mass is reached is split by the logits' bits into up to 704 again until
 // one value is left.  All sums are of integers, so neither the atomics' order nor the cut into CTAs matters.
 
-constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kBins = kMassPlaces >> 6, kSegUnits = 64, kSegs = 256;
-constexpr int kUses = 8;  // values that CTAs send each other, each at a place of its own
+constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kBins = kMassPlaces >> 6, kGroup = kBins / kSampleWarps,
+              kSegUnits = 64, kSegs = 256;
+static_assert(kBins % kSampleWarps == 0 && kGroup % 2 == 0 && kGroup <= 64, "a warp adds up a group");
+constexpr int kUses = 10;   // values that CTAs send each other, each at a place of its own
+constexpr int kList = 512;  // tokens that one CTA ranks by comparing all with all
 
 struct SampleShared {
   uint32_t table[kExpSize];
-  uint64_t bin[2][kBins];   // of one search step, and of the next
+  uint64_t bin[2][kBins];                    // of one search step, and of the next
+  uint64_t groups[2][8][kSampleWarps];       // their sums over kGroup bins, of every CTA
   uint64_t seg[kSegs];
-  uint64_t part[kSampleWarps];
-  uint64_t sent[kUses][8];  // written by the CTA of that rank
-  uint64_t before, at;      // what find_bin found
-  int border;
+  uint64_t part[2][kSampleWarps];
+  uint64_t sent[kUses][8];                   // written by the CTA of that rank
+  uint64_t list[kList];                      // key and inverted index of tokens that are ranked one by one
+  uint64_t all[kList + 2];                   // the cluster's lists as one
+  uint64_t by_rank[kList], by_index[kList], sorted[kList];
+  uint64_t before, at;
+  int border, listed, first, kept;
 };
 
 __device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
@@ -158,6 +168,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   cluster_arrive();
   for (int i = tid; i < kExpSize; i += kSampleThreads) sh.table[i] = kExpTable.v[i];
   for (int i = tid; i < 2 * kBins; i += kSampleThreads) sh.bin[0][i] = 0;
+  if (tid == 0) sh.first = vocab;
   pdl_wait();
   pdl_trigger();
 
@@ -173,35 +184,36 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
 #pragma unroll
     for (int e = 0; e < E; ++e) most = fmaxf(most, to_f32(x.v[e]));
   };
-  if (tid < 2 && (tid == 0 || units > 1) && units > 0) {
-    const int u = tid == 0 ? 0 : units - 1;
-    Logits16<T> x;
-    for (int e = 0; e < E; ++e) {
-      const int i = u * E + e - phase;
-      x.v[e] = i >= 0 && i < v1 - v0 ? src[i] : from_f32<T>(-INFINITY);
-    }
-    take(u, x);
-  }
   {
     const uint4* in = reinterpret_cast<const uint4*>(src - phase);
     constexpr int kAhead = 4;
-    for (int u = 1 + tid; u < units - 1; u += kAhead * kSampleThreads) {
+    for (int u = tid; u < units; u += kAhead * kSampleThreads) {
       Logits16<T> x[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i)
-        if (u + i * kSampleThreads < units - 1) x[i].w = in[u + i * kSampleThreads];
+      for (int i = 0; i < kAhead; ++i) {
+        const int v = u + i * kSampleThreads;
+        if (v > 0 && v < units - 1) x[i].w = in[v];
+      }
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i)
-        if (u + i * kSampleThreads < units - 1) take(u + i * kSampleThreads, x[i]);
+      for (int i = 0; i < kAhead; ++i) {
+        const int v = u + i * kSampleThreads;
+        if (v == 0 || v == units - 1)
+          for (int e = 0; e < E; ++e) {
+            const int j = v * E + e - phase;
+            x[i].v[e] = j >= 0 && j < v1 - v0 ? src[j] : from_f32<T>(-INFINITY);
+          }
+        if (v < units) take(v, x[i]);
+      }
     }
   }
+  const float most_of_thread = most;
 #pragma unroll
   for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
-  if (lane == 0) sh.part[warp] = __float_as_uint(most);
+  if (lane == 0) sh.part[0][warp] = __float_as_uint(most);
   cluster_wait();  // every CTA of the cluster runs
   __syncthreads();
   if (tid < ctas) {
-    for (int i = 0; i < kSampleWarps; ++i) most = fmaxf(most, __uint_as_float(static_cast<uint32_t>(sh.part[i])));
+    for (int i = 0; i < kSampleWarps; ++i) most = fmaxf(most, __uint_as_float(static_cast<uint32_t>(sh.part[0][i])));
     cluster_store(&sh.sent[0][rank], tid, __float_as_uint(most));
   }
   cluster_sync();
@@ -225,151 +237,278 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   const bool infinite = top_key == kKeyInf;  // only its equals have mass
   MassOf mass;
   {
-    const double c = -2048.0 * 1.4426950408889634074 / static_cast<double>(one ? 1.0f : temp);
+    // -2048 log2(e) / T by the remainder of the rounded quotient
+    constexpr double kScale = -2048.0 * 1.4426950408889634074;
+    constexpr float kHigh = static_cast<float>(kScale), kLow = static_cast<float>(kScale - static_cast<double>(kHigh));
+    const float t = one ? 1.0f : temp;
     mass.half_top = 0.5f * top;
-    mass.c_hi = static_cast<float>(c);
-    mass.c_lo = static_cast<float>(c - mass.c_hi);
+    mass.c_hi = kHigh / t;
+    mass.c_lo = isinf(mass.c_hi) ? 0.0f : (fmaf(-mass.c_hi, t, kHigh) + kLow) / t;
   }
   // kept: logits above `cut`, and of those equal to it the tokens up to `last`
   float cut = infinite ? top : -FLT_MAX;
   int last = vocab - 1;
   auto kept = [&](float l, int index) { return l >= cut && (l != cut || index <= last); };
-  auto place_of = [&](float l) { return infinite ? 0 : mass.place(l); };
+  auto place_of = [&](float l) { return !infinite ? mass.place(l) : l == top ? 0 : kMassPlaces; };
   auto mass_of = [&](float l) -> uint64_t { return infinite ? 1ull << 44 : mass(l, sh.table); };
+
+  // what min_p leaves: exp(z - max z) >= min_p in masses
+  const uint64_t least = min_p >= 1.0f ? mass_of(top) : min_p > 0.0f ? times_fraction(mass_of(top), min_p, true) : 0;
+  auto aim = [&](uint64_t all) -> uint64_t {
+    const float u = p.u[row];
+    return u >= 1.0f ? all - 1 : u > 0.0f ? times_fraction(all, u, false) : 0;
+  };
+  auto put = [&](int index, float l, uint64_t all) {
+    p.token[row] = index;
+    if (!p.prob) return;
+    // share / all, by a fp32 reciprocal that one step makes exact to 2^-44
+    const int at = place_of(l);
+    const double share = infinite ? 0x1p44 : static_cast<double>(mass.digits(l, at, sh.table)) *
+                                                 __hiloint2double((1023 + 12 - (at >> kExpBits)) << 20, 0);
+    const double a = static_cast<double>(all), r = static_cast<double>(1.0f / static_cast<float>(all));
+    p.prob[row] = static_cast<float>(share * fma(fma(-a, r, 1.0), r, r));
+  };
+
+  // Inclusive sums over the threads.  `turn` alternates, so that one barrier a sum is enough.
+  auto scan = [&](uint64_t v, int turn, uint64_t& all) {
+    v = warp_scan(v);
+    if (lane == 31) sh.part[turn][warp] = v;
+    __syncthreads();
+    all = 0;
+#pragma unroll
+    for (int i = 0; i < kSampleWarps; ++i) {
+      if (i == warp) v += all;
+      all += sh.part[turn][i];
+    }
+    return v;
+  };
 
   // The first token in vocabulary order whose running measure exceeds aim(all of it): calls found(index, logit, all) in
   // one thread of the cluster.
   int uses = 1;
+  constexpr int kSeg = kSegUnits * E;
+  static_assert(kSeg <= kSampleThreads, "a segment's tokens are looked at by a thread each");
   auto walk = [&](auto measure, auto aim, auto found) {
     const int segs = (units + kSegUnits - 1) / kSegUnits;
     for (int s = warp; s < segs; s += kSampleWarps) {
       uint64_t sum = 0;
+#pragma unroll 1
+      for (int u = s * kSegUnits + lane; u < min((s + 1) * kSegUnits, units); u += 32) {
+        const Logits16<T> x = data[u];
 #pragma unroll
-      for (int i = 0; i < kSegUnits / 32; ++i) {
-        const int u = s * kSegUnits + 32 * i + lane;
-        if (u < units) {
-          const Logits16<T> x = data[u];
-#pragma unroll
-          for (int e = 0; e < E; ++e) sum += measure(to_f32(x.v[e]), first_index + u * E + e);
-        }
+        for (int e = 0; e < E; ++e) sum += measure(to_f32(x.v[e]), first_index + u * E + e);
       }
       sum = warp_sum(sum);
       if (lane == 0) sh.seg[s] = sum;
     }
     __syncthreads();
-    const int each = (segs + 31) / 32;
-    uint64_t mine = 0, run = 0;
-    if (warp == 0) {
-      for (int i = 0; i < each; ++i) mine += lane * each + i < segs ? sh.seg[lane * each + i] : 0;
-      run = warp_scan(mine);
-      const uint64_t sum = __shfl_sync(~0u, run, 31);
-      if (lane < ctas) cluster_store(&sh.sent[uses][rank], lane, sum);
-    }
+    uint64_t mine = tid < segs ? sh.seg[tid] : 0, sum, all = 0, base = 0;
+    const uint64_t run = scan(mine, 0, sum);
+    if (tid < ctas) cluster_store(&sh.sent[uses][rank], tid, sum);
     cluster_sync();
-    if (warp == 0) {
-      uint64_t base = 0, all = 0;
-      for (int i = 0; i < ctas; ++i) {
-        if (i == rank) base = all;
-        all += sh.sent[uses][i];
-      }
-      const uint64_t goal = aim(all);
-      run += base - mine;  // before this lane's segments
-      const uint32_t owner = __ballot_sync(~0u, run <= goal && goal < run + mine);
-      if (owner) {
-        int s = 0;
-        if (owner >> lane & 1)
-          for (s = lane * each; goal >= run + sh.seg[s]; ++s) run += sh.seg[s];
-        const int from = __ffs(owner) - 1;
-        s = __shfl_sync(~0u, s, from);
-        run = __shfl_sync(~0u, run, from);
-        // a lane's neighbouring units
-        uint64_t sum = 0;
-        constexpr int kEach = kSegUnits / 32;
-        const int u0 = s * kSegUnits + lane * kEach, u1 = min(u0 + kEach, units);
-        for (int u = u0; u < u1; ++u)
-          for (int e = 0; e < E; ++e) sum += measure(to_f32(data[u].v[e]), first_index + u * E + e);
-        run += warp_scan(sum) - sum;
-        if (run <= goal && goal < run + sum) {
-          for (int u = u0; u < u1; ++u)
-            for (int e = 0; e < E; ++e) {
-              const float l = to_f32(data[u].v[e]);
-              const uint64_t m = measure(l, first_index + u * E + e);
-              if (run <= goal && goal < run + m) found(first_index + u * E + e, l, all);
-              run += m;
-            }
-        }
-      }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i == rank) base = all;
+      if (i < ctas) all += sh.sent[uses][i];
     }
     ++uses;
+    const uint64_t goal = aim(all);
+    if (goal < base || goal >= base + sum) return;
+    if (base + run - mine <= goal && goal < base + run) sh.border = tid, sh.before = base + run - mine;
+    __syncthreads();
+    const int i = sh.border * kSeg + tid, index = first_index + i;
+    float l = 0.0f;
+    mine = 0;
+    if (tid < kSeg && i < units * E) {
+      l = to_f32(reinterpret_cast<const T*>(data)[i]);
+      mine = measure(l, index);
+    }
+    const uint64_t from = sh.before + scan(mine, 1, sum) - mine;
+    if (from <= goal && goal < from + mine) found(index, l, all);
   };
   if (one) {
-    walk([&](float l, int) -> uint64_t { return l == top; }, [](uint64_t) { return 0ull; },
-         [&](int index, float, uint64_t) {
-           p.token[row] = index;
-           if (p.prob) p.prob[row] = 1.0f;
-         });
+    if (most_of_thread == top)
+      for (int u = tid; u < units; u += kSampleThreads)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (to_f32(data[u].v[e]) == top) atomicMin(&sh.first, first_index + u * E + e);
+    __syncthreads();
+    if (tid == 0) cluster_store(&sh.sent[1][rank], 0, sh.first);
+    cluster_sync();
+    if (rank == 0 && tid == 0) {
+      int first = sh.first;
+      for (int i = 1; i < ctas; ++i) first = min(first, static_cast<int>(sh.sent[1][i]));
+      p.token[row] = first;
+      if (p.prob) p.prob[row] = 1.0f;
+    }
     return;
   }
 
-  // Adds up the cluster's bins of this step, finds the one in which the running measure reaches goal(all of it) (1 or
-  // more; 0: none) and returns the goal.
+  // Adds up the cluster's bins of this step, finds the one in which the running measure reaches goal_of(all of it) (1 or
+  // more; 0: none) and returns the goal.  Every CTA gets the others' sums over groups of bins, and reads one group.
   int step = 0;
   auto find_bin = [&](auto goal_of) -> uint64_t {
-    cluster_sync();
-    uint64_t a = 0, b = 0;
-    if (tid < kBins / 2)
-      for (int r = 0; r < ctas; ++r) {
-        uint64_t x, y;
-        cluster_load2(&sh.bin[step & 1][2 * tid], r, x, y);
-        a += x, b += y;
-      }
-    // the other CTAs have read the bins of the step before
-    for (int i = tid; i < kBins; i += kSampleThreads) sh.bin[~step & 1][i] = 0;
-    uint64_t run = warp_scan(a + b);
-    if (lane == 31) sh.part[warp] = run;
+    const int b = step & 1;
     __syncthreads();
-    uint64_t all = 0;
-    for (int i = 0; i < kSampleWarps; ++i) {
-      if (i == warp) run += all;
-      all += sh.part[i];
+    {
+      uint64_t v = lane < kGroup ? sh.bin[b][warp * kGroup + lane] : 0;
+      if (lane + 32 < kGroup) v += sh.bin[b][warp * kGroup + lane + 32];
+      v = warp_sum(v);
+      if (lane < ctas) cluster_store(&sh.groups[b][rank][warp], lane, v);
     }
-    const uint64_t goal = goal_of(all), before = run - a - b;
-    if (before < goal && goal <= run) {
-      const bool in_b = goal > before + a;
-      sh.border = 2 * tid + in_b;
-      sh.before = in_b ? before + a : before;
-      sh.at = in_b ? b : a;
+    cluster_sync();
+    // the other CTAs have read the bins of the step before
+    for (int i = tid; i < kBins; i += kSampleThreads) sh.bin[b ^ 1][i] = 0;
+    uint64_t mine = 0;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      if (r < ctas && lane < kSampleWarps) mine += sh.groups[b][r][lane];
+    uint64_t run = warp_scan(mine);
+    const uint64_t goal = goal_of(__shfl_sync(~0u, run, 31));
+    const uint32_t owner = __ballot_sync(~0u, run - mine < goal && goal <= run);
+    if (warp == 0 && owner) {
+      const int group = __ffs(owner) - 1;
+      const uint64_t base = __shfl_sync(~0u, run - mine, group);
+      uint64_t x[8], y[8], v = 0, w = 0;  // all of them under way at once
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        x[r] = y[r] = 0;
+        if (r < ctas && lane < kGroup / 2) cluster_load2(&sh.bin[b][group * kGroup + 2 * lane], r, x[r], y[r]);
+      }
+#pragma unroll
+      for (int r = 0; r < 8; ++r) v += x[r], w += y[r];
+      const uint64_t before = base + warp_scan(v + w) - v - w;
+      if (before < goal && goal <= before + v + w) {
+        const bool in_w = goal > before + v;
+        sh.border = group * kGroup + 2 * lane + in_w;
+        sh.before = in_w ? before + v : before;
+        sh.at = in_w ? w : v;
+      }
     }
     __syncthreads();
     ++step;
     return goal;
   };
-  // Shrinks the kept tokens to the shortest prefix of the ranking whose measure reaches goal_of(all of it).
-  auto shrink = [&](auto measure, auto goal_of) {
+  auto measure = [&](float l, bool counting) { return counting ? 1ull : mass_of(l); };
+  // logits that a bin can hold, with two places more at either end than it has (and what rounding takes)
+  const float unit = temp * 6.7690154e-4f;  // of a place: T ln(2) / 1024
+  auto low_of = [&](int bin) {
+    return infinite ? top : fmaxf(__fsub_rd(top, __fmul_ru(unit, 64.0f * bin + 66.1f)), -FLT_MAX);
+  };
+  auto high_of = [&](int bin) { return infinite ? top : fminf(__fsub_ru(top, __fmul_rd(unit, 64.0f * bin - 2.1f)), top); };
+  auto add_to = [&](int bin, uint64_t v) {  // in halves: a 64-bit atomic on shared memory is a loop
+    uint32_t* at = reinterpret_cast<uint32_t*>(&sh.bin[step & 1][bin]);
+    const uint32_t low = static_cast<uint32_t>(v), high = static_cast<uint32_t>(v >> 32) + (atomicAdd(at, low) > ~low);
+    if (high) atomicAdd(at + 1, high);
+  };
+  auto count_in = [&](int bin) { atomicAdd(reinterpret_cast<uint32_t*>(&sh.bin[step & 1][bin]), 1u); };
+
+  // Lists the cluster's wanted tokens of logits in [low, high] in sh.all of every CTA, if they are kList at most, and
+  // returns how many there are, or -1.
+  auto collect = [&](float low, float high, auto wanted) -> int {
+    if (tid == 0) sh.listed = 0;
+    __syncthreads();
     for (int u = tid; u < units; u += kSampleThreads) {
       const Logits16<T> x = data[u];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float l = to_f32(x.v[e]);
-        const int at = kept(l, first_index + u * E + e) ? place_of(l) : kMassPlaces;
-        if (at < kMassPlaces) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.bin[step & 1][at >> 6]), measure(l));
+        if (!(l >= low && l <= high) || !wanted(l, first_index + u * E + e)) continue;
+        const int i = atomicAdd(&sh.listed, 1);
+        if (i < kList)
+          sh.list[i] = static_cast<uint64_t>(orderable(l + 0.0f)) << 32 | ~static_cast<uint32_t>(first_index + u * E + e);
+      }
+    }
+    __syncthreads();
+    if (tid < ctas) cluster_store(&sh.sent[uses][rank], tid, sh.listed);
+    cluster_sync();
+    int n = 0, from = 0, at = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < ctas) {
+        const int c = static_cast<int>(sh.sent[uses][i]);
+        if (tid >= n && tid < n + c) from = i, at = tid - n;  // entry tid of all is entry `at` of CTA `from`
+        n += c;
+      }
+    ++uses;
+    if (n > kList) return -1;
+    uint64_t v = 0;  // one past the end as well: two entries are compared at a time
+    if (tid < n) asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(cluster_addr(&sh.list[at], from)) : "memory");
+    if (tid <= n) sh.all[tid] = v;
+    __syncthreads();
+    return n;
+  };
+  // Entry tid / each of the list and its places by rank and by index, from comparing all with all: `each` neighbouring
+  // lanes share an entry's comparisons.
+  auto rank_list = [&](int n, int each, int& by_rank, int& by_index) -> uint64_t {
+    const uint64_t mine = tid / each < n ? sh.all[tid / each] : 0;
+    int better = 0, earlier = 0;
+#pragma unroll 4
+    for (int j = 2 * (tid & (each - 1)); j < n; j += 2 * each) {
+      const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(&sh.all[j]);
+      better += (v.x > mine) + (v.y > mine);
+      earlier += (static_cast<uint32_t>(v.x) > static_cast<uint32_t>(mine)) + (static_cast<uint32_t>(v.y) > static_cast<uint32_t>(mine));
+    }
+    for (int d = each / 2; d; d >>= 1)
+      better += __shfl_xor_sync(~0u, better, d), earlier += __shfl_xor_sync(~0u, earlier, d);
+    by_rank = better, by_index = earlier;
+    return mine;
+  };
+  auto share_of = [&](int n) {
+    int each = 1;
+    while (each < 32 && n * each * 2 <= kSampleThreads) each *= 2;
+    return each;
+  };
+
+  // Shrinks the kept tokens to the shortest prefix of the ranking whose count or mass reaches goal_of(all of it).
+  bool limited = false;
+  auto shrink = [&](bool counting, auto goal_of) {
+    for (int u = tid; u < units; u += kSampleThreads) {
+      const Logits16<T> x = data[u];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float l = to_f32(x.v[e]);
+        const int at = !limited || kept(l, first_index + u * E + e) ? place_of(l) : kMassPlaces;
+        if (at >= kMassPlaces) continue;
+        if (counting)
+          count_in(at >> 6);
+        else
+          add_to(at >> 6, mass_of(l));
       }
     }
     uint64_t goal = find_bin(goal_of);
     if (goal == 0) return;
     goal -= sh.before;
-    // logits that the bin can hold, a place more at either end than it has
     const int bin = sh.border;
-    const double unit = static_cast<double>(temp) / (1024.0 * 1.4426950408889634074);
-    float low = top, high = top;
-    if (!infinite) {
-      low = fmaxf(__double2float_rd(top - unit * (64.0 * bin + 65.0)), -FLT_MAX);
-      high = fminf(__double2float_ru(top - unit * (64.0 * bin - 1.5)), top);
+    const float low = low_of(bin), high = high_of(bin);
+    auto in_bin = [&](float l, int index) { return place_of(l) >> 6 == bin && kept(l, index); };
+    limited = true;
+    // fp32 logits in a bin are few and all different; bf16 ones are many equals of two or three values
+    const int n = KS == 0 ? collect(low, high, in_bin) : -1;
+    if (n >= 0) {
+      const int each = share_of(n);
+      int better, earlier;
+      const uint64_t mine = rank_list(n, each, better, earlier);
+      if (tid / each < n && (tid & (each - 1)) == 0) {
+        sh.by_rank[better] = measure(key_value(static_cast<uint32_t>(mine >> 32)), counting);
+        sh.sorted[better] = mine;
+      }
+      __syncthreads();
+      const uint64_t v = tid < n ? sh.by_rank[tid] : 0;
+      uint64_t all;
+      const uint64_t run = scan(v, 0, all);
+      if (run - v < goal && goal <= run) sh.at = sh.sorted[tid];
+      __syncthreads();
+      cut = key_value(static_cast<uint32_t>(sh.at >> 32));
+      last = static_cast<int>(~static_cast<uint32_t>(sh.at));
+      return;
     }
+    // more tokens than the list takes: the bin is split by the logits' keys until one is left
     uint32_t kmin = orderable(low) >> KS, kmax = orderable(high + 0.0f) >> KS;
     for (bool ready = false; !ready;) {
       const uint32_t width = kmax - kmin;  // one less than the keys
       const int shift = width < kBins ? 0 : 32 - __clz(width / kBins);
+#pragma unroll 1
       for (int u = tid; u < units; u += kSampleThreads) {
         const Logits16<T> x = data[u];
 #pragma unroll
@@ -377,8 +516,8 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
           const float l = to_f32(x.v[e]);
           if (!(l >= low && l <= high)) continue;
           const uint32_t key = orderable(l + 0.0f) >> KS;
-          if (key < kmin || key > kmax || !kept(l, first_index + u * E + e) || place_of(l) >> 6 != bin) continue;
-          atomicAdd(reinterpret_cast<unsigned long long*>(&sh.bin[step & 1][(kmax - key) >> shift]), measure(l));
+          if (key >= kmin && key <= kmax && in_bin(l, first_index + u * E + e))
+            add_to((kmax - key) >> shift, measure(l, counting));
         }
       }
       find_bin([&](uint64_t) { return goal; });
@@ -389,56 +528,79 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     }
     // kmax is the border's key; its equals fall by index
     const float value = key_value(kmax & (0x80000000u >> KS) ? kmax << KS : kmax << KS | ((1u << KS) - 1));
-    const uint64_t m = measure(value), wanted = (goal + m - 1) / m;
-    const bool all = wanted * m >= sh.at;
-    int end = vocab - 1;
-    if (!all) {
+    const uint64_t m = measure(value, counting), wanted = (goal + m - 1) / m;
+    int end = value == cut ? last : vocab - 1;
+    if (wanted * m < sh.at) {
       walk([&](float l, int) -> uint64_t { return l == value; }, [&](uint64_t) { return wanted - 1; },
            [&](int index, float, uint64_t) {
-             for (int r = 0; r < ctas; ++r) cluster_store(&sh.sent[uses + 1][0], r, index);
+             for (int r = 0; r < ctas; ++r) cluster_store(&sh.sent[uses][0], r, index);
            });
       cluster_sync();
       end = static_cast<int>(sh.sent[uses][0]);
       ++uses;
-    } else if (value == cut) {
-      end = last;
     }
     cut = value;
     last = end;
   };
-  if (top_k > 1 && top_k < vocab)
-    shrink([](float) { return 1ull; },
-           [&](uint64_t all) -> uint64_t { return all > static_cast<uint64_t>(top_k) ? top_k : 0; });
-  if (top_p < 1.0f)
-    shrink([&](float l) { return mass_of(l); },
-           [&](uint64_t all) -> uint64_t { return max(times_fraction(all, top_p, true), static_cast<uint64_t>(1)); });
-  if (min_p > 0.0f && !infinite) {
-    const double border = static_cast<double>(top) + static_cast<double>(temp) * log(static_cast<double>(min_p));
-    const float b = __double2float_ru(border < top ? border : top);
-    if (b > cut) cut = b, last = vocab - 1;
+
+  if (top_k > 1 && top_k < vocab) {
+    // At least top_k tokens are in or above the bin that the top_k-th of the threads' largest is in; usually few more.
+    // The first CTA ranks them, applies the rules to the sorted masses and draws.
+    if (top_k <= kList / 2) {
+      const int place = place_of(most_of_thread);
+      if (place < kMassPlaces) count_in(place >> 6);
+      const uint64_t found = find_bin([&](uint64_t all) -> uint64_t { return all >= static_cast<uint64_t>(top_k) ? top_k : 0; });
+      const int n = found ? collect(low_of(sh.border), top, [](float, int) { return true; }) : -1;
+      if (n >= 0) {
+        cluster_sync();
+        if (rank != 0) return;
+        const int each = share_of(n), most_kept = min(top_k, n);
+        int better, earlier;
+        const uint64_t mine = rank_list(n, each, better, earlier);
+        const float logit = key_value(static_cast<uint32_t>(mine >> 32));
+        const bool lead = tid / each < n && (tid & (each - 1)) == 0;
+        const uint64_t w = lead ? mass_of(logit) : 0;
+        if (lead) sh.by_rank[better] = w;
+        __syncthreads();
+        uint64_t v = tid < most_kept ? sh.by_rank[tid] : 0, all;
+        uint64_t run = scan(v, 0, all);
+        int keep = most_kept;
+        if (top_p < 1.0f) {
+          const uint64_t goal = max(times_fraction(all, top_p, true), static_cast<uint64_t>(1));
+          if (run - v < goal && goal <= run) sh.kept = tid + 1;
+          __syncthreads();
+          keep = sh.kept;
+        }
+        if (lead) {
+          sh.by_index[earlier] = better < keep && w >= least ? w : 0;
+          sh.sorted[earlier] = mine;
+        }
+        __syncthreads();
+        v = tid < n ? sh.by_index[tid] : 0;
+        run = scan(v, 1, all);
+        const uint64_t goal = aim(all);
+        if (run - v <= goal && goal < run)
+          put(static_cast<int>(~static_cast<uint32_t>(sh.sorted[tid])), key_value(static_cast<uint32_t>(sh.sorted[tid] >> 32)), all);
+        return;
+      }
+    }
+    shrink(true, [&](uint64_t all) -> uint64_t { return all > static_cast<uint64_t>(top_k) ? top_k : 0; });
   }
-  walk([&](float l, int index) -> uint64_t { return kept(l, index) ? mass_of(l) : 0; },
-       [&](uint64_t all) -> uint64_t {
-         const float u = p.u[row];
-         return u >= 1.0f ? all - 1 : u > 0.0f ? times_fraction(all, u, false) : 0;
-       },
-       [&](int index, float l, uint64_t all) {
-         p.token[row] = index;
-         if (p.prob) {
-           double share = 0x1p44;
-           if (!infinite) {
-             const int at = mass.place(l);
-             share = ldexp(static_cast<double>(mass.digits(l, at, sh.table)), 12 - (at >> kExpBits));
-           }
-           p.prob[row] = static_cast<float>(share / static_cast<double>(all));
-         }
-       });
+  if (top_p < 1.0f)
+    shrink(false, [&](uint64_t all) -> uint64_t { return max(times_fraction(all, top_p, true), static_cast<uint64_t>(1)); });
+  walk(
+      [&](float l, int index) -> uint64_t {
+        if (!kept(l, index)) return 0;
+        const uint64_t m = mass_of(l);
+        return m >= least ? m : 0;
+      },
+      aim, put);
 }
 
 template <typename T>
 ssd_status sample_launch(const SampleParams& p, int rows, cudaStream_t s) {
   static std::atomic<uint64_t> ready{0};
-  constexpr int kHead = (sizeof(SampleShared) + 15) / 16 * 16, kMost = 200 << 10;
+  constexpr int kHead = (sizeof(SampleShared) + 15) / 16 * 16, kMost = SSD_SAMPLE_MAX_VOCAB / 8 * 4 + 32;
   if (ssd_status e = op_smem(ssd_sample_kernel<T>, kHead + kMost, ready, "ssd_sample")) return e;
   // CTAs of a row: as many as fill the SMs, a part of 2048 tokens or more each, and of a size that leaves room for two
   // CTAs an SM
