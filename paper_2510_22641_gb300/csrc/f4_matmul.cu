@@ -24,10 +24,60 @@ __device__ __forceinline__ float f4_scaled(float sum, uint32_t rho_x, uint32_t r
   return max(rho_x, rho_w) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : v;
 }
 
-template <typename T>
-__device__ __forceinline__ void f4_store(const F4MatmulParams& p, int m, int n, float v) {
-  if (p.residual) v += to_f32(static_cast<const T*>(p.residual)[m * p.r_row + n]);
-  static_cast<T*>(p.y)[m * p.y_row + n] = from_f32<T>(v);
+// Whether a scale is within 2^-60 .. 2^60, where a sum may be multiplied by one after the other.
+__device__ __forceinline__ bool f4_plain(uint32_t rho) { return rho - (67u << 23) <= (120u << 23); }
+
+// Bounded waits, of about two seconds: false when they run out.  By the SM's clock: one read of the global timer costs
+// as much as the products of half a stage.
+template <typename F>
+__device__ __forceinline__ bool f4_wait_for(F ready) {
+  long long start = 0;
+  for (uint32_t i = 1;; ++i) {
+    if (ready()) return true;
+    if ((i & 1023u) != 0) continue;
+    const long long now = clock64();
+    if (start == 0) start = now;
+    if (now - start > 4000000000ll) return false;
+  }
+}
+__device__ __forceinline__ bool f4_wait(uint64_t* bar, uint32_t parity) {
+  return f4_wait_for([&] { return mbar_try_wait(bar, parity); });
+}
+
+// N sums times their rows' scales (rho: of the x rows, in shared memory); NaN where the sums are not valid.
+template <int N>
+__device__ __forceinline__ void f4_scale(float* v, const uint32_t* rho, uint32_t rho_w, bool plain, bool valid) {
+  const float fw = __uint_as_float(rho_w);
+  if (plain && valid) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = v[j] * __uint_as_float(rho[j]) * fw;
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = valid ? f4_scaled(v[j], rho[j], rho_w) : __uint_as_float(0x7fc00000u);
+  }
+}
+
+// Stores N sums of weight row n and x rows m .. m + count - 1.  rho: of the x rows, in shared memory.  plain: both
+// rows' scales are f4_plain.
+template <typename T, int N>
+__device__ __forceinline__ void f4_store(const F4MatmulParams& p, int m, int n, int count, const float* v,
+                                         const uint32_t* rho, uint32_t rho_w, bool plain) {
+  T* y = static_cast<T*>(p.y) + m * p.y_row + n;
+  const float fw = __uint_as_float(rho_w);
+  if (plain && count >= N && !p.residual) {
+#pragma unroll
+    for (int j = 0; j < N; ++j, y += p.y_row) *y = from_f32<T>(v[j] * __uint_as_float(rho[j]) * fw);
+  } else {
+    const T* r = static_cast<const T*>(p.residual);
+    if (r) r += m * p.r_row + n;
+#pragma unroll
+    for (int j = 0; j < N; ++j, y += p.y_row) {
+      if (j >= count) break;
+      const float s = f4_scaled(v[j], rho[j], rho_w);
+      *y = from_f32<T>(r ? s + to_f32(*r) : s);
+      r += r ? p.r_row : 0;
+    }
+  }
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -38,26 +88,27 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float ld_cluster(uint32_t addr, uint32_t rank) {
+__device__ __forceinline__ float4 ld_cluster(uint32_t addr, uint32_t rank) {
   uint32_t a;
-  float v;
+  float4 v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
   return v;
 }
 
-// A tile is 128 weight rows (the matrix rows, so that few x rows are few columns) by up to BN x rows.
+// ------------------------------------------------------------------ up to 128 rows
+//
+// A tile is 128 weight rows (the matrix rows, so that few x rows are few columns) by all x rows, up to BN.
 template <int BN>
 struct F4Tile {
-  static constexpr int kRecords = (BN + kF4Rows - 1) / kF4Rows;  // of x
-  static constexpr int kStages = BN > 128 ? 4 : BN > 64 ? 5 : 4;
+  static constexpr int kStages = BN > 64 ? 3 : 4;  // two CTAs an SM
   static constexpr int kCodes = BN * kF4Cols / 2, kScales = kF4Record - kF4CodeBytes;
-  static constexpr int kStage = kF4Record + kCodes + kRecords * kScales;
-  // tensor memory columns: the sums, then each stage's scales (16 of w, 16 of each x record)
-  static constexpr int kSums = BN < 32 ? 32 : BN, kScaleCols = 16 + 16 * kRecords;
-  static constexpr int kCols = kSums + kStages * kScaleCols <= 256 ? 256 : 512;
+  static constexpr int kStage = kF4Record + kCodes + kScales;
+  // tensor memory columns: the sums, then each stage's scales (16 of w, 16 of x)
+  static constexpr int kSums = BN < 32 ? 32 : BN, kScaleCols = 32;
+  static constexpr int kCols = 256;
   static constexpr int kSmem = 1024 + kStages * kStage + 256 + BN * 4;
-  static_assert(kSums + kStages * kScaleCols <= kCols && kCols <= 512, "tensor memory");
+  static_assert(BN <= kF4Rows && kSums + kStages * kScaleCols <= kCols, "tensor memory");
   static_assert(BN * kF4Rows * 4 <= kStages * kStage, "partial sums take the stages' place");
 };
 
@@ -76,7 +127,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
   uint32_t* rho = reinterpret_cast<uint32_t*>(full) + 64;
   float* part = reinterpret_cast<float*>(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n0 = blockIdx.x * kF4Rows, m0 = blockIdx.y * BN, cols = min(BN, p.rows - m0), nn = (cols + 15) / 16 * 16;
+  const int n0 = blockIdx.x * kF4Rows, cols = p.rows, nn = (cols + 15) / 16 * 16;
   const int split = gridDim.z, rank = blockIdx.z;
   const int c0 = static_cast<int>(static_cast<int64_t>(p.chunks) * rank / split);
   const int c1 = static_cast<int>(static_cast<int64_t>(p.chunks) * (rank + 1) / split);
@@ -101,22 +152,18 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
   if (warp == 0) {
     if (lane == 0) {
       const uint8_t* w = p.w + static_cast<int64_t>(blockIdx.x) * p.chunks * kF4Record;
-      const uint8_t* x = p.x + static_cast<int64_t>(m0 / kF4Rows) * p.chunks * kF4Record;
-      const int records = (nn + kF4Rows - 1) / kF4Rows, last = nn - (records - 1) * kF4Rows;
-      const uint32_t x_bytes = nn * 128 + records * S::kScales;
+      const uint8_t* x = p.x;
       auto load_w = [&](int c) {
         const int s = (c - c0) % S::kStages;
-        mbar_arrive_expect_tx(&full[s], kF4Record + x_bytes);
+        mbar_arrive_expect_tx(&full[s], kF4Record + nn * 128 + S::kScales);
         bulk_load(smem + s * S::kStage, w + static_cast<int64_t>(c) * kF4Record, kF4Record, &full[s]);
       };
       auto load_x = [&](int c) {
         const int s = (c - c0) % S::kStages;
         uint8_t* at = smem + s * S::kStage + kF4Record;
-        for (int r = 0; r < records; ++r) {
-          const uint8_t* rec = x + (static_cast<int64_t>(r) * p.chunks + c) * kF4Record;
-          bulk_load(at + r * kF4CodeBytes, rec, (r + 1 < records ? kF4Rows : last) * 128, &full[s]);
-          bulk_load(at + S::kCodes + r * S::kScales, rec + kF4CodeBytes, S::kScales, &full[s]);
-        }
+        const uint8_t* rec = x + static_cast<int64_t>(c) * kF4Record;
+        bulk_load(at, rec, nn * 128, &full[s]);
+        bulk_load(at + S::kCodes, rec + kF4CodeBytes, S::kScales, &full[s]);
       };
       if (!p.early) pdl_wait();
       const int ahead = min(c1, c0 + S::kStages);
@@ -126,7 +173,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
       int c = ahead;
       for (; c < c1; ++c) {
         const int i = c - c0;
-        if (!mbar_wait(&empty[i % S::kStages], (i / S::kStages - 1) & 1)) break;
+        if (!f4_wait(&empty[i % S::kStages], (i / S::kStages - 1) & 1)) break;
         load_w(c);
         load_x(c);
       }
@@ -137,7 +184,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
       const uint32_t idesc = umma_idesc_f4(kF4Rows, nn);
       for (int c = c0; c < c1; ++c) {
         const int i = c - c0, s = i % S::kStages;
-        if (!mbar_wait(&full[s], (i / S::kStages) & 1)) {
+        if (!f4_wait(&full[s], (i / S::kStages) & 1)) {
           ok = false;
           break;
         }
@@ -146,15 +193,12 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
           tmem_copy_scales(sa + 4 * kk, umma_desc_scales(at + kF4CodeBytes + 512 * kk));
-#pragma unroll
-          for (int r = 0; r < S::kRecords; ++r)
-            tmem_copy_scales(sb + 4 * (S::kRecords * kk + r),
-                             umma_desc_scales(at + kF4Record + S::kCodes + r * S::kScales + 512 * kk));
+          tmem_copy_scales(sb + 4 * kk, umma_desc_scales(at + kF4Record + S::kCodes + 512 * kk));
         }
         const uint64_t a = umma_desc_sw128(at), b = umma_desc_sw128(at + kF4Record);
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)  // 64 columns are 32 bytes of the 128-byte rows
-          umma_f4(tmem, a + 2 * kk, b + 2 * kk, idesc, sa + 4 * kk, sb + 4 * S::kRecords * kk, i > 0 || kk > 0);
+          umma_f4(tmem, a + 2 * kk, b + 2 * kk, idesc, sa + 4 * kk, sb + 4 * kk, i > 0 || kk > 0);
         umma_commit(&empty[s]);
       }
       if (ok) umma_commit(done);
@@ -162,10 +206,13 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
   } else {
     const int q = warp & 3, n = n0 + q * 32 + lane;
     pdl_wait();
-    for (int i = threadIdx.x - 64; i < cols; i += 128) rho[i] = p.x_rho[m0 + i];
+    for (int i = threadIdx.x - 64; i < cols; i += 128) rho[i] = p.x_rho[i];
     const uint32_t rho_w = n < p.n ? p.w_rho[n] : 0u;
     named_bar_sync(1, 128);
-    ok = mbar_wait(done, 0);
+    bool plain = f4_plain(rho_w);
+    for (int i = 0; i < cols; ++i) plain &= f4_plain(rho[i]);
+    plain = __all_sync(~0u, plain || n >= p.n);
+    ok = f4_wait(done, 0);
     tmem_fence_after();
     for (int c = 0; c < nn; c += 16) {
       float v[16];
@@ -176,9 +223,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
 #pragma unroll
         for (int j = 0; j < 16; ++j) part[(c + j) * kF4Rows + q * 32 + lane] = v[j];
       } else if (n < p.n) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (c + j < cols) f4_store<T>(p, m0 + c + j, n, f4_scaled(v[j], rho[c + j], rho_w));
+        f4_store<T, 16>(p, c, n, cols - c, v, rho + c, rho_w, plain);
       }
     }
   }
@@ -186,15 +231,32 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
   tmem_fence_before();
   __syncthreads();
   if (split > 1) {
+    // every CTA adds up a part of the x rows, four weight rows a lane, eight loads under way at a time
     cluster_barrier();
-    const int i0 = cols * rank / split, i1 = cols * (rank + 1) / split, n = n0 + (threadIdx.x & 127);
-    if (threadIdx.x < 128 && n < p.n) {
-      const uint32_t rho_w = p.w_rho[n];
-      for (int i = i0; i < i1; ++i) {
-        float v = 0.0f;
-        const uint32_t at = smem_u32(&part[i * kF4Rows + threadIdx.x]);
-        for (int r = 0; r < split; ++r) v += ld_cluster(at, r);
-        f4_store<T>(p, m0 + i, n, f4_scaled(v, rho[i], rho_w));
+    const int i0 = cols * rank / split, i1 = cols * (rank + 1) / split, n = n0 + 4 * lane;
+    const uint32_t at = smem_u32(part + 4 * lane);
+    uint32_t rho_w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) rho_w[j] = n + j < p.n ? p.w_rho[n + j] : 0;
+    constexpr int kAhead = 4;
+    for (int i = i0 + warp; i < i1; i += kAhead * 6) {
+      float4 v[kAhead] = {};
+      for (int r = 0; r < split; ++r) {
+        float4 t[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if (i + 6 * k < i1) t[k] = ld_cluster(at + (i + 6 * k) * kF4Rows * 4, r);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if (i + 6 * k < i1) v[k].x += t[k].x, v[k].y += t[k].y, v[k].z += t[k].z, v[k].w += t[k].w;
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (i + 6 * k >= i1) break;
+        const float s[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (n + j < p.n) f4_store<T, 1>(p, i + 6 * k, n + j, 1, s + j, rho + i + 6 * k, rho_w[j], false);
       }
     }
     __syncwarp();
@@ -206,28 +268,298 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
   }
 }
 
+// ------------------------------------------------------------------ many rows
+//
+// Pairs of CTAs, two SMs each, go over tiles of 256 weight rows by 256 x rows, x rows fastest, so that the pairs at work
+// share few weight rows and weights are read from memory once.  A product of the pair takes 128 weight rows and half of the
+// x rows from either CTA's shared memory.  Warp 0 copies, warp 1 of the first CTA issues the products, warps 10..13 move
+// the scales, warps 2..9 take a tile's sums into registers and give the tensor memory back before they store them.
+
+__device__ __forceinline__ uint32_t cluster_map(const void* p, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  return a;
+}
+// Arrives at another CTA's barrier.  What it tells of lies in tensor memory (written, and fenced by tcgen05.fence) or came
+// by bulk copies whose own barrier was waited for; no ordinary store is published, so cluster-wide release and acquire,
+// which cost 700 cycles a stage, are not needed.
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// The products issued so far arrive at this barrier of both CTAs when they are done.
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+      "h"(static_cast<uint16_t>(3))
+      : "memory");
+}
+
+constexpr int kF4PairThreads = 448;
+struct F4Pair {
+  static constexpr int kStages = 5;
+  static constexpr int kCodes = 128 * 128, kScales = kF4Record - kF4CodeBytes;  // half of the x rows' codes; all their scales
+  static constexpr int kStage = kF4Record + kCodes + 2 * kScales;
+  static constexpr int kSums = 256, kScaleCols = 16 + 32;
+  static constexpr int kSmem = 1024 + kStages * kStage + 256 + 2 * 256 * 4;
+  static_assert(kSums + kStages * kScaleCols <= 512, "tensor memory");
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kF4PairThreads, 1) ssd_f4_matmul_pair_kernel(const F4MatmulParams p) {
+  using S = F4Pair;
+  constexpr int BN = 256;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);
+  uint64_t* empty = full + S::kStages;
+  uint64_t* scaled = empty + S::kStages;  // a stage's scales are in both CTAs' tensor memory (the first one's barrier)
+  uint64_t* done = scaled + S::kStages;   // a tile's sums are complete
+  uint64_t* taken = done + 1;           // and in registers, of both CTAs (the first one's barrier)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(taken + 1);
+  volatile int* stop = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  uint32_t* rho = reinterpret_cast<uint32_t*>(full) + 64;  // [2][256]: of this tile and of the next
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
+  const int w_tiles = (p.n + kF4Rows - 1) / kF4Rows, tiles_m = (p.rows + BN - 1) / BN, tiles = tiles_m * ((w_tiles + 1) / 2);
+  const int first = blockIdx.x / 2, step = gridDim.x / 2;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1), mbar_init(&scaled[s], 8);
+    mbar_init(done, 1);
+    mbar_init(taken, 16);
+    *stop = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tmem_fence_before();
+  __syncthreads();
+  cluster_barrier();
+  tmem_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_wait();
+  pdl_trigger();
+
+  // columns of a tile: a multiple of 32, as each CTA holds half of them
+  auto tile_cols = [&](int m0) { return (min(BN, p.rows - m0) + 31) / 32 * 32; };
+  if (warp == 0) {
+    // ---- copies, one a lane: the weight record; the CTA's half of the x codes, from up to two records; their scales
+    int s = 0, phase = 1;
+    bool ok = true;
+    for (int t = first; t < tiles && ok; t += step) {
+      const int m0 = t % tiles_m * BN, nt = min(t / tiles_m * 2 + rank, w_tiles - 1);
+      const int half = tile_cols(m0) / 2, records = (2 * half + kF4Rows - 1) / kF4Rows;
+      const int r0 = rank * half, r = (lane - 1) & 1;                                      // this CTA's first x row; record
+      const int a = max(r0 - r * kF4Rows, 0), e = min(r0 + half - r * kF4Rows, kF4Rows);   // its rows of that record
+      const uint8_t* src = p.x + (static_cast<int64_t>(m0 / kF4Rows) + r) * p.chunks * kF4Record;
+      int to = 0;
+      uint32_t size = 0;
+      if (lane == 0) {
+        src = p.w + static_cast<int64_t>(nt) * p.chunks * kF4Record;
+        size = kF4Record;
+      } else if (lane < 3 && a < e) {
+        src += a * 128;
+        to = kF4Record + (r * kF4Rows + a - r0) * 128;
+        size = (e - a) * 128;
+      } else if ((lane == 3 || lane == 4) && r < records) {
+        src += kF4CodeBytes;
+        to = kF4Record + S::kCodes + r * S::kScales;
+        size = S::kScales;
+      }
+      const uint32_t bytes = kF4Record + half * 128 + records * S::kScales;
+      for (int c = 0; c < p.chunks; ++c, src += kF4Record) {
+        ok = __all_sync(~0u, !*stop && f4_wait(&empty[s], phase));
+        if (!ok) break;
+        if (lane == 0) mbar_arrive_expect_tx(&full[s], bytes);
+        __syncwarp();
+        if (size) bulk_load(smem + s * S::kStage + to, src, size, &full[s]);
+        if (++s == S::kStages) s = 0, phase ^= 1;
+      }
+    }
+    if (!ok) {
+      *stop = 1;  // the copies under way land before the CTA leaves
+      for (int i = 0; i < S::kStages; ++i) mbar_wait_for(&full[i], i < s ? phase ^ 1 : phase, 100000000ull);
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      int s = 0, phase = 0, it = 0;
+      bool ok = true;
+      const uint64_t a0 = umma_desc_sw128(smem_u32(smem)), b0 = umma_desc_sw128(smem_u32(smem) + kF4Record);
+      for (int t = first; t < tiles && ok; t += step, ++it) {
+        const uint32_t idesc = umma_idesc_f4(2 * kF4Rows, tile_cols(t % tiles_m * BN));
+        if (*stop || !f4_wait(taken, (it & 1) ^ 1)) break;
+        tmem_fence_after();
+        uint32_t more = 0;
+        for (int c = 0; c < p.chunks; ++c) {
+          ok = f4_wait(&full[s], phase) && f4_wait(&scaled[s], phase);
+          if (!ok) break;
+          tmem_fence_after();
+          const uint32_t sa = tmem + S::kSums + s * S::kScaleCols, sb = sa + 16;
+          const uint64_t a = a0 + s * (S::kStage >> 4), b = b0 + s * (S::kStage >> 4);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            umma_f4<2>(tmem, a + 2 * kk, b + 2 * kk, idesc, sa + 4 * kk, sb + 8 * kk, more);
+            more = 1;
+          }
+          umma_commit_pair(&empty[s]);
+          if (++s == S::kStages) s = 0, phase ^= 1;
+        }
+        if (ok) umma_commit_pair(done);
+      }
+    }
+  } else if (warp >= 10) {
+    // ---- the scales, from shared to tensor memory by way of registers: as copies (tcgen05.cp) they go through the
+    // products' pipe, 48 cycles for 512 bytes, 12 of them a stage whose four products take 512
+    const uint32_t quarter = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    int s = 0, phase = 0;
+    bool ok = true;
+    const uint32_t arrive0 = cluster_map(scaled, 0);
+    for (int t = first; t < tiles && ok; t += step)
+      for (int c = 0; c < p.chunks; ++c) {
+        ok = __all_sync(~0u, !*stop && f4_wait(&full[s], phase));
+        if (!ok) break;
+        const uint8_t* at = smem + s * S::kStage + kF4CodeBytes + lane * 16;
+        const uint32_t to = tmem + quarter + S::kSums + s * S::kScaleCols;
+        uint4 v[4];
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) v[kk] = *reinterpret_cast<const uint4*>(at + 512 * kk);
+        tmem_st16(to, reinterpret_cast<const uint32_t*>(v));
+        at += kF4Record - kF4CodeBytes + S::kCodes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            v[kk] = *reinterpret_cast<const uint4*>(at + (kk & 1) * S::kScales + 512 * (2 * h + (kk >> 1)));
+          tmem_st16(to + 16 + 16 * h, reinterpret_cast<const uint32_t*>(v));
+        }
+        tmem_wait_st();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(arrive0 + 8 * s);
+        if (++s == S::kStages) s = 0, phase ^= 1;
+      }
+  } else {
+    const int q = warp & 3, half = (warp - 2) >> 2, i = threadIdx.x - 64;
+    const uint32_t taken_bar = cluster_map(taken, 0);
+    int it = 0;
+    for (int t = first; t < tiles; t += step, ++it) {
+      const int m0 = t % tiles_m * BN, n = (t / tiles_m * 2 + rank) * kF4Rows + q * 32 + lane, cols = min(BN, p.rows - m0);
+      uint32_t* rx = rho + (it & 1) * BN;
+      const uint32_t mine = i < cols ? p.x_rho[m0 + i] : 127u << 23;
+      rx[i] = mine;
+      const uint32_t rho_w = n < p.n ? p.w_rho[n] : 127u << 23;
+      int plain;
+      asm volatile(
+          "{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.and.pred q, 1, 256, p;\n selp.b32 %0, 1, 0, q;\n}"
+          : "=r"(plain)
+          : "r"(static_cast<int>(f4_plain(mine) && f4_plain(rho_w)))
+          : "memory");
+      const bool ok = !*stop && f4_wait(done, it & 1);  // after a failure the rest is NaN
+      tmem_fence_after();
+      // 128 columns a warp, 32 at a time.  bf16 results are scaled and packed as they are read, fp32 ones take two turns
+      // of 64: the registers of 14 warps hold no more.  The tensor memory is given back after the last read.
+      const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16) + half * (BN / 2);
+      const int left = cols - half * (BN / 2);
+      auto release = [&] {
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(taken_bar);
+      };
+      if (!ok) *stop = 1;
+      const bool store = n < p.n;
+      rx += half * (BN / 2);
+      if constexpr (sizeof(T) == 2) {
+        uint32_t h[BN / 4];
+#pragma unroll
+        for (int c = 0; c < BN / 2; c += 32) {
+          float v[32];
+          tmem_ld32(from + c, v);
+          f4_scale<32>(v, rx + c, rho_w, plain, ok);
+          // residuals are added before the rounding
+          if (p.residual && store)
+            for (int j = 0; j < 32; ++j)
+              if (c + j < left) v[j] += to_f32(static_cast<const T*>(p.residual)[(m0 + half * (BN / 2) + c + j) * p.r_row + n]);
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v[j], v[j + 1]);
+            h[(c + j) / 2] = *reinterpret_cast<const uint32_t*>(&b);
+          }
+        }
+        release();
+        if (store) {
+          __nv_bfloat16* y = static_cast<__nv_bfloat16*>(p.y) + (m0 + half * (BN / 2)) * p.y_row + n;
+          if (left >= BN / 2) {
+#pragma unroll
+            for (int j = 0; j < BN / 2; ++j, y += p.y_row) *y = __ushort_as_bfloat16(static_cast<uint16_t>(h[j / 2] >> (16 * (j & 1))));
+          } else {
+#pragma unroll
+            for (int j = 0; j < BN / 2; ++j, y += p.y_row)
+              if (j < left) *y = __ushort_as_bfloat16(static_cast<uint16_t>(h[j / 2] >> (16 * (j & 1))));
+          }
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < BN / 2; c += 64) {
+          float v[64];
+          tmem_ld32(from + c, v);
+          tmem_ld32(from + c + 32, v + 32);
+          if (c + 64 == BN / 2) release();
+          f4_scale<64>(v, rx + c, rho_w, plain, ok);
+          if (!store) continue;
+          T* y = static_cast<T*>(p.y) + (m0 + half * (BN / 2) + c) * p.y_row + n;
+          const T* r = static_cast<const T*>(p.residual) + (m0 + half * (BN / 2) + c) * p.r_row + n;
+#pragma unroll
+          for (int j = 0; j < 64; ++j, y += p.y_row)
+            if (c + j < left) *y = p.residual ? v[j] + r[j * p.r_row] : v[j];
+        }
+      }
+    }
+  }
+  tmem_fence_before();
+  __syncthreads();
+  cluster_barrier();  // neither CTA leaves while the pair's products or arrivals may touch it
+  if (warp == 1) {
+    tmem_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+template <typename T>
+ssd_status f4_launch_pair(const F4MatmulParams& p, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  if (ssd_status e = op_smem(ssd_f4_matmul_pair_kernel<T>, F4Pair::kSmem, ready, "ssd_f4_matmul")) return e;
+  const int64_t tiles = static_cast<int64_t>((p.n + 255) / 256) * ((p.rows + 255) / 256);
+  if (tiles > 0x3fffffff) return op_fail(SSD_ERR_INVALID_ARG, "ssd_f4_matmul: %d rows of %d", p.rows, p.n);
+  return op_launch_cluster("ssd_f4_matmul", ssd_f4_matmul_pair_kernel<T>, dim3(tiles < 76 ? 2 * static_cast<unsigned>(tiles) : 152u),
+                           kF4PairThreads, F4Pair::kSmem, dim3(2), s, p);
+}
+
 template <int BN, typename T>
 ssd_status f4_launch(const F4MatmulParams& p, int split, cudaStream_t s) {
   static std::atomic<uint64_t> ready{0};
   constexpr int smem = F4Tile<BN>::kSmem;
   if (ssd_status e = op_smem(ssd_f4_matmul_kernel<BN, T>, smem, ready, "ssd_f4_matmul")) return e;
-  const dim3 grid((p.n + kF4Rows - 1) / kF4Rows, (p.rows + BN - 1) / BN, split);
+  const dim3 grid((p.n + kF4Rows - 1) / kF4Rows, 1, split);
   return op_launch_cluster("ssd_f4_matmul", ssd_f4_matmul_kernel<BN, T>, grid, 192, smem, dim3(1, 1, split), s, p);
 }
 
 template <typename T>
 ssd_status f4_dispatch(const F4MatmulParams& p, cudaStream_t s) {
-  const int bn = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : p.rows <= 128 ? 128 : 256;
-  const int64_t tiles = static_cast<int64_t>((p.n + kF4Rows - 1) / kF4Rows) * ((p.rows + bn - 1) / bn);
-  const int64_t slots = 152 * (bn <= 64 ? 2 : 1);
+  if (p.rows > 128) return f4_launch_pair<T>(p, s);
+  const int bn = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
+  const int tiles = (p.n + kF4Rows - 1) / kF4Rows;
+  // A cluster shares a tile's columns as long as that leaves a CTA an SM (1 x 4096 x 4096: one CTA a tile 11.2 us, four
+  // 7.1; with more CTAs than SMs the clusters wait for each other's places: 64 x 11008 x 4096 one 12.8, two 20.5).
   int split = 1;
-  while (split < 8 && tiles * split * 2 <= slots && split * 2 <= p.chunks) split *= 2;
+  while (split < 8 && tiles * split * 2 <= 152 && split * 2 <= p.chunks) split *= 2;
   switch (bn) {
     case 16: return f4_launch<16, T>(p, split, s);
     case 32: return f4_launch<32, T>(p, split, s);
     case 64: return f4_launch<64, T>(p, split, s);
-    case 128: return f4_launch<128, T>(p, split, s);
-    default: return f4_launch<256, T>(p, split, s);
+    default: return f4_launch<128, T>(p, split, s);
   }
 }
 
