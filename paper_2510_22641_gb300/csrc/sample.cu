@@ -8,21 +8,22 @@ namespace {
 
 // ------------------------------------------------------------------ masses
 //
-// The mass of a token is exp((l - top) / T) as an integer with 44 bits after the point, so that sums are exact in any
-// order.  With y = -1024 log2(e) (top - l) / T held as a pair of floats and N = floor(y - 1/16), f = y - N,
-//   2^(y / 1024) = 2^(N >> 10) * 2^((N & 1023) / 1024) * 2^(f / 1024):
-// a table of 1024 values, a polynomial for 2^(f / 1024) - 1 < 2^-10, one multiplication, one shift.
+// The mass of a token is exp((l - top) / T) up to a factor that is the same for the whole row, as an integer with 44 bits
+// after the point, so that sums are exact in any order.  With c = 1024 log2(e) / T as a pair of floats, n = l c rounded to
+// an integer, f = l c - n (by fused multiply-adds, to 2^-25) and a token's place n(top) - n(l),
+//   exp(l / T) 2^(-n(top) / 1024) = 2^-(place >> 10) * 2^(-(place & 1023) / 1024) * 2^(f / 1024):
+// a table of 1024 values, a polynomial, one multiplication, one shift.
 
 constexpr int kExpBits = 10, kExpSize = 1 << kExpBits;
 struct ExpTable {
   uint32_t v[kExpSize];
 };
-// 2^(j / 1024) * 2^31, a little less so that a value times 2^(1.07 / 1024) still fits 32 bits (the common factor
-// cancels).  The Taylor series of e^x, x < ln 2, in 64 bits when this is compiled.
+// 2^(-j / 1024) * 2^32, less so that a value times 2^(1.11 / 1024) still fits 32 bits (the common factor cancels).  The
+// Taylor series of e^x, 0 <= x < ln 2, in 64 bits when this is compiled.
 constexpr ExpTable make_exp_table() {
   ExpTable t = {};
   for (int j = 0; j < kExpSize; ++j) {
-    const double x = 0.693147180559945309417232 * j / kExpSize;
+    const double x = 0.693147180559945309417232 * (kExpSize - j) / kExpSize;
     double sum = 1.0, term = 1.0;
     for (int i = 1; i < 24; ++i) {
       term *= x / i;
@@ -34,31 +35,31 @@ constexpr ExpTable make_exp_table() {
 }
 __device__ constexpr ExpTable kExpTable = make_exp_table();
 
-// Tokens 44 octaves below the largest have none.
-constexpr int kMassPlaces = 44 << kExpBits;
+// Tokens 44 octaves below the largest have no mass.
+constexpr uint32_t kMassPlaces = 44u << kExpBits;
 
 struct MassOf {
-  float half_top, c_hi, c_lo;  // top / 2; the pair -2048 log2(e) / T
+  float origin;      // 0; the largest logit where c times it leaves the integers below 2^22 (then l - origin is exact
+                     // wherever there is mass)
+  float c_hi, c_lo;  // 1024 log2(e) / T
+  uint32_t top;      // bits of the largest logit's `number`
 
-  // ~N, 65536 or more (also of a NaN) where there is no mass.  It does not fall as l falls.
-  __device__ __forceinline__ int place(float l) const {
-    const float t = fmaf(fmaf(-0.5f, l, half_top), c_hi, -0.0625f);
-    return t > -65536.0f ? ~(__float_as_int(__fadd_rd(t, 12582912.0f)) - 0x4B400000) : 65536;
-  }
-  // The mass as a 32-bit number that belongs 12 - (place >> 10) places to the left.
-  __device__ __forceinline__ uint32_t digits(float l, int place, const uint32_t* table) const {
-    const float b = -0.5f * l, d = half_top + b, bb = d - half_top;
-    const float lo = (half_top - (d - bb)) + (b - bb);  // d + lo = (top - l) / 2 exactly
-    const float y = d * c_hi;
-    const float e = fmaf(lo, c_hi, fmaf(d, c_lo, fmaf(d, c_hi, -y)));
-    const float f = (y + static_cast<float>(place + 1)) + e;
-    // 2^32 (2^(f / 1024) - 1) = f a + f^2 a^2 / 2! ..  with a = ln 2 / 1024, times 2^32
-    const float q = fmaf(f, fmaf(f, fmaf(f, 0.2220f, 983.9678f), 2907270.0f), 8388608.0f);
-    const uint32_t t = table[~place & (kExpSize - 1)];
-    return t + __umulhi(t, __float_as_uint(q) - 0x4B000000u);
+  // 1.5 * 2^23 + n as a float; it does not fall as l rises.
+  __device__ __forceinline__ float number(float l) const { return fmaf(l - origin, c_hi, 12582912.0f); }
+  // kMassPlaces or more: no mass (also for -infinity and NaN, whose bits are far away).
+  __device__ __forceinline__ uint32_t place(float l) const { return top - __float_as_uint(number(l)); }
+  // The mass as a 32-bit number that belongs 12 - (place >> 10) places to the left.  Of infinite logits f is a NaN, whose
+  // bits make the same digits for all of them.
+  __device__ __forceinline__ uint32_t digits(float l, uint32_t place, const uint32_t* table) const {
+    const float x = l - origin, n = number(l) - 12582912.0f;
+    const float f = fmaf(x, c_lo, fmaf(x, c_hi, -n));
+    // 2^32 (2^((f + 0.6) / 1024) - 1), the series at f = 0: with a = ln 2 / 1024, 2^32 e^(0.6 a) (1 + a f + a^2 f^2 / 2! ..) - 2^32
+    const float q = fmaf(f, fmaf(f, fmaf(f, 0.22210662f, 984.36748f), 2908451.0f), 8388608.0f + 1744716.25f);
+    const uint32_t t = table[place & (kExpSize - 1)];
+    return t + __umulhi(t, __float_as_uint(q) & 0x7fffffu);
   }
   __device__ __forceinline__ uint64_t operator()(float l, const uint32_t* table) const {
-    const int at = place(l);
+    const uint32_t at = place(l);
     return at < kMassPlaces ? (static_cast<uint64_t>(digits(l, at, table)) << 12) >> (at >> kExpBits) : 0ull;
   }
 };
@@ -66,7 +67,7 @@ struct MassOf {
 __device__ __forceinline__ float key_value(uint32_t key) {  // the inverse of orderable
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
-constexpr uint32_t kKeyNone = 0x007fffffu, kKeyInf = 0xff800000u;  // orderable(-inf), orderable(inf)
+constexpr uint32_t kKeyNone = 0x007fffffu;  // orderable(-infinity)
 
 // floor(a * f) of f in [0, 1), f's digits below 2^-64 cut off; up: the ceiling.  In integers: a 64-bit float operation
 // costs an SM of this GPU 16 cycles a warp.
@@ -94,7 +95,7 @@ struct SampleParams {
 // mass each; the bin in which the rule's count or mass is reached is split by the logits' bits into up to 704 again until
 // one value is left.  All sums are of integers, so neither the atomics' order nor the cut into CTAs matters.
 
-constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kBins = kMassPlaces >> 6, kGroup = kBins / kSampleWarps,
+constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kBins = static_cast<int>(kMassPlaces >> 6), kGroup = kBins / kSampleWarps,
               kSegUnits = 64, kSegs = 256;
 static_assert(kBins % kSampleWarps == 0 && kGroup % 2 == 0 && kGroup <= 64, "a warp adds up a group");
 constexpr int kUses = 10;   // values that CTAs send each other, each at a place of its own
@@ -234,23 +235,22 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     return;
   }
   const bool one = !(temp >= 0x1p-100f) || top_k == 1 || top_p <= 0.0f || min_p > 1.0f;  // the first-ranked token
-  const bool infinite = top_key == kKeyInf;  // only its equals have mass
   MassOf mass;
   {
-    // -2048 log2(e) / T by the remainder of the rounded quotient
-    constexpr double kScale = -2048.0 * 1.4426950408889634074;
+    // 1024 log2(e) / T by the remainder of the rounded quotient
+    constexpr double kScale = 1024.0 * 1.4426950408889634074;
     constexpr float kHigh = static_cast<float>(kScale), kLow = static_cast<float>(kScale - static_cast<double>(kHigh));
     const float t = one ? 1.0f : temp;
-    mass.half_top = 0.5f * top;
     mass.c_hi = kHigh / t;
-    mass.c_lo = isinf(mass.c_hi) ? 0.0f : (fmaf(-mass.c_hi, t, kHigh) + kLow) / t;
+    mass.c_lo = (fmaf(-mass.c_hi, t, kHigh) + kLow) / t;
+    mass.origin = fabsf(top * mass.c_hi) < 2097152.0f || isinf(top) ? 0.0f : top;
+    mass.top = __float_as_uint(mass.number(top));
   }
   // kept: logits above `cut`, and of those equal to it the tokens up to `last`
-  float cut = infinite ? top : -FLT_MAX;
+  float cut = -FLT_MAX;
   int last = vocab - 1;
   auto kept = [&](float l, int index) { return l >= cut && (l != cut || index <= last); };
-  auto place_of = [&](float l) { return !infinite ? mass.place(l) : l == top ? 0 : kMassPlaces; };
-  auto mass_of = [&](float l) -> uint64_t { return infinite ? 1ull << 44 : mass(l, sh.table); };
+  auto mass_of = [&](float l) { return mass(l, sh.table); };
 
   // what min_p leaves: exp(z - max z) >= min_p in masses
   const uint64_t least = min_p >= 1.0f ? mass_of(top) : min_p > 0.0f ? times_fraction(mass_of(top), min_p, true) : 0;
@@ -262,9 +262,9 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     p.token[row] = index;
     if (!p.prob) return;
     // share / all, by a fp32 reciprocal that one step makes exact to 2^-44
-    const int at = place_of(l);
-    const double share = infinite ? 0x1p44 : static_cast<double>(mass.digits(l, at, sh.table)) *
-                                                 __hiloint2double((1023 + 12 - (at >> kExpBits)) << 20, 0);
+    const uint32_t at = mass.place(l);
+    const double share = static_cast<double>(mass.digits(l, at, sh.table)) *
+                         __hiloint2double((1023 + 12 - static_cast<int>(at >> kExpBits)) << 20, 0);
     const double a = static_cast<double>(all), r = static_cast<double>(1.0f / static_cast<float>(all));
     p.prob[row] = static_cast<float>(share * fma(fma(-a, r, 1.0), r, r));
   };
@@ -345,14 +345,15 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   }
 
   // Adds up the cluster's bins of this step, finds the one in which the running measure reaches goal_of(all of it) (1 or
-  // more; 0: none) and returns the goal.  Every CTA gets the others' sums over groups of bins, and reads one group.
+  // more; 0: none) and returns the goal.  masses: bin b holds digits, which belong 12 - (b >> 4) places to the left.  Every CTA gets the others' sums over groups of bins, and reads one group.
   int step = 0;
-  auto find_bin = [&](auto goal_of) -> uint64_t {
+  auto find_bin = [&](bool masses, auto goal_of) -> uint64_t {
     const int b = step & 1;
+    auto value_of = [&](uint64_t v, int bin) { return masses ? v << 12 >> (bin >> 4) : v; };
     __syncthreads();
     {
-      uint64_t v = lane < kGroup ? sh.bin[b][warp * kGroup + lane] : 0;
-      if (lane + 32 < kGroup) v += sh.bin[b][warp * kGroup + lane + 32];
+      uint64_t v = lane < kGroup ? value_of(sh.bin[b][warp * kGroup + lane], warp * kGroup + lane) : 0;
+      if (lane + 32 < kGroup) v += value_of(sh.bin[b][warp * kGroup + lane + 32], warp * kGroup + lane + 32);
       v = warp_sum(v);
       if (lane < ctas) cluster_store(&sh.groups[b][rank][warp], lane, v);
     }
@@ -376,7 +377,8 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
         if (r < ctas && lane < kGroup / 2) cluster_load2(&sh.bin[b][group * kGroup + 2 * lane], r, x[r], y[r]);
       }
 #pragma unroll
-      for (int r = 0; r < 8; ++r) v += x[r], w += y[r];
+      for (int r = 0; r < 8; ++r)
+        v += value_of(x[r], group * kGroup + 2 * lane), w += value_of(y[r], group * kGroup + 2 * lane + 1);
       const uint64_t before = base + warp_scan(v + w) - v - w;
       if (before < goal && goal <= before + v + w) {
         const bool in_w = goal > before + v;
@@ -389,17 +391,15 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     ++step;
     return goal;
   };
-  auto measure = [&](float l, bool counting) { return counting ? 1ull : mass_of(l); };
   // logits that a bin can hold, with two places more at either end than it has (and what rounding takes)
   const float unit = temp * 6.7690154e-4f;  // of a place: T ln(2) / 1024
   auto low_of = [&](int bin) {
-    return infinite ? top : fmaxf(__fsub_rd(top, __fmul_ru(unit, 64.0f * bin + 66.1f)), -FLT_MAX);
+    return isinf(top) ? top : fmaxf(__fsub_rd(top, __fmul_ru(unit, 64.0f * bin + 66.1f)), -FLT_MAX);
   };
-  auto high_of = [&](int bin) { return infinite ? top : fminf(__fsub_ru(top, __fmul_rd(unit, 64.0f * bin - 2.1f)), top); };
-  auto add_to = [&](int bin, uint64_t v) {  // in halves: a 64-bit atomic on shared memory is a loop
+  auto high_of = [&](int bin) { return isinf(top) ? top : fminf(__fsub_ru(top, __fmul_rd(unit, 64.0f * bin - 2.1f)), top); };
+  auto add_to = [&](int bin, uint32_t v) {  // by halves: a 64-bit atomic on shared memory is a loop
     uint32_t* at = reinterpret_cast<uint32_t*>(&sh.bin[step & 1][bin]);
-    const uint32_t low = static_cast<uint32_t>(v), high = static_cast<uint32_t>(v >> 32) + (atomicAdd(at, low) > ~low);
-    if (high) atomicAdd(at + 1, high);
+    if (atomicAdd(at, v) > ~v) atomicAdd(at + 1, 1u);
   };
   auto count_in = [&](int bin) { atomicAdd(reinterpret_cast<uint32_t*>(&sh.bin[step & 1][bin]), 1u); };
 
@@ -468,20 +468,23 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float l = to_f32(x.v[e]);
-        const int at = !limited || kept(l, first_index + u * E + e) ? place_of(l) : kMassPlaces;
-        if (at >= kMassPlaces) continue;
+        const uint32_t at = mass.place(l);
+        if (at >= kMassPlaces || (limited && !kept(l, first_index + u * E + e))) continue;
         if (counting)
           count_in(at >> 6);
         else
-          add_to(at >> 6, mass_of(l));
+          add_to(at >> 6, mass.digits(l, at, sh.table));
       }
     }
-    uint64_t goal = find_bin(goal_of);
+    uint64_t goal = find_bin(!counting, goal_of);
     if (goal == 0) return;
     goal -= sh.before;
     const int bin = sh.border;
+    // within the bin masses are their digits, which all belong equally far to the left
+    if (!counting) goal = ((goal << (bin >> 4)) + 4095) >> 12;
+    auto measure = [&](float l) -> uint64_t { return counting ? 1u : mass.digits(l, mass.place(l), sh.table); };
     const float low = low_of(bin), high = high_of(bin);
-    auto in_bin = [&](float l, int index) { return place_of(l) >> 6 == bin && kept(l, index); };
+    auto in_bin = [&](float l, int index) { return mass.place(l) >> 6 == static_cast<uint32_t>(bin) && kept(l, index); };
     limited = true;
     // fp32 logits in a bin are few and all different; bf16 ones are many equals of two or three values
     const int n = KS == 0 ? collect(low, high, in_bin) : -1;
@@ -490,7 +493,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
       int better, earlier;
       const uint64_t mine = rank_list(n, each, better, earlier);
       if (tid / each < n && (tid & (each - 1)) == 0) {
-        sh.by_rank[better] = measure(key_value(static_cast<uint32_t>(mine >> 32)), counting);
+        sh.by_rank[better] = measure(key_value(static_cast<uint32_t>(mine >> 32)));
         sh.sorted[better] = mine;
       }
       __syncthreads();
@@ -517,10 +520,10 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
           if (!(l >= low && l <= high)) continue;
           const uint32_t key = orderable(l + 0.0f) >> KS;
           if (key >= kmin && key <= kmax && in_bin(l, first_index + u * E + e))
-            add_to((kmax - key) >> shift, measure(l, counting));
+            add_to((kmax - key) >> shift, static_cast<uint32_t>(measure(l)));
         }
       }
-      find_bin([&](uint64_t) { return goal; });
+      find_bin(false, [&](uint64_t) { return goal; });
       goal -= sh.before;
       kmax -= static_cast<uint32_t>(sh.border) << shift;
       kmin = max(kmin, kmax - ((1u << shift) - 1));
@@ -528,7 +531,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     }
     // kmax is the border's key; its equals fall by index
     const float value = key_value(kmax & (0x80000000u >> KS) ? kmax << KS : kmax << KS | ((1u << KS) - 1));
-    const uint64_t m = measure(value, counting), wanted = (goal + m - 1) / m;
+    const uint64_t m = measure(value), wanted = (goal + m - 1) / m;
     int end = value == cut ? last : vocab - 1;
     if (wanted * m < sh.at) {
       walk([&](float l, int) -> uint64_t { return l == value; }, [&](uint64_t) { return wanted - 1; },
@@ -547,9 +550,9 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     // At least top_k tokens are in or above the bin that the top_k-th of the threads' largest is in; usually few more.
     // The first CTA ranks them, applies the rules to the sorted masses and draws.
     if (top_k <= kList / 2) {
-      const int place = place_of(most_of_thread);
+      const uint32_t place = mass.place(most_of_thread);
       if (place < kMassPlaces) count_in(place >> 6);
-      const uint64_t found = find_bin([&](uint64_t all) -> uint64_t { return all >= static_cast<uint64_t>(top_k) ? top_k : 0; });
+      const uint64_t found = find_bin(false, [&](uint64_t all) -> uint64_t { return all >= static_cast<uint64_t>(top_k) ? top_k : 0; });
       const int n = found ? collect(low_of(sh.border), top, [](float, int) { return true; }) : -1;
       if (n >= 0) {
         cluster_sync();
