@@ -60,7 +60,8 @@ struct MassOf {
   }
   __device__ __forceinline__ uint64_t operator()(float l, const uint32_t* table) const {
     const uint32_t at = place(l);
-    return at < kMassPlaces ? (static_cast<uint64_t>(digits(l, at, table)) << 12) >> (at >> kExpBits) : 0ull;
+    const uint64_t v = static_cast<uint64_t>(digits(l, at, table)) << 12 >> (at >> kExpBits & 63);
+    return at < kMassPlaces ? v : 0ull;
   }
 };
 
@@ -99,6 +100,7 @@ constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kBins = 
               kSegUnits = 64, kSegs = 256;
 static_assert(kBins % kSampleWarps == 0 && kGroup % 2 == 0 && kGroup <= 64, "a warp adds up a group");
 constexpr int kUses = 10;   // values that CTAs send each other, each at a place of its own
+constexpr int kPieces = 4;  // copies of a CTA's part of the row
 constexpr int kList = 512;  // tokens that one CTA ranks by comparing all with all
 
 struct SampleShared {
@@ -110,9 +112,10 @@ struct SampleShared {
   uint64_t sent[kUses][8];                   // written by the CTA of that rank
   uint64_t list[kList];                      // key and inverted index of tokens that are ranked one by one
   uint64_t all[kList + 2];                   // the cluster's lists as one
-  uint64_t by_rank[kList], by_index[kList], sorted[kList];
+  uint64_t by_rank[kList], sorted[kList];
   uint64_t before, at;
-  int border, listed, first, kept;
+  uint64_t arrived[kPieces];                 // barriers of the row's pieces
+  int border, listed, first, kept, failed;
 };
 
 __device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
@@ -167,9 +170,6 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int ctas = gridDim.x, rank = blockIdx.x, row = blockIdx.y, vocab = p.vocab;
   cluster_arrive();
-  for (int i = tid; i < kExpSize; i += kSampleThreads) sh.table[i] = kExpTable.v[i];
-  for (int i = tid; i < 2 * kBins; i += kSampleThreads) sh.bin[0][i] = 0;
-  if (tid == 0) sh.first = vocab;
   pdl_wait();
   pdl_trigger();
 
@@ -179,32 +179,35 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   const T* const src = static_cast<const T*>(p.logits) + row * p.row_stride + v0;
   const int phase = static_cast<int>(reinterpret_cast<uintptr_t>(src) / sizeof(T) % E);
   const int units = v1 > v0 ? (phase + v1 - v0 + E - 1) / E : 0, first_index = v0 - phase;
-  float most = -INFINITY;
-  auto take = [&](int u, const Logits16<T>& x) {
-    data[u] = x;
-#pragma unroll
-    for (int e = 0; e < E; ++e) most = fmaxf(most, to_f32(x.v[e]));
-  };
-  {
+  // the units inside the row are copied in kPieces, and looked at as they arrive
+  const int piece = (units + kPieces * kSampleThreads - 1) / (kPieces * kSampleThreads) * kSampleThreads;
+  if (tid == 0) {
+    for (int i = 0; i < kPieces; ++i) mbar_init(&sh.arrived[i], 1);
+    sh.failed = 0;
+    fence_mbar_init();
     const uint4* in = reinterpret_cast<const uint4*>(src - phase);
-    constexpr int kAhead = 4;
-    for (int u = tid; u < units; u += kAhead * kSampleThreads) {
-      Logits16<T> x[kAhead];
+    for (int i = 0; i < kPieces; ++i) {
+      const int u0 = max(i * piece, 1), u1 = min((i + 1) * piece, units - 1);
+      mbar_arrive_expect_tx(&sh.arrived[i], u0 < u1 ? (u1 - u0) * 16 : 0);
+      if (u0 < u1) bulk_load(data + u0, in + u0, (u1 - u0) * 16, &sh.arrived[i]);
+    }
+  }
+  if (warp == 1 && lane < 2 * E) {  // the first and the last unit
+    const int u = lane < E ? 0 : units - 1, i = u * E + lane % E - phase;
+    if (u >= 0) data[u].v[lane % E] = i >= 0 && i < v1 - v0 ? src[i] : from_f32<T>(-INFINITY);
+  }
+  for (int i = tid; i < kExpSize; i += kSampleThreads) sh.table[i] = kExpTable.v[i];
+  for (int i = tid; i < 2 * kBins; i += kSampleThreads) sh.bin[0][i] = 0;
+  if (tid == 0) sh.first = vocab;
+  __syncthreads();
+  float most = -INFINITY;
+  for (int i = 0; i < kPieces; ++i) {
+    if (!mbar_wait(&sh.arrived[i], 0)) sh.failed = 1;
+#pragma unroll 2
+    for (int u = i * piece + tid; u < min((i + 1) * piece, units); u += kSampleThreads) {
+      const Logits16<T> x = data[u];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int v = u + i * kSampleThreads;
-        if (v > 0 && v < units - 1) x[i].w = in[v];
-      }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int v = u + i * kSampleThreads;
-        if (v == 0 || v == units - 1)
-          for (int e = 0; e < E; ++e) {
-            const int j = v * E + e - phase;
-            x[i].v[e] = j >= 0 && j < v1 - v0 ? src[j] : from_f32<T>(-INFINITY);
-          }
-        if (v < units) take(v, x[i]);
-      }
+      for (int e = 0; e < E; ++e) most = fmaxf(most, to_f32(x.v[e]));
     }
   }
   const float most_of_thread = most;
@@ -215,11 +218,15 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   __syncthreads();
   if (tid < ctas) {
     for (int i = 0; i < kSampleWarps; ++i) most = fmaxf(most, __uint_as_float(static_cast<uint32_t>(sh.part[0][i])));
-    cluster_store(&sh.sent[0][rank], tid, __float_as_uint(most));
+    cluster_store(&sh.sent[0][rank], tid, static_cast<uint64_t>(sh.failed) << 32 | __float_as_uint(most));
   }
   cluster_sync();
   float top = -INFINITY;
-  for (int i = 0; i < ctas; ++i) top = fmaxf(top, __uint_as_float(static_cast<uint32_t>(sh.sent[0][i])));
+  bool failed = false;
+  for (int i = 0; i < ctas; ++i) {
+    top = fmaxf(top, __uint_as_float(static_cast<uint32_t>(sh.sent[0][i])));
+    failed |= sh.sent[0][i] >> 32 != 0;
+  }
   const uint32_t top_key = orderable(top + 0.0f);
 
   const ssd_sampling& h = p.how;
@@ -227,11 +234,13 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   const float top_p = h.top_p_rows ? h.top_p_rows[row] : h.top_p;
   const float min_p = h.min_p_rows ? h.min_p_rows[row] : h.min_p;
   const int top_k = h.top_k_rows ? h.top_k_rows[row] : h.top_k;
-  if (top_key <= kKeyNone) {
+  if (top_key <= kKeyNone || failed) {
     if (rank == 0 && tid == 0) {
       p.token[row] = -1;
-      if (p.prob) p.prob[row] = 0.0f;
+      if (p.prob) p.prob[row] = failed ? NAN : 0.0f;
     }
+    if (failed)  // the copies under way land before the CTA leaves
+      for (int i = 0; i < kPieces; ++i) mbar_wait_for(&sh.arrived[i], 0, 100000000ull);
     return;
   }
   const bool one = !(temp >= 0x1p-100f) || top_k == 1 || top_p <= 0.0f || min_p > 1.0f;  // the first-ranked token
@@ -283,8 +292,8 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     return v;
   };
 
-  // The first token in vocabulary order whose running measure exceeds aim(all of it): calls found(index, logit, all) in
-  // one thread of the cluster.
+  // The first token in vocabulary order whose running measure (0 of logits below `cut`) exceeds aim(all of it): calls
+  // found(index, logit, all) in one thread of the cluster.
   int uses = 1;
   constexpr int kSeg = kSegUnits * E;
   static_assert(kSeg <= kSampleThreads, "a segment's tokens are looked at by a thread each");
@@ -295,6 +304,10 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
 #pragma unroll 1
       for (int u = s * kSegUnits + lane; u < min((s + 1) * kSegUnits, units); u += 32) {
         const Logits16<T> x = data[u];
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < E; ++e) any |= to_f32(x.v[e]) >= cut;
+        if (!any) continue;
 #pragma unroll
         for (int e = 0; e < E; ++e) sum += measure(to_f32(x.v[e]), first_index + u * E + e);
       }
@@ -397,11 +410,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     return isinf(top) ? top : fmaxf(__fsub_rd(top, __fmul_ru(unit, 64.0f * bin + 66.1f)), -FLT_MAX);
   };
   auto high_of = [&](int bin) { return isinf(top) ? top : fminf(__fsub_ru(top, __fmul_rd(unit, 64.0f * bin - 2.1f)), top); };
-  auto add_to = [&](int bin, uint32_t v) {  // by halves: a 64-bit atomic on shared memory is a loop
-    uint32_t* at = reinterpret_cast<uint32_t*>(&sh.bin[step & 1][bin]);
-    if (atomicAdd(at, v) > ~v) atomicAdd(at + 1, 1u);
-  };
-  auto count_in = [&](int bin) { atomicAdd(reinterpret_cast<uint32_t*>(&sh.bin[step & 1][bin]), 1u); };
+  auto low_half = [&](int bin) { return reinterpret_cast<uint32_t*>(&sh.bin[step & 1][bin]); };
 
   // Lists the cluster's wanted tokens of logits in [low, high] in sh.all of every CTA, if they are kList at most, and
   // returns how many there are, or -1.
@@ -465,16 +474,22 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   auto shrink = [&](bool counting, auto goal_of) {
     for (int u = tid; u < units; u += kSampleThreads) {
       const Logits16<T> x = data[u];
+      uint32_t v[E], old[E], place[E];
+      bool on[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float l = to_f32(x.v[e]);
-        const uint32_t at = mass.place(l);
-        if (at >= kMassPlaces || (limited && !kept(l, first_index + u * E + e))) continue;
-        if (counting)
-          count_in(at >> 6);
-        else
-          add_to(at >> 6, mass.digits(l, at, sh.table));
+        place[e] = mass.place(l);
+        on[e] = place[e] < kMassPlaces && (!limited || kept(l, first_index + u * E + e));
+        v[e] = 1;
+        if (!counting) v[e] = mass.digits(l, place[e], sh.table);
       }
+      // low halves, and then what they carry: a 64-bit atomic on shared memory is a loop
+#pragma unroll
+      for (int e = 0; e < E; ++e) old[e] = on[e] ? atomicAdd(low_half(place[e] >> 6), v[e]) : 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (on[e] && old[e] > ~v[e]) atomicAdd(low_half(place[e] >> 6) + 1, 1u);
     }
     uint64_t goal = find_bin(!counting, goal_of);
     if (goal == 0) return;
@@ -520,7 +535,11 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
           if (!(l >= low && l <= high)) continue;
           const uint32_t key = orderable(l + 0.0f) >> KS;
           if (key >= kmin && key <= kmax && in_bin(l, first_index + u * E + e))
-            add_to((kmax - key) >> shift, static_cast<uint32_t>(measure(l)));
+          {
+            const uint32_t v = static_cast<uint32_t>(measure(l));
+            uint32_t* const at = low_half((kmax - key) >> shift);
+            if (atomicAdd(at, v) > ~v) atomicAdd(at + 1, 1u);
+          }
         }
       }
       find_bin(false, [&](uint64_t) { return goal; });
@@ -551,7 +570,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     // The first CTA ranks them, applies the rules to the sorted masses and draws.
     if (top_k <= kList / 2) {
       const uint32_t place = mass.place(most_of_thread);
-      if (place < kMassPlaces) count_in(place >> 6);
+      if (place < kMassPlaces) atomicAdd(low_half(place >> 6), 1u);
       const uint64_t found = find_bin(false, [&](uint64_t all) -> uint64_t { return all >= static_cast<uint64_t>(top_k) ? top_k : 0; });
       const int n = found ? collect(low_of(sh.border), top, [](float, int) { return true; }) : -1;
       if (n >= 0) {
@@ -575,11 +594,11 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
           keep = sh.kept;
         }
         if (lead) {
-          sh.by_index[earlier] = better < keep && w >= least ? w : 0;
+          sh.list[earlier] = better < keep && w >= least ? w : 0;
           sh.sorted[earlier] = mine;
         }
         __syncthreads();
-        v = tid < n ? sh.by_index[tid] : 0;
+        v = tid < n ? sh.list[tid] : 0;
         run = scan(v, 1, all);
         const uint64_t goal = aim(all);
         if (run - v <= goal && goal < run)
@@ -593,9 +612,8 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     shrink(false, [&](uint64_t all) -> uint64_t { return max(times_fraction(all, top_p, true), static_cast<uint64_t>(1)); });
   walk(
       [&](float l, int index) -> uint64_t {
-        if (!kept(l, index)) return 0;
         const uint64_t m = mass_of(l);
-        return m >= least ? m : 0;
+        return kept(l, index) && m >= least ? m : 0;
       },
       aim, put);
 }
@@ -609,7 +627,7 @@ ssd_status sample_launch(const SampleParams& p, int rows, cudaStream_t s) {
   // CTAs an SM
   int ctas = 1;
   while (ctas < 8 && ((static_cast<int64_t>(rows) * ctas < 152 && p.vocab / ctas > 4096) ||
-                      static_cast<int64_t>(p.vocab) * sizeof(T) / ctas > (88 << 10)))
+                      static_cast<int64_t>(p.vocab) * sizeof(T) / ctas > (113 << 10) - kHead))
     ctas *= 2;
   const int per = (p.vocab + ctas - 1) / ctas, bytes = per * static_cast<int>(sizeof(T)) + 32;
   for (int first = 0; first < rows; first += 65535) {  // what a grid's second dimension takes
