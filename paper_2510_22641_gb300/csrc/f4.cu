@@ -69,27 +69,52 @@ __device__ __forceinline__ int f4_row_exponent(uint32_t amax) {
   return max(static_cast<int>(amax >> 23) - 127 - 11 + ((amax & 0x7fffffu) > 0x280000u ? 1 : 0), -100);
 }
 
-// One row's 16-column group, half of it (8 columns) in this lane and half in lane ^ 1, times the row's down = 2^-e: the
-// scale's byte and the 8 codes.  A quotient is fma(y, h, y * l) of its divisor's reciprocal h + l, exact to 2^-47, and
-// so correctly rounded: numerators have 24 bits and divisors (6, s) at most 4, so no quotient lies nearer than 2^-30 to
-// the middle of two fp32 numbers.
+// Four pairs to a word of codes, to nearest even, at most 6.
+__device__ __forceinline__ uint32_t to_e2m1(const float2* q) {
+  uint32_t w;
+  asm("{\n .reg .b8 a, b, c, d;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}"
+      : "=r"(w)
+      : "f"(q[0].x), "f"(q[0].y), "f"(q[1].x), "f"(q[1].y), "f"(q[2].x), "f"(q[2].y), "f"(q[3].x), "f"(q[3].y));
+  return w;
+}
+__device__ __forceinline__ float approx_reciprocal(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// One row's 16-column group, half of it (8 columns, largest magnitude `bits`) in this lane and half in lane ^ 1, times the
+// row's down = 2^-e: the scale's byte and the 8 codes.  A quotient is fma(y, h, y * l) of its divisor's reciprocal h + l,
+// exact to 2^-45, and so correctly rounded: numerators have 24 bits and divisors (6, s) at most 4, so no quotient lies
+// nearer than 2^-30 to the middle of two fp32 numbers.
 template <typename T>
-__device__ __forceinline__ void f4_encode(const Raw8<T>& x, float down, uint32_t& scale, uint32_t& codes) {
-  uint32_t bits = x.amax();
+__device__ __forceinline__ void f4_encode(const Raw8<T>& x, uint32_t bits, float down, uint32_t& scale, uint32_t& codes) {
   bits = max(bits, __shfl_xor_sync(~0u, bits, 1));
   constexpr float kSixth = 1.0f / 6.0f, kSixthLow = static_cast<float>(1.0 / 6.0 - static_cast<double>(kSixth));
   const float m = __uint_as_float(bits) * down;
   scale = __nv_cvt_float_to_fp8(fmaf(m, kSixth, m * kSixthLow), __NV_SATFINITE, __NV_E4M3);
-  const float s = e4m3_value(scale), h = scale ? __frcp_rn(s) : 0.0f, l = fmaf(-s, h, 1.0f) * h;
-  codes = 0;
+  const float s = e4m3_value(scale);
+  float h = approx_reciprocal(s), l = fmaf(-s, h, 1.0f) * h;
+  if (scale == 0) h = l = 0.0f;
+  float2 q[4];
+  // the row's power of two goes into the reciprocal, but where that would push its low part out of range
+  if (down >= 0x1p-70f) {
+    h *= down, l *= down;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float2 y = x.pair(i);
-    y.x *= down, y.y *= down;
-    y.x = fmaf(y.x, h, y.x * l);
-    y.y = fmaf(y.y, h, y.y * l);
-    codes |= static_cast<uint32_t>(__nv_cvt_float2_to_fp4x2(y, __NV_E2M1, cudaRoundNearest)) << (8 * i);
+    for (int i = 0; i < 4; ++i) {
+      const float2 y = x.pair(i);
+      q[i] = make_float2(fmaf(y.x, h, y.x * l), fmaf(y.y, h, y.y * l));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 y = make_float2(x.pair(i).x * down, x.pair(i).y * down);
+      q[i] = make_float2(fmaf(y.x, h, y.x * l), fmaf(y.y, h, y.y * l));
+    }
   }
+  codes = to_e2m1(q);
 }
 
 struct F4Row {  // what a row's largest magnitude says
@@ -106,10 +131,10 @@ struct F4Row {  // what a row's largest magnitude says
 
 // Writes 8 columns' codes, and a group's scale as one of four in a word.
 template <typename T>
-__device__ __forceinline__ void f4_put(const Raw8<T>& x, const F4Row& f, uint8_t* at, int r) {
+__device__ __forceinline__ void f4_put(const Raw8<T>& x, uint32_t bits, const F4Row& f, uint8_t* at, int r) {
   const int lane = threadIdx.x & 31;
   uint32_t scale, codes;
-  f4_encode(x, f.down, scale, codes);
+  f4_encode(x, bits, f.down, scale, codes);
   if (f.bad) scale = codes = 0;
   *reinterpret_cast<uint32_t*>(at + f4_code_byte(r, lane * 8)) = codes;
   scale <<= 8 * (lane >> 1 & 3);
@@ -130,13 +155,13 @@ __global__ void __launch_bounds__(256) ssd_f4_pack_kernel(const F4PackParams p) 
   const bool on = row < p.rows;
   const T* src = static_cast<const T*>(p.x) + (on ? row : 0) * p.x_row;
   Raw8<T> x[J];
-  uint32_t amax = 0;
+  uint32_t amax = 0, most[J];
 #pragma unroll
   for (int j = 0; j < J; ++j)
     if (c0 + j * p.warps < p.chunks) x[j].template load<VEC>(src, (c0 + j * p.warps) * kF4Cols + lane * 8, p.k);
 #pragma unroll
   for (int j = 0; j < J; ++j)
-    if (c0 + j * p.warps < p.chunks) amax = max(amax, x[j].amax());
+    if (c0 + j * p.warps < p.chunks) amax = max(amax, most[j] = x[j].amax());
   amax = __reduce_max_sync(~0u, amax);
   if (p.warps > 1) {
     if (lane == 0) part[warp] = amax;
@@ -150,7 +175,7 @@ __global__ void __launch_bounds__(256) ssd_f4_pack_kernel(const F4PackParams p) 
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const int c = c0 + j * p.warps;
-    if (c < p.chunks) f4_put(x[j], f, rec + static_cast<int64_t>(c) * kF4Record, row % kF4Rows);
+    if (c < p.chunks) f4_put(x[j], most[j], f, rec + static_cast<int64_t>(c) * kF4Record, row % kF4Rows);
   }
 }
 
@@ -177,48 +202,65 @@ __global__ void __launch_bounds__(256) ssd_f4_pack_long_kernel(const F4PackParam
   uint8_t* rec = p.out + static_cast<int64_t>(row / kF4Rows) * p.chunks * kF4Record;
   for (int c = warp; c < p.chunks; c += 8) {
     x.template load<VEC>(src, c * kF4Cols + lane * 8, p.k);
-    f4_put(x, f, rec + static_cast<int64_t>(c) * kF4Record, row % kF4Rows);
+    f4_put(x, x.amax(), f, rec + static_cast<int64_t>(c) * kF4Record, row % kF4Rows);
   }
 }
 
-// A CTA per record: 8 columns of a row a lane.  Products of code and scale have 6 bits and are exact in fp16.
+// A CTA per record: a warp takes four rows at a time, of each 4 columns a lane and the 4 that are 128 further, so that
+// neighbouring lanes store neighbouring bytes.  Products of code and scale have 6 bits and are exact in fp16.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) ssd_f4_unpack_kernel(const uint8_t* packed, int rows, int k, int chunks,
                                                             const float* rho, T* out) {
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31, chunk = blockIdx.x, tile = blockIdx.y, col = chunk * kF4Cols + lane * 8;
+  const int lane = threadIdx.x & 31, chunk = blockIdx.x, tile = blockIdx.y, col = chunk * kF4Cols + lane * 4;
   const uint8_t* at = packed + (static_cast<int64_t>(tile) * chunks + chunk) * kF4Record;
   const int end = min(rows - tile * kF4Rows, kF4Rows);
-  if (col >= k) return;
-#pragma unroll 4
-  for (int r = threadIdx.x >> 5; r < end; r += 8) {
-    const int64_t row = static_cast<int64_t>(tile) * kF4Rows + r;
-    const uint32_t codes = *reinterpret_cast<const uint32_t*>(at + f4_code_byte(r, lane * 8));
-    const __half2 s = __half2half2(
-        __half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(at[f4_scale_byte(r, lane * 8)]), __NV_E4M3)));
-    const float f = rho[row];
-    float v[8];
+  rho += static_cast<int64_t>(tile) * kF4Rows;
+  out += static_cast<int64_t>(tile) * kF4Rows * k + col;
+  for (int r0 = threadIdx.x >> 5; r0 < end; r0 += 32) {
+    uint32_t codes[4][2], scale[4][2];
+    float f[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const __half2 c(__nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(codes >> (8 * i)), __NV_E2M1));
-      const float2 t = __half22float2(__hmul2(c, s));
-      v[2 * i] = t.x * f, v[2 * i + 1] = t.y * f;
-    }
-    T* y = out + row * k + col;
-    if (VEC && col + 8 <= k) {
-      if constexpr (sizeof(T) == 4) {
-        reinterpret_cast<float4*>(y)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(y)[1] = make_float4(v[4], v[5], v[6], v[7]);
-      } else {
-        __nv_bfloat162 h[4];
-        for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<uint4*>(y) = *reinterpret_cast<const uint4*>(h);
-      }
-    } else {
+      const int r = r0 + 8 * i;
+      if (r >= end) break;
+      f[i] = rho[r];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (col + i < k) y[i] = from_f32<T>(v[i]);
+      for (int h = 0; h < 2; ++h) {
+        codes[i][h] = *reinterpret_cast<const uint16_t*>(at + f4_code_byte(r, lane * 4 + 128 * h));
+        scale[i][h] = at[f4_scale_byte(r, lane * 4 + 128 * h)];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + 8 * i;
+      if (r >= end) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const __half2 s = __half2half2(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(scale[i][h]), __NV_E4M3)));
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const __half2 c(__nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(codes[i][h] >> (8 * j)), __NV_E2M1));
+          const float2 t = __half22float2(__hmul2(c, s));
+          v[2 * j] = t.x * f[i], v[2 * j + 1] = t.y * f[i];
+        }
+        T* y = out + static_cast<int64_t>(r) * k + 128 * h;
+        const int left = k - col - 128 * h;
+        if (VEC && left >= 4) {
+          if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
+          } else {
+            const __nv_bfloat162 b[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
+            *reinterpret_cast<uint2*>(y) = *reinterpret_cast<const uint2*>(b);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (j < left) y[j] = from_f32<T>(v[j]);
+        }
+      }
     }
   }
 }
@@ -239,7 +281,7 @@ template <typename T>
 ssd_status f4_unpack_dispatch(const uint8_t* in, int rows, int k, T* out, cudaStream_t s) {
   const int chunks = f4_chunks(k);
   const float* rho = reinterpret_cast<const float*>(in + f4_scales_at(rows, k));
-  const bool vec = reinterpret_cast<uintptr_t>(out) % 16 == 0 && k % (16 / sizeof(T)) == 0;
+  const bool vec = reinterpret_cast<uintptr_t>(out) % (4 * sizeof(T)) == 0 && k % 4 == 0;
   for (int first = 0; first < rows; first += 65535 * kF4Rows) {  // what a grid's second dimension takes
     const int n = rows - first < 65535 * kF4Rows ? rows - first : 65535 * kF4Rows;
     const dim3 grid(chunks, (n + kF4Rows - 1) / kF4Rows);
