@@ -25,15 +25,15 @@ def set_fault_injection(kind: int, countdown: int) -> None:
 def __getattr__(name):
     # torch is only needed for the wrappers; the ABI loader works without it.
     if name in ("SSDModel", "bf16_bits_to_device", "encdec_device_weights"):
-        from . import model
-        return getattr(model, name)
-    if name in ("KV8Cache", "KV8Step", "W4Weight", "F4Rows", "F4Weight"):
-        from . import lowbit
-        return getattr(lowbit, name)
-    if name in ("Rotary", "sample"):
-        from . import heads
-        return getattr(heads, name)
-    raise AttributeError(name)
+        from . import model as module
+    elif name in ("KV8Cache", "KV8Step", "W4Weight", "F4Rows", "F4Weight"):
+        from . import lowbit as module
+    elif name in ("Rotary", "sample"):
+        from . import heads as module
+    else:
+        raise AttributeError(name)
+    value = globals()[name] = getattr(module, name)   # the next access finds it there
+    return value
 
 
 def config_dict(shape, draft_exit_k: int, in_kind: int, in_hidden: int, gamma_max: int, max_seq: int,

@@ -15,6 +15,9 @@ from . import _binding as B
 from .lowbit import _call, _fail, _rows2, _rows3, _type
 
 
+_Heads = B.SSDHeads * 2
+
+
 class Rotary:
     """Rotary positions of heads of `head_dim` elements (ssd_rotary): the first `rotary_dim` turn, in pairs
     (i, i + rotary_dim / 2) or, interleaved, (2 i, 2 i + 1), by theta^(-2 i / rotary_dim) radians a position.
@@ -59,40 +62,46 @@ class Rotary:
         """ssd_rotary_apply: the heads of q [rows][heads][head_dim] and k [rows][kv heads][head_dim] (or None),
         normed where a gain [head_dim] is given, turned by pos int32 [rows] or [rows][axes].  Returns (q_out, k_out),
         which may be q and k themselves."""
-        i, rows, d = q.get_device(), q.shape[0], self.head_dim
-        if not q.is_cuda:
+        i, d, code = q.get_device(), self.head_dim, _type(q.dtype, "q")
+        rows = q.shape[0] if q.dim() else 0
+        if i < 0:
             _fail(f"q: a CUDA tensor expected, got {q.device}")
-        if pos.dtype is not torch.int32 or pos.get_device() != i or pos.shape != ((rows, self.axes) if pos.dim() != 1 else (rows,)) \
-                or (pos.dim() == 1 and self.axes != 1):
-            _fail(f"pos: int32 [{rows}][{self.axes}] on {q.device} expected, got {pos.dtype} {tuple(pos.shape)} on {pos.device}")
-        code, dtype = _type(q.dtype, "q"), q.dtype
-        both = (B.SSDHeads * 2)()
-        outs = []
-        for h, x, y, gain, what in ((both[0], q, q_out, q_gain, "q"), (both[1], k, k_out, k_gain, "k")):
-            if x is None:
-                if y is not None or gain is not None:
-                    _fail(f"{what}: missing")
-                outs.append(None)
-                continue
-            if x.dim() != 3:
-                _fail(f"{what}: [rows][heads][{d}] expected, got {tuple(x.shape)}")
-            shape = (rows, x.shape[1], d)
-            xs = _rows3(x, shape, i, what)
-            if y is None:
-                y = torch.empty(shape, dtype=dtype, device=x.device)
-            ys = _rows3(y, shape, i, what + "_out")
-            if x.dtype is not dtype or y.dtype is not dtype:
-                _fail(f"{what} and its output: {dtype} expected, got {x.dtype} and {y.dtype}")
-            h.x, h.y, h.heads, h.x_row, h.x_head, h.y_row, h.y_head = x.data_ptr(), y.data_ptr(), shape[1], xs[0], xs[1], ys[0], ys[1]
-            if gain is not None:
-                if gain.shape != (d,) or gain.get_device() != i or not gain.is_contiguous():
-                    _fail(f"{what}_gain: contiguous [{d}] on {q.device} expected, got {tuple(gain.shape)} on {gain.device}")
-                h.gain, h.gain_type = gain.data_ptr(), _type(gain.dtype, what + "_gain")
-            outs.append(y)
-        st = pos.stride()
-        _call(i, self.lib.ssd_rotary_apply, self._ref, both, 1 if k is None else 2, code, rows, pos.data_ptr(), st[0],
-              st[1] if len(st) > 1 else 0)
-        return tuple(outs)
+        ps, pst = pos.shape, pos.stride()
+        if pos.dtype is not torch.int32 or pos.get_device() != i or \
+                (ps != (rows, self.axes) and (self.axes != 1 or ps != (rows,))):
+            _fail(f"pos: int32 [{rows}][{self.axes}] on {q.device} expected, got {pos.dtype} {tuple(ps)} on {pos.device}")
+        q_out, first = self._operand(q, q_out, q_gain, rows, i, q.dtype, "q")
+        if k is None:
+            if k_out is not None or k_gain is not None:
+                _fail("k: missing")
+            both = _Heads(first)
+        else:
+            k_out, second = self._operand(k, k_out, k_gain, rows, i, q.dtype, "k")
+            both = _Heads(first, second)
+        _call(i, self.lib.ssd_rotary_apply, self._ref, both, 1 if k is None else 2, code, rows, pos.data_ptr(), pst[0],
+              pst[1] if len(pst) > 1 else 0)
+        return q_out, k_out
+
+    def _operand(self, x, y, gain, rows: int, index: int, dtype: torch.dtype, what: str) -> tuple:
+        """The output and the fields of an ssd_heads."""
+        d, shape = self.head_dim, x.shape
+        if len(shape) != 3 or x.dtype is not dtype:
+            _fail(f"{what}: {dtype} [rows][heads][{d}] expected, got {x.dtype} {tuple(shape)}")
+        heads = shape[1]
+        xs = _rows3(x, (rows, heads, d), index, what)
+        if y is None:
+            y = torch.empty(shape, dtype=dtype, device=x.device)
+            y_row, y_head = heads * d, d
+        else:
+            y_row, y_head, _ = _rows3(y, (rows, heads, d), index, what + "_out")
+            if y.dtype is not dtype:
+                _fail(f"{what}_out: {dtype} expected, got {y.dtype}")
+        g, g_type = None, 0
+        if gain is not None:
+            if gain.shape != (d,) or gain.get_device() != index or not gain.is_contiguous():
+                _fail(f"{what}_gain: contiguous [{d}] on {x.device} expected, got {tuple(gain.shape)} on {gain.device}")
+            g, g_type = gain.data_ptr(), _type(gain.dtype, what + "_gain")
+        return y, (x.data_ptr(), y.data_ptr(), heads, xs[0], xs[1], y_row, y_head, g, g_type)
 
 
 def sample(logits: torch.Tensor, u: torch.Tensor, temperature: float | torch.Tensor = 1.0,
@@ -101,28 +110,32 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: float | torch.Ten
     """ssd_sample: one token per row of logits [rows][vocab] (bfloat16 or float32) from the random numbers u
     (float32 [rows], in [0, 1)).  Each setting is a number for all rows or a tensor [rows] (top_k int32, the others
     float32).  Returns int32 [rows]; with_prob: also the tokens' probabilities among the kept ones, float32 [rows]."""
-    lib = B.load()
-    if logits.dim() != 2 or not logits.is_cuda:
+    lib, i = B.load(), logits.get_device()
+    if i < 0 or logits.dim() != 2:
         _fail(f"logits: [rows][vocab] on a GPU expected, got {tuple(logits.shape)} on {logits.device}")
     rows, vocab = logits.shape
-    i = logits.get_device()
-    stride, code = _rows2(logits, (rows, vocab), i, "logits"), _type(logits.dtype, "logits")
+    one, device = (rows,), logits.device
 
     def per_row(t: torch.Tensor, dtype: torch.dtype, what: str) -> int:
-        if t.dtype is not dtype or t.shape != (rows,) or t.get_device() != i or not t.is_contiguous():
-            _fail(f"{what}: contiguous {dtype} [{rows}] on {logits.device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        if t.dtype is not dtype or t.shape != one or t.get_device() != i or not t.is_contiguous():
+            _fail(f"{what}: contiguous {dtype} [{rows}] on {device} expected, got {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 
-    how = B.SSDSampling()
-    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_p", top_p, torch.float32),
-                               ("min_p", min_p, torch.float32), ("top_k", top_k, torch.int32)):
-        if torch.is_tensor(value):
-            setattr(how, name + "_rows", per_row(value, dtype, name))
-        else:
-            setattr(how, name, value)
+    tensor, f32, i32 = torch.Tensor, torch.float32, torch.int32
+    t_rows = p_rows = m_rows = k_rows = None
+    if isinstance(temperature, tensor):
+        temperature, t_rows = 0.0, per_row(temperature, f32, "temperature")
+    if isinstance(top_p, tensor):
+        top_p, p_rows = 0.0, per_row(top_p, f32, "top_p")
+    if isinstance(min_p, tensor):
+        min_p, m_rows = 0.0, per_row(min_p, f32, "min_p")
+    if isinstance(top_k, tensor):
+        top_k, k_rows = 0, per_row(top_k, i32, "top_k")
+    how = B.SSDSampling(temperature, top_p, min_p, top_k, t_rows, p_rows, m_rows, k_rows)
     if out is None:
-        out = torch.empty(rows, dtype=torch.int32, device=logits.device)
-    prob = torch.empty(rows, dtype=torch.float32, device=logits.device) if with_prob else None
-    _call(i, lib.ssd_sample, logits.data_ptr(), code, rows, vocab, stride, per_row(u, torch.float32, "u"), ctypes.byref(how),
-          per_row(out, torch.int32, "out"), None if prob is None else prob.data_ptr())
+        out = torch.empty(one, dtype=i32, device=device)
+    prob = torch.empty(one, dtype=f32, device=device) if with_prob else None
+    _call(i, lib.ssd_sample, logits.data_ptr(), _type(logits.dtype, "logits"), rows, vocab,
+          _rows2(logits, (rows, vocab), i, "logits"), per_row(u, f32, "u"), ctypes.byref(how), per_row(out, i32, "out"),
+          None if prob is None else prob.data_ptr())
     return (out, prob) if with_prob else out

@@ -270,35 +270,39 @@ def _rows2(t: torch.Tensor, shape: tuple, index: int, what: str) -> int:
     return st[0]
 
 
+def _f4_buffer(lib, rows: int, k: int, device) -> torch.Tensor:
+    size = lib.ssd_f4_bytes(rows, k)
+    if size < 0:
+        _fail(lib.ssd_op_last_error().decode())
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
 class F4Rows:
     """Rows [rows][k] packed to 4-bit floats with a scale per 16 columns and one per row (ssd_f4_pack).
 
     F4Weight.matmul takes them in place of a tensor, so that rows that meet several weights are packed once."""
 
     def __init__(self, x: torch.Tensor):
-        self.lib = B.load()
         if x.dim() != 2 or not x.is_cuda:
             _fail(f"a 2-D CUDA tensor expected, got {tuple(x.shape)} on {x.device}")
-        self.shape, self.dtype, self.device, self._index = x.shape, x.dtype, x.device, x.get_device()
-        size = self.lib.ssd_f4_bytes(*x.shape)
-        if size < 0:
-            _fail(self.lib.ssd_op_last_error().decode())
-        self.packed = torch.empty(size, dtype=torch.uint8, device=x.device)
+        self.lib, self.shape, self.device, self._index = B.load(), x.shape, x.device, x.get_device()
+        self.packed = _f4_buffer(self.lib, *x.shape, x.device)
         self._packed = self.packed.data_ptr()
         self.pack(x)
 
     def pack(self, x: torch.Tensor) -> F4Rows:
         """Packs other rows of the same shape into this buffer."""
-        st, code = _rows2(x, self.shape, self._index, "x"), _type(x.dtype, "x")
-        _call(self._index, self.lib.ssd_f4_pack, x.data_ptr(), code, self.shape[0], self.shape[1], st, self._packed)
-        self.dtype = x.dtype
+        shape, index, dtype = self.shape, self._index, x.dtype
+        _call(index, self.lib.ssd_f4_pack, x.data_ptr(), _type(dtype, "x"), shape[0], shape[1], _rows2(x, shape, index, "x"),
+              self._packed)
+        self.dtype = dtype
         return self
 
     def dequantize(self, dtype: torch.dtype = torch.float32) -> torch.Tensor:
         """The values [rows][k] that the codes stand for."""
-        code = _type(dtype, "dtype")
-        out = torch.empty(self.shape, dtype=dtype, device=self.device)
-        _call(self._index, self.lib.ssd_f4_unpack, self._packed, self.shape[0], self.shape[1], out.data_ptr(), code)
+        code, shape = _type(dtype, "dtype"), self.shape
+        out = torch.empty(shape, dtype=dtype, device=self.device)
+        _call(self._index, self.lib.ssd_f4_unpack, self._packed, shape[0], shape[1], out.data_ptr(), code)
         return out
 
 
@@ -313,33 +317,29 @@ class F4Weight(F4Rows):
                residual: torch.Tensor | None = None) -> torch.Tensor:
         """x W^T (+ residual) for x [rows][k] in bfloat16 or float32, packed on the way, or packed already
         (ssd_f4_matmul).  The result has x's type (for F4Rows the type of the rows that were packed)."""
-        i, n, k, dtype = self._index, self.n, self.k, x.dtype
+        i, n, k, shape, dtype = self._index, self.n, self.k, x.shape, x.dtype
         code = _type(dtype, "x")
+        if len(shape) != 2 or shape[1] != k:
+            _fail(f"x: [rows][{k}] expected, got {tuple(shape)}")
+        rows = shape[0]
         if isinstance(x, F4Rows):
-            if x.shape[1] != k or x._index != i:
-                _fail(f"x: [rows][{k}] on {self.device} expected, got {tuple(x.shape)} on {x.device}")
-            rows, px, xs, xcode, work = x.shape[0], x._packed, 0, B.SSD_TYPE_F4, None
+            if x._index != i:
+                _fail(f"x: on cuda:{i} expected, got {x.device}")
+            px, xs, xcode, work = x._packed, 0, B.SSD_TYPE_F4, None
         else:
-            if x.dim() != 2:
-                _fail(f"x: [rows][{k}] expected, got {tuple(x.shape)}")
-            rows, px, xcode, work = x.shape[0], x.data_ptr(), code, None
-            xs = _rows2(x, (rows, k), i, "x")
-            if rows:
-                size = self.lib.ssd_f4_bytes(rows, k)
-                if size < 0:
-                    _fail(self.lib.ssd_op_last_error().decode())
-                work = torch.empty(size, dtype=torch.uint8, device=self.device)
+            px, xs, xcode = x.data_ptr(), _rows2(x, shape, i, "x"), code
+            work = _f4_buffer(self.lib, rows, k, self.device) if rows else None
         if out is None:
             out, os = torch.empty((rows, n), dtype=dtype, device=self.device), n
         else:
             os = _rows2(out, (rows, n), i, "out")
             if out.dtype is not dtype:
                 _fail(f"out: {dtype} expected, got {out.dtype}")
-        rs = 0
+        res, rs = None, 0
         if residual is not None:
-            rs = _rows2(residual, (rows, n), i, "residual")
+            res, rs = residual.data_ptr(), _rows2(residual, (rows, n), i, "residual")
             if residual.dtype is not dtype:
                 _fail(f"residual: {dtype} expected, got {residual.dtype}")
-        _call(i, self.lib.ssd_f4_matmul, self._packed, n, k, px, xcode, rows, xs, out.data_ptr(), code, os,
-              None if residual is None else residual.data_ptr(), rs, None if work is None else work.data_ptr())
+        _call(i, self.lib.ssd_f4_matmul, self._packed, n, k, px, xcode, rows, xs, out.data_ptr(), code, os, res, rs,
+              None if work is None else work.data_ptr())
         return out
