@@ -619,6 +619,8 @@ SSD_API ssd_status ssd_w4_matmul(const void* packed, int n, int k, int group, co
  * the matrix instructions take them, then rho [rows].  ssd_f4_bytes: -1 for a shape that is not supported
  * (rows or k < 1, rows > 2^23, k > 2^20). */
 SSD_API int64_t ssd_f4_bytes(int rows, int k);
+/* Bytes of ssd_f4_matmul's work for rows that are not packed yet (0: none), -1 for a shape that is not supported. */
+SSD_API int64_t ssd_f4_work_bytes(int rows, int k);
 
 /* Pack x: device, type SSD_TYPE_*, [rows][x_row_stride], aligned to its elements; packed: device, ssd_f4_bytes() of
  * them, 16-byte aligned.  x and packed must not overlap. */
@@ -630,9 +632,9 @@ SSD_API ssd_status ssd_f4_pack(const void* x, int type, int rows, int k, int64_t
 SSD_API ssd_status ssd_f4_unpack(const void* packed, int rows, int k, void* out, int type, void* cuda_stream);
 
 /* y = x W^T (+ residual) of packed w [n][k], fp32 sums of the codes' exact products, each row's scaled in fp32.
- *   x: device, x_type SSD_TYPE_BF16 / FP32: [rows][x_row_stride], packed into work first (ssd_f4_bytes(rows, k),
- *     16-byte aligned, of this call alone until it has run); SSD_TYPE_F4: rows packed by ssd_f4_pack
- *     (x_row_stride and work are not looked at)
+ *   x: device, x_type SSD_TYPE_BF16 / FP32: [rows][x_row_stride], packed into work first (ssd_f4_work_bytes(rows, k),
+ *     16-byte aligned, of this call alone until it has run; few short rows need none, and work is not looked at);
+ *     SSD_TYPE_F4: rows packed by ssd_f4_pack (x_row_stride and work are not looked at)
  *   y: device, type SSD_TYPE_BF16 / FP32, [rows][y_row_stride];  residual: device [rows][res_row_stride] of the same
  *     type, or NULL; may be y itself (same rows), else must not overlap it.  y must not overlap x, w or work. */
 SSD_API ssd_status ssd_f4_matmul(const void* w, int n, int k, const void* x, int x_type, int rows,

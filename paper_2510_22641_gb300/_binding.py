@@ -52,7 +52,7 @@ EXPORTED = ("ssd_create", "ssd_destroy", "ssd_prefill", "ssd_draft", "ssd_verify
             "ssd_lm_head_static", "ssd_profile_projection", "ssd_set_fault_injection", "ssd_probe_bounded_wait",
             "ssd_kv8_data_bytes", "ssd_kv8_work_bytes", "ssd_kv8_step_ints", "ssd_kv8_plan", "ssd_kv8_append",
             "ssd_kv8_read", "ssd_kv8_attention", "ssd_kv8_status", "ssd_w4_bytes", "ssd_w4_work_bytes", "ssd_w4_pack",
-            "ssd_w4_unpack", "ssd_w4_matmul", "ssd_f4_bytes", "ssd_f4_pack", "ssd_f4_unpack", "ssd_f4_matmul",
+            "ssd_w4_unpack", "ssd_w4_matmul", "ssd_f4_bytes", "ssd_f4_work_bytes", "ssd_f4_pack", "ssd_f4_unpack", "ssd_f4_matmul",
             "ssd_rotary_init", "ssd_rotary_apply", "ssd_sample", "ssd_op_last_error",
             "ssd_status_string", "ssd_last_error")
 
@@ -191,7 +191,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.ssd_rel_bucket.restype = ctypes.c_int
     for name, args in {"ssd_kv8_data_bytes": [vp], "ssd_kv8_work_bytes": [vp], "ssd_kv8_step_ints": [i32, i32],
                        "ssd_w4_bytes": [i32, i32, i32], "ssd_w4_work_bytes": [i32, i32],
-                       "ssd_f4_bytes": [i32, i32]}.items():
+                       "ssd_f4_bytes": [i32, i32], "ssd_f4_work_bytes": [i32, i32]}.items():
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = i64
     lib.ssd_op_last_error.argtypes = []

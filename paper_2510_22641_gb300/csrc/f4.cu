@@ -1,7 +1,4 @@
 // 4-bit floats: packing rows and reading them back.
-#include <cuda_fp4.h>
-#include <cuda_fp8.h>
-
 #include "f4.cuh"
 
 namespace ssd {
@@ -14,134 +11,6 @@ struct F4PackParams {
   uint8_t* out;
   float* rho;
 };
-
-// Eight neighbouring columns as they lie in memory: fp32 numbers, or pairs of bf16.
-template <typename T>
-struct Raw8 {
-  uint32_t w[2 * sizeof(T)];
-
-  // From `col` on, zeros past k.  VEC: 16-byte aligned.
-  template <bool VEC>
-  __device__ __forceinline__ void load(const T* p, int col, int k) {
-    if (VEC && col + 8 <= k) {
-#pragma unroll
-      for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i)
-        reinterpret_cast<uint4*>(w)[i] = reinterpret_cast<const uint4*>(p + col)[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (sizeof(T) == 4) {
-          w[i] = col + i < k ? __float_as_uint(p[col + i]) : 0u;
-        } else {
-          const uint32_t v = col + i < k ? __bfloat16_as_ushort(p[col + i]) : 0u;
-          w[i / 2] = i & 1 ? w[i / 2] | v << 16 : v;
-        }
-      }
-    }
-  }
-  // The largest magnitude's bits as those of a float: a NaN is above infinity, infinity above the rest.
-  __device__ __forceinline__ uint32_t amax() const {
-    if constexpr (sizeof(T) == 4) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7fffffffu);
-      return m;
-    } else {
-      uint32_t m = 0;  // of the even and the odd columns
-#pragma unroll
-      for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
-      return max(m << 16, m & 0xffff0000u);
-    }
-  }
-  __device__ __forceinline__ float2 pair(int i) const {
-    if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
-    return bf16x2_to_float2(w[i]);
-  }
-};
-
-__device__ __forceinline__ float e4m3_value(uint32_t byte) {
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(byte), __NV_E4M3)));
-}
-
-// A row's scale from the bits of its largest magnitude: the exponent of the smallest 2^e with amax <= 2688 2^e
-// (2688 = 1.3125 * 2^11), at least -100.
-__device__ __forceinline__ int f4_row_exponent(uint32_t amax) {
-  return max(static_cast<int>(amax >> 23) - 127 - 11 + ((amax & 0x7fffffu) > 0x280000u ? 1 : 0), -100);
-}
-
-// Four pairs to a word of codes, to nearest even, at most 6.
-__device__ __forceinline__ uint32_t to_e2m1(const float2* q) {
-  uint32_t w;
-  asm("{\n .reg .b8 a, b, c, d;\n"
-      " cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
-      " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}"
-      : "=r"(w)
-      : "f"(q[0].x), "f"(q[0].y), "f"(q[1].x), "f"(q[1].y), "f"(q[2].x), "f"(q[2].y), "f"(q[3].x), "f"(q[3].y));
-  return w;
-}
-__device__ __forceinline__ float approx_reciprocal(float v) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
-
-// One row's 16-column group, half of it (8 columns, largest magnitude `bits`) in this lane and half in lane ^ 1, times the
-// row's down = 2^-e: the scale's byte and the 8 codes.  A quotient is fma(y, h, y * l) of its divisor's reciprocal h + l,
-// exact to 2^-45, and so correctly rounded: numerators have 24 bits and divisors (6, s) at most 4, so no quotient lies
-// nearer than 2^-30 to the middle of two fp32 numbers.
-template <typename T>
-__device__ __forceinline__ void f4_encode(const Raw8<T>& x, uint32_t bits, float down, uint32_t& scale, uint32_t& codes) {
-  bits = max(bits, __shfl_xor_sync(~0u, bits, 1));
-  constexpr float kSixth = 1.0f / 6.0f, kSixthLow = static_cast<float>(1.0 / 6.0 - static_cast<double>(kSixth));
-  const float m = __uint_as_float(bits) * down;
-  scale = __nv_cvt_float_to_fp8(fmaf(m, kSixth, m * kSixthLow), __NV_SATFINITE, __NV_E4M3);
-  const float s = e4m3_value(scale);
-  float h = approx_reciprocal(s), l = fmaf(-s, h, 1.0f) * h;
-  if (scale == 0) h = l = 0.0f;
-  float2 q[4];
-  // the row's power of two goes into the reciprocal, but where that would push its low part out of range
-  if (down >= 0x1p-70f) {
-    h *= down, l *= down;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 y = x.pair(i);
-      q[i] = make_float2(fmaf(y.x, h, y.x * l), fmaf(y.y, h, y.y * l));
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 y = make_float2(x.pair(i).x * down, x.pair(i).y * down);
-      q[i] = make_float2(fmaf(y.x, h, y.x * l), fmaf(y.y, h, y.y * l));
-    }
-  }
-  codes = to_e2m1(q);
-}
-
-struct F4Row {  // what a row's largest magnitude says
-  bool bad;
-  float down;
-  __device__ __forceinline__ F4Row(uint32_t amax) {
-    bad = amax >= 0x7f800000u;
-    down = __uint_as_float(static_cast<uint32_t>(127 - (bad ? 0 : f4_row_exponent(amax))) << 23);
-  }
-  __device__ __forceinline__ float rho() const {
-    return __uint_as_float(bad ? 0x7fc00000u : (254u << 23) - __float_as_uint(down));
-  }
-};
-
-// Writes 8 columns' codes, and a group's scale as one of four in a word.
-template <typename T>
-__device__ __forceinline__ void f4_put(const Raw8<T>& x, uint32_t bits, const F4Row& f, uint8_t* at, int r) {
-  const int lane = threadIdx.x & 31;
-  uint32_t scale, codes;
-  f4_encode(x, bits, f.down, scale, codes);
-  if (f.bad) scale = codes = 0;
-  *reinterpret_cast<uint32_t*>(at + f4_code_byte(r, lane * 8)) = codes;
-  scale <<= 8 * (lane >> 1 & 3);
-  scale |= __shfl_xor_sync(~0u, scale, 2);
-  scale |= __shfl_xor_sync(~0u, scale, 4);
-  if ((lane & 7) == 0) *reinterpret_cast<uint32_t*>(at + f4_scale_byte(r, lane * 8)) = scale;
-}
 
 // A row is held in registers between its maximum and its codes, by p.warps warps (1, 2, 4 or 8) of up to J chunks of
 // 256 columns each, 8 columns a lane; the CTA has 8 warps.  The row is read once.
@@ -175,7 +44,8 @@ __global__ void __launch_bounds__(256) ssd_f4_pack_kernel(const F4PackParams p) 
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const int c = c0 + j * p.warps;
-    if (c < p.chunks) f4_put(x[j], most[j], f, rec + static_cast<int64_t>(c) * kF4Record, row % kF4Rows);
+    uint8_t* at = rec + static_cast<int64_t>(c) * kF4Record;
+    if (c < p.chunks) f4_put(x[j], most[j], f, at, at + kF4CodeBytes, row % kF4Rows);
   }
 }
 
@@ -202,7 +72,8 @@ __global__ void __launch_bounds__(256) ssd_f4_pack_long_kernel(const F4PackParam
   uint8_t* rec = p.out + static_cast<int64_t>(row / kF4Rows) * p.chunks * kF4Record;
   for (int c = warp; c < p.chunks; c += 8) {
     x.template load<VEC>(src, c * kF4Cols + lane * 8, p.k);
-    f4_put(x, x.amax(), f, rec + static_cast<int64_t>(c) * kF4Record, row % kF4Rows);
+    uint8_t* at = rec + static_cast<int64_t>(c) * kF4Record;
+    f4_put(x, x.amax(), f, at, at + kF4CodeBytes, row % kF4Rows);
   }
 }
 
@@ -323,6 +194,11 @@ extern "C" {
 int64_t ssd_f4_bytes(int rows, int k) {
   if (f4_check_shape(rows, k)) return -1;
   return f4_scales_at(rows, k) + static_cast<int64_t>((rows + kF4Rows - 1) / kF4Rows) * kF4Rows * 4;
+}
+
+int64_t ssd_f4_work_bytes(int rows, int k) {
+  if (f4_check_shape(rows, k)) return -1;
+  return f4_packs_inside(rows, k) ? 0 : ssd_f4_bytes(rows, k);
 }
 
 ssd_status ssd_f4_pack(const void* x, int type, int rows, int k, int64_t x_row_stride, void* packed, void* cuda_stream) {

@@ -1,6 +1,8 @@
 // Products of rows and weights that are both packed to 4-bit floats.
 #include "f4.cuh"
 
+#include <type_traits>
+
 #include "tcgen05.cuh"
 
 namespace ssd {
@@ -11,6 +13,9 @@ struct F4MatmulParams {
   const uint32_t *w_rho, *x_rho;
   int n, rows, chunks;
   int early;  // the launch before writes x alone: w may be read ahead of it
+  const void* rows_in;  // rows that are packed here (x is not looked at)
+  int64_t rows_stride;
+  int k, vec;
   void* y;
   const void* residual;
   int64_t y_row, r_row;
@@ -107,15 +112,17 @@ struct F4Tile {
   // tensor memory columns: the sums, then each stage's scales (16 of w, 16 of x)
   static constexpr int kSums = BN < 32 ? 32 : BN, kScaleCols = 32;
   static constexpr int kCols = 256;
-  static constexpr int kSmem = 1024 + kStages * kStage + 256 + BN * 4;
+  static constexpr int kSmem = 1024 + kStages * kStage + 256 + BN * 4 + 64;
   static_assert(BN <= kF4Rows && kSums + kStages * kScaleCols <= kCols, "tensor memory");
   static_assert(BN * kF4Rows * 4 <= kStages * kStage, "partial sums take the stages' place");
 };
 
 // Warp 0 copies records to shared memory, warp 1 issues the products, warps 2..5 read the sums.  The CTAs of a
-// cluster split the columns and add up in rank order through shared memory.
-template <int BN, typename T>
+// cluster split the columns and add up in rank order through shared memory.  X: void, or the type of up to four rows that
+// are packed here: warps 2..5 find their largest magnitudes and write their codes and scales to the stages.
+template <int BN, typename T, typename X>
 __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams p) {
+  constexpr bool kPack = !std::is_void_v<X>;
   using S = F4Tile<BN>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -133,7 +140,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
   const int c1 = static_cast<int>(static_cast<int64_t>(p.chunks) * (rank + 1) / split);
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < S::kStages; ++s) mbar_init(&full[s], 1), mbar_init(&empty[s], 1);
+    for (int s = 0; s < S::kStages; ++s) mbar_init(&full[s], kPack ? 1 + cols : 1), mbar_init(&empty[s], 1);
     mbar_init(done, 1);
     fence_mbar_init();
   }
@@ -155,10 +162,11 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
       const uint8_t* x = p.x;
       auto load_w = [&](int c) {
         const int s = (c - c0) % S::kStages;
-        mbar_arrive_expect_tx(&full[s], kF4Record + nn * 128 + S::kScales);
+        mbar_arrive_expect_tx(&full[s], kF4Record + (kPack ? 0 : nn * 128 + S::kScales));
         bulk_load(smem + s * S::kStage, w + static_cast<int64_t>(c) * kF4Record, kF4Record, &full[s]);
       };
       auto load_x = [&](int c) {
+        if (kPack) return;
         const int s = (c - c0) % S::kStages;
         uint8_t* at = smem + s * S::kStage + kF4Record;
         const uint8_t* rec = x + static_cast<int64_t>(c) * kF4Record;
@@ -206,13 +214,55 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
   } else {
     const int q = warp & 3, n = n0 + q * 32 + lane;
     pdl_wait();
-    for (int i = threadIdx.x - 64; i < cols; i += 128) rho[i] = p.x_rho[i];
+    if constexpr (kPack) {
+      using P = std::conditional_t<kPack, X, float>;
+      const P* const x = static_cast<const P*>(p.rows_in);
+      uint32_t* const part = rho + BN;  // [4 rows][4 warps]
+      auto load = [&](Raw8<P>& v, int r, int c) {
+        if (p.vec)
+          v.template load<true>(x + r * p.rows_stride, c * kF4Cols + lane * 8, p.k);
+        else
+          v.template load<false>(x + r * p.rows_stride, c * kF4Cols + lane * 8, p.k);
+      };
+      for (int r = 0; r < cols; ++r) {
+        uint32_t most = 0;
+#pragma unroll 4
+        for (int c = warp - 2; c < p.chunks; c += 4) {
+          Raw8<P> v;
+          load(v, r, c);
+          most = max(most, v.amax());
+        }
+        most = __reduce_max_sync(~0u, most);
+        if (lane == 0) part[4 * r + warp - 2] = most;
+      }
+      named_bar_sync(1, 128);
+      int turn = 0;  // of the four warps
+      for (int c = c0; c < c1 && ok; ++c) {
+        const int i = c - c0, s = i % S::kStages;
+        uint8_t* const at = smem + s * S::kStage + kF4Record;
+        for (int r = 0; r < cols; ++r, ++turn) {
+          if ((turn & 3) != warp - 2) continue;
+          ok = __all_sync(~0u, i < S::kStages || f4_wait(&empty[s], (i / S::kStages - 1) & 1));
+          if (!ok) break;
+          const F4Row f(max(max(part[4 * r], part[4 * r + 1]), max(part[4 * r + 2], part[4 * r + 3])));
+          if (lane == 0) rho[r] = __float_as_uint(f.rho());
+          Raw8<P> v;
+          load(v, r, c);
+          f4_put(v, v.amax(), f, at, at + S::kCodes, r);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&full[s]);
+        }
+      }
+    } else {
+      for (int i = threadIdx.x - 64; i < cols; i += 128) rho[i] = p.x_rho[i];
+    }
     const uint32_t rho_w = n < p.n ? p.w_rho[n] : 0u;
     named_bar_sync(1, 128);
     bool plain = f4_plain(rho_w);
     for (int i = 0; i < cols; ++i) plain &= f4_plain(rho[i]);
     plain = __all_sync(~0u, plain || n >= p.n);
-    ok = f4_wait(done, 0);
+    ok = ok && f4_wait(done, 0);
     tmem_fence_after();
     for (int c = 0; c < nn; c += 16) {
       float v[16];
@@ -537,17 +587,17 @@ ssd_status f4_launch_pair(const F4MatmulParams& p, cudaStream_t s) {
                            kF4PairThreads, F4Pair::kSmem, dim3(2), s, p);
 }
 
-template <int BN, typename T>
+template <int BN, typename T, typename X = void>
 ssd_status f4_launch(const F4MatmulParams& p, int split, cudaStream_t s) {
   static std::atomic<uint64_t> ready{0};
   constexpr int smem = F4Tile<BN>::kSmem;
-  if (ssd_status e = op_smem(ssd_f4_matmul_kernel<BN, T>, smem, ready, "ssd_f4_matmul")) return e;
+  if (ssd_status e = op_smem(ssd_f4_matmul_kernel<BN, T, X>, smem, ready, "ssd_f4_matmul")) return e;
   const dim3 grid((p.n + kF4Rows - 1) / kF4Rows, 1, split);
-  return op_launch_cluster("ssd_f4_matmul", ssd_f4_matmul_kernel<BN, T>, grid, 192, smem, dim3(1, 1, split), s, p);
+  return op_launch_cluster("ssd_f4_matmul", ssd_f4_matmul_kernel<BN, T, X>, grid, 192, smem, dim3(1, 1, split), s, p);
 }
 
 template <typename T>
-ssd_status f4_dispatch(const F4MatmulParams& p, cudaStream_t s) {
+ssd_status f4_dispatch(const F4MatmulParams& p, int x_type, cudaStream_t s) {
   if (p.rows > 128) return f4_launch_pair<T>(p, s);
   const int bn = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
   const int tiles = (p.n + kF4Rows - 1) / kF4Rows;
@@ -555,6 +605,8 @@ ssd_status f4_dispatch(const F4MatmulParams& p, cudaStream_t s) {
   // 7.1; with more CTAs than SMs the clusters wait for each other's places: 64 x 11008 x 4096 one 12.8, two 20.5).
   int split = 1;
   while (split < 8 && tiles * split * 2 <= 152 && split * 2 <= p.chunks) split *= 2;
+  if (p.rows_in)
+    return x_type == SSD_TYPE_FP32 ? f4_launch<16, T, float>(p, split, s) : f4_launch<16, T, __nv_bfloat16>(p, split, s);
   switch (bn) {
     case 16: return f4_launch<16, T>(p, split, s);
     case 32: return f4_launch<32, T>(p, split, s);
@@ -580,8 +632,9 @@ ssd_status ssd_f4_matmul(const void* w, int n, int k, const void* x, int x_type,
     return op_fail(SSD_ERR_INVALID_ARG, "x_type %d", x_type);
   if (rows == 0) return SSD_OK;
   if (ssd_status s = f4_check_shape(rows, k)) return s;
-  const void* xp = packed ? x : work;
-  if (!w || !x || !y || !xp || reinterpret_cast<uintptr_t>(w) % 16 || reinterpret_cast<uintptr_t>(xp) % 16)
+  const bool inside = !packed && f4_packs_inside(rows, k);
+  const void* xp = packed || inside ? x : work;
+  if (!w || !x || !y || !xp || reinterpret_cast<uintptr_t>(w) % 16 || (!inside && reinterpret_cast<uintptr_t>(xp) % 16))
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_f4_matmul: null or unaligned buffer");
   const int size = type == SSD_TYPE_FP32 ? 4 : 2, xsize = x_type == SSD_TYPE_FP32 ? 4 : 2;
   if ((reinterpret_cast<uintptr_t>(y) | reinterpret_cast<uintptr_t>(residual)) % size ||
@@ -592,24 +645,28 @@ ssd_status ssd_f4_matmul(const void* w, int n, int k, const void* x, int x_type,
       pb{xp, 1, 1, 0, 0, xbytes}, xb{x, rows, 1, x_row_stride * xsize, 0, static_cast<int64_t>(k) * xsize},
       rb{residual, rows, 1, res_row_stride * size, 0, static_cast<int64_t>(n) * size};
   if (!op_apart(yb)) return op_fail(SSD_ERR_INVALID_ARG, "ssd_f4_matmul: rows of y overlap");
-  if (op_overlap(yb, wb, 1) || op_overlap(yb, pb, 1) || (!packed && op_overlap(yb, xb, 1)))
+  if (op_overlap(yb, wb, 1) || (!inside && op_overlap(yb, pb, 1)) || (!packed && op_overlap(yb, xb, 1)))
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_f4_matmul: y overlaps x, w or work");
-  if (!packed && (op_overlap(pb, xb, 1) || op_overlap(pb, wb, 1) || (residual && op_overlap(pb, rb, 1))))
+  if (!packed && !inside && (op_overlap(pb, xb, 1) || op_overlap(pb, wb, 1) || (residual && op_overlap(pb, rb, 1))))
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_f4_matmul: work overlaps x, w or the residual");
   const bool in_place = residual == y && (rows == 1 || res_row_stride == y_row_stride);
   if (residual && !in_place && op_overlap(rb, yb, 1))
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_f4_matmul: y overlaps the residual and is not the same rows");
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (!packed)
+  if (!packed && !inside)
     if (ssd_status e = f4_pack_rows("ssd_f4_matmul", x, x_type, rows, k, x_row_stride, work, s)) return e;
   F4MatmulParams p{};
   p.w = static_cast<const uint8_t*>(w);
   p.x = static_cast<const uint8_t*>(xp);
   p.w_rho = reinterpret_cast<const uint32_t*>(p.w + f4_scales_at(n, k));
   p.x_rho = reinterpret_cast<const uint32_t*>(p.x + f4_scales_at(rows, k));
-  p.n = n, p.rows = rows, p.chunks = f4_chunks(k), p.early = !packed;
+  p.n = n, p.rows = rows, p.chunks = f4_chunks(k), p.early = !packed && !inside, p.k = k;
+  if (inside) {
+    p.rows_in = x, p.rows_stride = x_row_stride;
+    p.vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (rows == 1 || x_row_stride % (16 / xsize) == 0);
+  }
   p.y = y, p.residual = residual, p.y_row = y_row_stride, p.r_row = res_row_stride;
-  return type == SSD_TYPE_FP32 ? f4_dispatch<float>(p, s) : f4_dispatch<__nv_bfloat16>(p, s);
+  return type == SSD_TYPE_FP32 ? f4_dispatch<float>(p, x_type, s) : f4_dispatch<__nv_bfloat16>(p, x_type, s);
 }
 
 }  // extern "C"

@@ -270,8 +270,7 @@ def _rows2(t: torch.Tensor, shape: tuple, index: int, what: str) -> int:
     return st[0]
 
 
-def _f4_buffer(lib, rows: int, k: int, device) -> torch.Tensor:
-    size = lib.ssd_f4_bytes(rows, k)
+def _f4_buffer(lib, size: int, device) -> torch.Tensor:
     if size < 0:
         _fail(lib.ssd_op_last_error().decode())
     return torch.empty(size, dtype=torch.uint8, device=device)
@@ -286,7 +285,7 @@ class F4Rows:
         if x.dim() != 2 or not x.is_cuda:
             _fail(f"a 2-D CUDA tensor expected, got {tuple(x.shape)} on {x.device}")
         self.lib, self.shape, self.device, self._index = B.load(), x.shape, x.device, x.get_device()
-        self.packed = _f4_buffer(self.lib, *x.shape, x.device)
+        self.packed = _f4_buffer(self.lib, self.lib.ssd_f4_bytes(*x.shape), x.device)
         self._packed = self.packed.data_ptr()
         self.pack(x)
 
@@ -328,7 +327,9 @@ class F4Weight(F4Rows):
             px, xs, xcode, work = x._packed, 0, B.SSD_TYPE_F4, None
         else:
             px, xs, xcode = x.data_ptr(), _rows2(x, shape, i, "x"), code
-            work = _f4_buffer(self.lib, rows, k, self.device) if rows else None
+            work, size = None, self.lib.ssd_f4_work_bytes(rows, k) if rows else 0
+            if size:
+                work = _f4_buffer(self.lib, size, self.device)
         if out is None:
             out, os = torch.empty((rows, n), dtype=dtype, device=self.device), n
         else:

@@ -100,6 +100,20 @@ def test_product(rows, n, k, dtype):
     assert torch.equal(y, w.matmul(packed))      # and from rows that were packed before
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("n,k", [(1, 16), (130, 255), (4096, 4096), (20000, 4096), (70, 16384), (300, 5000)])
+def test_product_that_packs_its_rows(rows, n, k, dtype):
+    """Few short rows have no launch of their own: the same bits as of rows packed before, any alignment."""
+    w = lib.F4Weight(normal((n, k), 1, 0.02, torch.bfloat16))
+    base = uneven(rows, k + 8, 2, DT[dtype])
+    for x in (base[:, :k], base[:, 1:k + 1], base[:, 8:k + 8]):
+        packed = lib.F4Rows(x)
+        y = w.matmul(x)
+        assert torch.equal(y, w.matmul(packed))
+        check_product(y, packed.dequantize(), w.dequantize())
+
+
 @pytest.mark.parametrize("rows,n,k", [(1, 30000, 2048), (5, 64, 14336), (40, 11000, 5120), (640, 4096, 2048), (3001, 1300, 768),
                                       (1000, 9001, 1040), (8192, 200, 160)])
 def test_product_of_large_shapes(rows, n, k):

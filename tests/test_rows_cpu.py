@@ -40,6 +40,15 @@ def test_packed_sizes(l):
         assert l.ssd_f4_bytes(*bad) == -1
 
 
+def test_work_sizes(l):
+    """Few short rows are packed by the product itself."""
+    for rows, k in ((1, 1), (1, 16384), (4, 4096)):
+        assert l.ssd_f4_work_bytes(rows, k) == 0
+    for rows, k in ((1, 16385), (4, 4097), (5, 64), (300, 4096)):
+        assert l.ssd_f4_work_bytes(rows, k) == l.ssd_f4_bytes(rows, k) > 0
+    assert l.ssd_f4_work_bytes(0, 5) == -1 and l.ssd_f4_work_bytes(5, 0) == -1
+
+
 def pack(l, **over):
     a = dict(x=4096, type=0, rows=4, k=64, stride=64, packed=1 << 20) | over
     return l.ssd_f4_pack(a["x"], a["type"], a["rows"], a["k"], a["stride"], a["packed"], None)
@@ -64,7 +73,7 @@ MB = 1 << 20
 
 
 def matmul(l, **over):
-    a = dict(w=MB, n=100, k=64, x=8 * MB, x_type=0, rows=3, xs=64, y=16 * MB, type=0, ys=100, res=None, rs=0,
+    a = dict(w=MB, n=100, k=64, x=8 * MB, x_type=0, rows=5, xs=64, y=16 * MB, type=0, ys=100, res=None, rs=0,
              work=24 * MB) | over
     return l.ssd_f4_matmul(a["w"], a["n"], a["k"], a["x"], a["x_type"], a["rows"], a["xs"], a["y"], a["type"], a["ys"],
                            a["res"], a["rs"], a["work"], None)
