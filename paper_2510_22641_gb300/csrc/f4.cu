@@ -7,35 +7,35 @@ namespace {
 struct F4PackParams {
   const void* x;
   int64_t x_row;
-  int rows, k, chunks, warps;
+  int rows, k, chunks, warps_log;
   uint8_t* out;
   float* rho;
 };
 
-// A row is held in registers between its maximum and its codes, by p.warps warps (1, 2, 4 or 8) of up to J chunks of
+// A row is held in registers between its maximum and its codes, by `warps` warps (1, 2, 4 or 8) of up to J chunks of
 // 256 columns each, 8 columns a lane; the CTA has 8 warps.  The row is read once.
 template <typename T, bool VEC, int J>
 __global__ void __launch_bounds__(256) ssd_f4_pack_kernel(const F4PackParams p) {
   pdl_wait();
   pdl_trigger();
   __shared__ uint32_t part[8];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = warp % p.warps;
-  const int row = blockIdx.x * (8 / p.warps) + warp / p.warps;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = 1 << p.warps_log, c0 = warp & (warps - 1);
+  const int row = (blockIdx.x << (3 - p.warps_log)) + (warp >> p.warps_log);
   const bool on = row < p.rows;
   const T* src = static_cast<const T*>(p.x) + (on ? row : 0) * p.x_row;
   Raw8<T> x[J];
   uint32_t amax = 0, most[J];
 #pragma unroll
   for (int j = 0; j < J; ++j)
-    if (c0 + j * p.warps < p.chunks) x[j].template load<VEC>(src, (c0 + j * p.warps) * kF4Cols + lane * 8, p.k);
+    if (c0 + j * warps < p.chunks) x[j].template load<VEC>(src, (c0 + j * warps) * kF4Cols + lane * 8, p.k);
 #pragma unroll
   for (int j = 0; j < J; ++j)
-    if (c0 + j * p.warps < p.chunks) amax = max(amax, most[j] = x[j].amax());
+    if (c0 + j * warps < p.chunks) amax = max(amax, most[j] = x[j].amax());
   amax = __reduce_max_sync(~0u, amax);
-  if (p.warps > 1) {
+  if (warps > 1) {
     if (lane == 0) part[warp] = amax;
     __syncthreads();
-    for (int i = 0; i < p.warps; ++i) amax = max(amax, part[warp - c0 + i]);
+    amax = __reduce_max_sync(~0u, part[warp - c0 + (lane & (warps - 1))]);
   }
   if (!on) return;
   const F4Row f(amax);
@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(256) ssd_f4_pack_kernel(const F4PackParams p) 
   uint8_t* rec = p.out + static_cast<int64_t>(row / kF4Rows) * p.chunks * kF4Record;
 #pragma unroll
   for (int j = 0; j < J; ++j) {
-    const int c = c0 + j * p.warps;
+    const int c = c0 + j * warps;
     uint8_t* at = rec + static_cast<int64_t>(c) * kF4Record;
     if (c < p.chunks) f4_put(x[j], most[j], f, at, at + kF4CodeBytes, row % kF4Rows);
   }
@@ -139,8 +139,8 @@ __global__ void __launch_bounds__(256) ssd_f4_unpack_kernel(const uint8_t* packe
 template <typename T, bool VEC>
 ssd_status f4_pack_dispatch(const char* what, F4PackParams& p, cudaStream_t s) {
   // one warp a row as long as it holds the row in two chunks a lane; eight from 8 chunks on
-  p.warps = p.chunks <= 2 ? 1 : p.chunks <= 4 ? 2 : p.chunks <= 8 ? 4 : 8;
-  const int each = 8 / p.warps;
+  p.warps_log = p.chunks <= 2 ? 0 : p.chunks <= 4 ? 1 : p.chunks <= 8 ? 2 : 3;
+  const int each = 8 >> p.warps_log;
   const dim3 grid((p.rows + each - 1) / each);
   if (p.chunks <= 16) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 2>, grid, 256, 0, s, p);
   if (p.chunks <= 32) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 4>, grid, 256, 0, s, p);

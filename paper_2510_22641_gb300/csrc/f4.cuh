@@ -114,19 +114,13 @@ __device__ __forceinline__ void f4_encode(const Raw8<T>& x, uint32_t bits, float
   if (scale == 0) h = l = 0.0f;
   float2 q[4];
   // the row's power of two goes into the reciprocal, but where that would push its low part out of range
-  if (down >= 0x1p-70f) {
-    h *= down, l *= down;
+  const bool fold = down >= 0x1p-70f;
+  if (fold) h *= down, l *= down;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 y = x.pair(i);
-      q[i] = make_float2(fmaf(y.x, h, y.x * l), fmaf(y.y, h, y.y * l));
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 y = make_float2(x.pair(i).x * down, x.pair(i).y * down);
-      q[i] = make_float2(fmaf(y.x, h, y.x * l), fmaf(y.y, h, y.y * l));
-    }
+  for (int i = 0; i < 4; ++i) {
+    Float2x y(x.pair(i).x, x.pair(i).y);
+    if (!fold) y = y * Float2x(down);
+    q[i] = fma2(y, Float2x(h), y * Float2x(l)).get();
   }
   codes = to_e2m1(q);
 }

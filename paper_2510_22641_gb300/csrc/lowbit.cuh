@@ -164,6 +164,31 @@ __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// Two floats that one instruction adds, multiplies or does both with, each rounded as a float.
+struct Float2x {
+  uint64_t v;
+  __device__ __forceinline__ Float2x() = default;
+  __device__ __forceinline__ Float2x(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ explicit Float2x(float a) : Float2x(a, a) {}
+  __device__ __forceinline__ float2 get() const {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+  }
+};
+__device__ __forceinline__ Float2x operator*(Float2x a, Float2x b) {
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
+  return a;
+}
+__device__ __forceinline__ Float2x operator+(Float2x a, Float2x b) {
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
+  return a;
+}
+__device__ __forceinline__ Float2x fma2(Float2x a, Float2x b, Float2x c) {
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(a.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return a;
+}
+
 // Four consecutive elements.  VEC: p is aligned to them all.
 template <bool VEC>
 __device__ __forceinline__ float4 load4(const float* p) {

@@ -188,13 +188,13 @@ __global__ void __launch_bounds__(256) ssd_rotary_kernel(const __grid_constant__
     }
     const bool normed = NORM && o.gain;
     // a pair (u, v) becomes (u c - v s, v c + u s), with the gains of its elements in the factors
-    float uc[V], vs[V], vc[V], us[V];
+    float uc[V], vs[V], vc[V], us[V];  // vs negative
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const float2 f = turns ? cs[slot * V + j] : make_float2(1.0f, 0.0f);
       const int iu = APART ? at + j : at + 2 * j, iv = APART ? with + j : iu + 1;
       const float gu = NORM ? gain[i * p.r.head_dim + iu] : 1.0f, gv = NORM ? gain[i * p.r.head_dim + iv] : 1.0f;
-      uc[j] = gu * f.x, vs[j] = gv * f.y, vc[j] = gv * f.x, us[j] = gu * f.y;
+      uc[j] = gu * f.x, vs[j] = -(gv * f.y), vc[j] = gv * f.x, us[j] = gu * f.y;
     }
     const T* x = static_cast<const T*>(o.x) + row * o.x_row + (t * in_warp + mine) * o.x_head;
     T* y = static_cast<T*>(o.y) + row * o.y_row + (t * in_warp + mine) * o.y_head;
@@ -214,10 +214,20 @@ __global__ void __launch_bounds__(256) ssd_rotary_kernel(const __grid_constant__
       if (t + stride < turns_of) load(t + stride, x);
       float inv = 1.0f;
       if (normed) {
-        float sum = 0.0f, more = 0.0f;
+        float sum = 0.0f;
+        if constexpr (V % 2 == 0) {
+          Float2x a(0.0f), b(0.0f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum = fmaf(e[j], e[j], sum), more = fmaf(e[V + j], e[V + j], more);
-        sum += more;
+          for (int j = 0; j < V; j += 2) {
+            const Float2x u(e[j], e[j + 1]), v(e[V + j], e[V + j + 1]);
+            a = fma2(u, u, a), b = fma2(v, v, b);
+          }
+          const float2 s = (a + b).get();
+          sum = s.x + s.y;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2 * V; ++j) sum = fmaf(e[j], e[j], sum);
+        }
         if (pow2) {
           for (int d = 1; d < slots; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
         } else {  // sums of the lanes above within the head, then the first lane's
@@ -230,15 +240,28 @@ __global__ void __launch_bounds__(256) ssd_rotary_kernel(const __grid_constant__
         inv = rsqrtf(fmaf(sum, p.per_element, p.r.eps));
       }
       float r[2 * V];
+      if constexpr (APART && V % 2 == 0) {
+        const Float2x f(inv);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int k = APART ? j : 2 * j, l = APART ? V + j : 2 * j + 1;
-        r[k] = e[k] * uc[j], r[l] = e[l] * vc[j];
-        if (turns && (APART || slot * V + j < half)) {
-          r[k] = __fmaf_rn(e[k], uc[j], -__fmul_rn(e[l], vs[j]));
-          r[l] = __fmaf_rn(e[l], vc[j], __fmul_rn(e[k], us[j]));
+        for (int j = 0; j < V; j += 2) {
+          const Float2x u(e[j], e[j + 1]), v(e[V + j], e[V + j + 1]), c(uc[j], uc[j + 1]), d(vc[j], vc[j + 1]);
+          Float2x a = u * c, b = v * d;
+          if (turns) a = fma2(u, c, v * Float2x(vs[j], vs[j + 1])), b = fma2(v, d, u * Float2x(us[j], us[j + 1]));
+          if (NORM) a = a * f, b = b * f;
+          const float2 x2 = a.get(), y2 = b.get();
+          r[j] = x2.x, r[j + 1] = x2.y, r[V + j] = y2.x, r[V + j + 1] = y2.y;
         }
-        if (NORM) r[k] *= inv, r[l] *= inv;
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const int k = APART ? j : 2 * j, l = APART ? V + j : 2 * j + 1;
+          r[k] = e[k] * uc[j], r[l] = e[l] * vc[j];
+          if (turns && (APART || slot * V + j < half)) {
+            r[k] = __fmaf_rn(e[k], uc[j], __fmul_rn(e[l], vs[j]));
+            r[l] = __fmaf_rn(e[l], vc[j], __fmul_rn(e[k], us[j]));
+          }
+          if (NORM) r[k] *= inv, r[l] *= inv;
+        }
       }
       Unit<T, V> ra, rb;
       ra.pack(r), rb.pack(r + V);

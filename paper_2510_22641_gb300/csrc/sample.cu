@@ -58,10 +58,25 @@ struct MassOf {
     const uint32_t t = table[place & (kExpSize - 1)];
     return t + __umulhi(t, __float_as_uint(q) & 0x7fffffu);
   }
+  // Places and digits of two logits, the same bits.
+  __device__ __forceinline__ void two(float l, float m, const uint32_t* table, uint32_t* place, uint32_t* w) const {
+    const Float2x x = Float2x(l, m) + Float2x(-origin), c(c_hi), one(12582912.0f), n = fma2(x, c, one);
+    const Float2x f = fma2(x, Float2x(c_lo), fma2(x, c, fma2(n, Float2x(-1.0f), one)));
+    const Float2x q = fma2(f, fma2(f, fma2(f, Float2x(0.22210662f), Float2x(984.36748f)), Float2x(2908451.0f)),
+                           Float2x(8388608.0f + 1744716.25f));
+    const float2 ns = n.get(), qs = q.get();
+    place[0] = top - __float_as_uint(ns.x), place[1] = top - __float_as_uint(ns.y);
+    const uint32_t t = table[place[0] & (kExpSize - 1)], u = table[place[1] & (kExpSize - 1)];
+    w[0] = t + __umulhi(t, __float_as_uint(qs.x) & 0x7fffffu);
+    w[1] = u + __umulhi(u, __float_as_uint(qs.y) & 0x7fffffu);
+  }
+  static __device__ __forceinline__ uint64_t value(uint32_t w, uint32_t place) {
+    const uint64_t v = static_cast<uint64_t>(w) << 12 >> (place >> kExpBits & 63);
+    return place < kMassPlaces ? v : 0ull;
+  }
   __device__ __forceinline__ uint64_t operator()(float l, const uint32_t* table) const {
     const uint32_t at = place(l);
-    const uint64_t v = static_cast<uint64_t>(digits(l, at, table)) << 12 >> (at >> kExpBits & 63);
-    return at < kMassPlaces ? v : 0ull;
+    return value(digits(l, at, table), at);
   }
 };
 
@@ -293,7 +308,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   };
 
   // The first token in vocabulary order whose running measure (0 of logits below `cut`) exceeds aim(all of it): calls
-  // found(index, logit, all) in one thread of the cluster.
+  // found(index, logit, all) in one thread of the cluster.  measure(l, m, index): of two neighbouring tokens together.
   int uses = 1;
   constexpr int kSeg = kSegUnits * E;
   static_assert(kSeg <= kSampleThreads, "a segment's tokens are looked at by a thread each");
@@ -309,7 +324,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
         for (int e = 0; e < E; ++e) any |= to_f32(x.v[e]) >= cut;
         if (!any) continue;
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum += measure(to_f32(x.v[e]), first_index + u * E + e);
+        for (int e = 0; e < E; e += 2) sum += measure(to_f32(x.v[e]), to_f32(x.v[e + 1]), first_index + u * E + e);
       }
       sum = warp_sum(sum);
       if (lane == 0) sh.seg[s] = sum;
@@ -334,7 +349,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     mine = 0;
     if (tid < kSeg && i < units * E) {
       l = to_f32(reinterpret_cast<const T*>(data)[i]);
-      mine = measure(l, index);
+      mine = measure(l, -INFINITY, index);
     }
     const uint64_t from = sh.before + scan(mine, 1, sum) - mine;
     if (from <= goal && goal < from + mine) found(index, l, all);
@@ -477,12 +492,12 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
       uint32_t v[E], old[E], place[E];
       bool on[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float l = to_f32(x.v[e]);
-        place[e] = mass.place(l);
+      for (int e = 0; e < E; e += 2) {
+        const float l = to_f32(x.v[e]), m = to_f32(x.v[e + 1]);
+        mass.two(l, m, sh.table, place + e, v + e);
         on[e] = place[e] < kMassPlaces && (!limited || kept(l, first_index + u * E + e));
-        v[e] = 1;
-        if (!counting) v[e] = mass.digits(l, place[e], sh.table);
+        on[e + 1] = place[e + 1] < kMassPlaces && (!limited || kept(m, first_index + u * E + e + 1));
+        if (counting) v[e] = v[e + 1] = 1;
       }
       // low halves, and then what they carry: a 64-bit atomic on shared memory is a loop
 #pragma unroll
@@ -553,7 +568,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     const uint64_t m = measure(value), wanted = (goal + m - 1) / m;
     int end = value == cut ? last : vocab - 1;
     if (wanted * m < sh.at) {
-      walk([&](float l, int) -> uint64_t { return l == value; }, [&](uint64_t) { return wanted - 1; },
+      walk([&](float l, float m, int) -> uint64_t { return (l == value) + (m == value); }, [&](uint64_t) { return wanted - 1; },
            [&](int index, float, uint64_t) {
              for (int r = 0; r < ctas; ++r) cluster_store(&sh.sent[uses][0], r, index);
            });
@@ -611,9 +626,11 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   if (top_p < 1.0f)
     shrink(false, [&](uint64_t all) -> uint64_t { return max(times_fraction(all, top_p, true), static_cast<uint64_t>(1)); });
   walk(
-      [&](float l, int index) -> uint64_t {
-        const uint64_t m = mass_of(l);
-        return kept(l, index) && m >= least ? m : 0;
+      [&](float l, float m, int index) -> uint64_t {
+        uint32_t place[2], w[2];
+        mass.two(l, m, sh.table, place, w);
+        const uint64_t a = MassOf::value(w[0], place[0]), b = MassOf::value(w[1], place[1]);
+        return (kept(l, index) && a >= least ? a : 0) + (kept(m, index + 1) && b >= least ? b : 0);
       },
       aim, put);
 }
