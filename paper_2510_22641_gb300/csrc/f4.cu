@@ -138,14 +138,17 @@ __global__ void __launch_bounds__(256) ssd_f4_unpack_kernel(const uint8_t* packe
 
 template <typename T, bool VEC>
 ssd_status f4_pack_dispatch(const char* what, F4PackParams& p, cudaStream_t s) {
-  // one warp a row as long as it holds the row in two chunks a lane; eight from 8 chunks on
-  p.warps_log = p.chunks <= 2 ? 0 : p.chunks <= 4 ? 1 : p.chunks <= 8 ? 2 : 3;
-  const int each = 8 >> p.warps_log;
-  const dim3 grid((p.rows + each - 1) / each);
-  if (p.chunks <= 16) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 2>, grid, 256, 0, s, p);
-  if (p.chunks <= 32) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 4>, grid, 256, 0, s, p);
-  if (p.chunks <= 64) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 8>, grid, 256, 0, s, p);
-  return op_launch(what, ssd_f4_pack_long_kernel<T, VEC>, grid, 256, 0, s, p);
+  // Many rows: as few warps a row as hold it in four chunks a lane, which spreads what a warp does once; few rows: two
+  // chunks, for more warps.
+  const int each = p.rows >= 152 * 8 ? 4 : 2;
+  p.warps_log = 0;
+  while (p.warps_log < 3 && p.chunks > each << p.warps_log) ++p.warps_log;
+  const int in_cta = 8 >> p.warps_log, held = (p.chunks + (1 << p.warps_log) - 1) >> p.warps_log;
+  const dim3 grid((p.rows + in_cta - 1) / in_cta);
+  if (held <= 2) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 2>, grid, 256, 0, s, p);
+  if (held <= 4) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 4>, grid, 256, 0, s, p);
+  if (held <= 8) return op_launch(what, ssd_f4_pack_kernel<T, VEC, 8>, grid, 256, 0, s, p);
+  return op_launch(what, ssd_f4_pack_long_kernel<T, VEC>, dim3(p.rows), 256, 0, s, p);
 }
 
 template <typename T>
