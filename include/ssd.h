@@ -628,7 +628,7 @@ SSD_API ssd_status ssd_f4_pack(const void* x, int type, int rows, int k, int64_t
                                void* cuda_stream);
 
 /* The values of packed rows: out device [rows][k], type SSD_TYPE_* (c * s * rho rounded to it; exact but for rho near
- * the ends of its range). */
+ * the ends of its range).  out and packed must not overlap. */
 SSD_API ssd_status ssd_f4_unpack(const void* packed, int rows, int k, void* out, int type, void* cuda_stream);
 
 /* y = x W^T (+ residual) of packed w [n][k], fp32 sums of the codes' exact products, each row's scaled in fp32.
@@ -636,7 +636,9 @@ SSD_API ssd_status ssd_f4_unpack(const void* packed, int rows, int k, void* out,
  *     16-byte aligned, of this call alone until it has run; few short rows need none, and work is not looked at);
  *     SSD_TYPE_F4: rows packed by ssd_f4_pack (x_row_stride and work are not looked at)
  *   y: device, type SSD_TYPE_BF16 / FP32, [rows][y_row_stride];  residual: device [rows][res_row_stride] of the same
- *     type, or NULL; may be y itself (same rows), else must not overlap it.  y must not overlap x, w or work. */
+ *     type, or NULL; may be y itself (same rows), else must not overlap it.  y must not overlap x, w or work.
+ * The result of a row is the same however many rows come with it up to 128, and from 129 on; the two differ in the order
+ * of sums.  Should a wait inside the kernel run out (two seconds), the sums it waited for are NaN. */
 SSD_API ssd_status ssd_f4_matmul(const void* w, int n, int k, const void* x, int x_type, int rows,
                                  int64_t x_row_stride, void* y, int type, int64_t y_row_stride, const void* residual,
                                  int64_t res_row_stride, void* work, void* cuda_stream);
@@ -702,13 +704,14 @@ typedef struct {
  *   top_p * mass of all of these (all where top_p >= 1); of these those with exp(z - max z) >= min_p; and the first
  *   in any case.  The token is the first kept one in vocabulary order whose running mass of kept ones exceeds
  *   u * the kept mass (the last with mass, should u be 1 or more).
- * temperature <= 0 takes the first-ranked token.  A NaN logit counts as -infinity; rows that have no more than that
+ * temperature <= 0 (or below 2^-100) takes the first-ranked token.  A NaN logit counts as -infinity; rows that have no more than that
  * give token -1 and prob 0.  Where the largest logit is +infinity, those that are share the mass.  NaN settings act as
  * temperature 0, top_p 1, min_p 0, u 0.
  *   logits: device, type SSD_TYPE_*, [rows][row_stride];  u: device fp32 [rows], in [0, 1)
  *   token: device int32 [rows];  prob: device fp32 [rows], the token's share of the kept mass, or NULL
- * Masses are exp(z - max z) to about 2^-33 of themselves or 2^-44, held as integers, so the result does not depend on
- * the order of any sum.  vocab at most SSD_SAMPLE_MAX_VOCAB. */
+ * Masses are exp(z - max z) to about 2^-30 of themselves or 2^-44, held as integers, so the result does not depend on
+ * the order of any sum.  vocab at most SSD_SAMPLE_MAX_VOCAB.  token and prob must not overlap each other or an input.
+ * Should a wait inside the kernel run out (two seconds), the row's token is -1 and its prob NaN. */
 SSD_API ssd_status ssd_sample(const void* logits, int type, int rows, int vocab, int64_t row_stride, const float* u,
                               const ssd_sampling* how, int32_t* token, float* prob, void* cuda_stream);
 

@@ -222,6 +222,8 @@ ssd_status ssd_f4_unpack(const void* packed, int rows, int k, void* out, int typ
   const int size = type == SSD_TYPE_FP32 ? 4 : 2;
   if (!out || !packed || reinterpret_cast<uintptr_t>(packed) % 16 || reinterpret_cast<uintptr_t>(out) % size)
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_f4_unpack: null or unaligned buffer");
+  if (op_overlap({out, 1, 1, 0, 0, static_cast<int64_t>(rows) * k * size}, {packed, 1, 1, 0, 0, ssd_f4_bytes(rows, k)}, 1))
+    return op_fail(SSD_ERR_INVALID_ARG, "ssd_f4_unpack: out overlaps packed");
   const uint8_t* in = static_cast<const uint8_t*>(packed);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   return type == SSD_TYPE_FP32 ? f4_unpack_dispatch(in, rows, k, static_cast<float*>(out), s)

@@ -376,9 +376,15 @@ ssd_status ssd_rotary_apply(const ssd_rotary* r, const ssd_heads* operand, int n
   for (int i = 0; i < n; ++i) {
     const ssd_heads& a = operand[i];
     const OpRows y{a.y, rows, a.heads, a.y_row, a.y_head, r->head_dim};
+    const OpRows bytes{a.y, rows, a.heads, a.y_row * size, a.y_head * size, static_cast<int64_t>(r->head_dim) * size};
+    if (op_overlap(bytes, {pos, rows, r->axes, pos_row * 4, pos_axis * 4, 4}, 1))
+      return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: an output overlaps the positions");
     if (!op_apart(y)) return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: heads of an output overlap");
     for (int j = 0; j < n; ++j) {
       const ssd_heads& b = operand[j];
+      const int64_t gain = r->head_dim * (b.gain_type == SSD_TYPE_FP32 ? 4 : 2);
+      if (b.gain && op_overlap(bytes, {b.gain, 1, 1, 0, 0, gain}, 1))
+        return op_fail(SSD_ERR_INVALID_ARG, "ssd_rotary_apply: an output overlaps a gain");
       const bool same = i == j && a.y == b.x && (rows == 1 || a.y_row == b.x_row) && (a.heads == 1 || a.y_head == b.x_head);
       if ((!same && op_overlap(y, {b.x, rows, b.heads, b.x_row, b.x_head, r->head_dim}, size)) ||
           (j > i && op_overlap(y, {b.y, rows, b.heads, b.y_row, b.y_head, r->head_dim}, size)))

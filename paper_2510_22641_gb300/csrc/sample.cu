@@ -682,6 +682,18 @@ extern "C" ssd_status ssd_sample(const void* logits, int type, int rows, int voc
                           reinterpret_cast<uintptr_t>(how->top_k_rows);
   if (words % 4 || reinterpret_cast<uintptr_t>(logits) % (type == SSD_TYPE_FP32 ? 4 : 2))
     return op_fail(SSD_ERR_INVALID_ARG, "ssd_sample: buffers must be aligned to their elements");
+  const int size = type == SSD_TYPE_FP32 ? 4 : 2;
+  const OpRows in{logits, rows, 1, row_stride * size, 0, static_cast<int64_t>(vocab) * size};
+  auto row_words = [&](const void* a) { return OpRows{a, 1, 1, 0, 0, static_cast<int64_t>(rows) * 4}; };
+  for (const void* y : {static_cast<const void*>(token), static_cast<const void*>(prob)}) {
+    if (!y) continue;
+    bool shared = op_overlap(row_words(y), in, 1) || (y == token && prob && op_overlap(row_words(y), row_words(prob), 1));
+    for (const void* x : {static_cast<const void*>(u), static_cast<const void*>(how->temperature_rows),
+                          static_cast<const void*>(how->top_p_rows), static_cast<const void*>(how->min_p_rows),
+                          static_cast<const void*>(how->top_k_rows)})
+      shared |= x && op_overlap(row_words(y), row_words(x), 1);
+    if (shared) return op_fail(SSD_ERR_INVALID_ARG, "ssd_sample: an output overlaps another buffer");
+  }
   const SampleParams p{logits, row_stride, vocab, u, *how, token, prob};
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   return type == SSD_TYPE_FP32 ? sample_launch<float>(p, rows, s) : sample_launch<__nv_bfloat16>(p, rows, s);

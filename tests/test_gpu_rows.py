@@ -122,6 +122,16 @@ def test_product_of_large_shapes(rows, n, k):
     check_product(w.matmul(x), lib.F4Rows(x).dequantize(), w.dequantize())
 
 
+@pytest.mark.parametrize("n,k", [(4096, 1000), (300, 5120), (22016, 512)])
+def test_rows_of_a_product_do_not_depend_on_their_company(n, k):
+    w, x = lib.F4Weight(normal((n, k), 1, 0.02)), uneven(700, k, 2)
+    few, many = w.matmul(x[:128]), w.matmul(x)
+    for m in (1, 3, 5, 16, 17, 40, 64, 65, 100):
+        assert torch.equal(w.matmul(x[:m]), few[:m]) and torch.equal(w.matmul(x[128 - m:128]), few[128 - m:])
+    for m in (129, 150, 256, 257, 500):
+        assert torch.equal(w.matmul(x[:m]), many[:m])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("rows", [1, 6, 150, 300])
 def test_product_adds_a_residual_and_takes_views(rows, dtype):

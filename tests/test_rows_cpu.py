@@ -63,6 +63,7 @@ def test_pack_refused(l, over):
 
 
 @pytest.mark.parametrize("over", [{"packed": None}, {"out": None}, {"packed": 4104}, {"out": 4098, "type": 1}, {"type": 2},
+                                  {"out": 4096 + 18432}, {"out": 4096 - 512},
                                   {"rows": 0}, {"k": -1}], ids=str)
 def test_unpack_refused(l, over):
     a = dict(packed=4096, rows=4, k=64, out=1 << 20, type=1) | over
@@ -135,7 +136,8 @@ def test_rotary_calls_refused(l):
     bad = [[heads(x=None)], [heads(y=None)], [heads(heads=0)], [heads(x=MB + 1)], [heads(gain=8, gain_type=2)],
            [heads(gain=9, gain_type=0)], [heads(), heads()], [heads(y=MB + 128)], [heads(y=MB, y_head=32)],
            [heads(), heads(x=3 * MB, y=MB)], [heads(), heads(x=2 * MB, y=3 * MB)], [],
-           [heads(y_row=0)], [heads(y_head=0)], [heads(y_row=255)], [heads(y_head=63)], [heads(y_row=64, y_head=64 * 4)],
+           [heads(gain=2 * MB + 64, gain_type=1)], [heads(), heads(x=3 * MB, y=5 * MB, gain=2 * MB + 256 * 8 + 500, gain_type=0)],
+           [heads(y=4 * MB - 2)], [heads(y_row=0)], [heads(y_head=0)], [heads(y_row=255)], [heads(y_head=63)], [heads(y_row=64, y_head=64 * 4)],
            [heads(y_row=-255)]]
     for i, ops in enumerate(bad):
         assert apply(l, r, ops) == INVALID, i
@@ -154,7 +156,9 @@ def test_rotary_calls_refused(l):
 
 @pytest.mark.parametrize("over", [{n: None} for n in ("logits", "u", "token", "how")] +
                          [{"type": 2}, {"rows": -1}, {"vocab": 0}, {"vocab": 262145}, {"logits": MB + 1},
-                          {"logits": MB + 2, "type": 1}, {"u": MB + 2}, {"token": MB + 1}, {"prob": MB + 1}], ids=str)
+                          {"logits": MB + 2, "type": 1}, {"u": MB + 2}, {"token": MB + 1}, {"prob": MB + 1},
+                          {"token": MB + 396}, {"token": 2 * MB + 4}, {"prob": 2 * MB - 4}, {"prob": 3 * MB + 4}, {"prob": MB}],
+                         ids=str)
 def test_sample_refused(l, over):
     how = B.SSDSampling(temperature=1.0, top_p=1.0)
     a = dict(logits=MB, type=0, rows=2, vocab=100, stride=100, u=2 * MB, how=ctypes.byref(how), token=3 * MB, prob=None) | over
@@ -168,6 +172,8 @@ def test_sample_settings_refused(l):
     for name in ("temperature_rows", "top_p_rows", "min_p_rows", "top_k_rows"):
         c = B.SSDSampling.from_buffer_copy(how)
         setattr(c, name, MB + 2)
+        assert l.ssd_sample(MB, 0, 2, 100, 100, 2 * MB, ctypes.byref(c), 3 * MB, None, None) == INVALID
+        setattr(c, name, 3 * MB + 4)
         assert l.ssd_sample(MB, 0, 2, 100, 100, 2 * MB, ctypes.byref(c), 3 * MB, None, None) == INVALID
 
 
