@@ -12,6 +12,9 @@ struct F4PackParams {
   float* rho;
 };
 
+// Packing reads x and writes 0.56 bytes an element; what bounds it is instructions (16 an element, 74 % of the issue
+// slots): 22016 x 4096 bf16 in 50 us (floor 34).  Read twice, eight warps a row, correctly rounded reciprocals: 77.
+//
 // A row is held in registers between its maximum and its codes, by `warps` warps (1, 2, 4 or 8) of up to J chunks of
 // 256 columns each, 8 columns a lane; the CTA has 8 warps.  The row is read once.
 template <typename T, bool VEC, int J>
@@ -77,6 +80,10 @@ __global__ void __launch_bounds__(256) ssd_f4_pack_long_kernel(const F4PackParam
   }
 }
 
+// Reading back writes 4 bytes an element (to fp32) for 0.56 read: 22016 x 4096 in 65 us, 0.94 of the copy rate; eight
+// neighbouring columns a lane, whose stores leave every second 16 bytes to the next instruction, took 81, a column a
+// thread 357.
+//
 // A CTA per record: a warp takes four rows at a time, of each 4 columns a lane and the 4 that are 128 further, so that
 // neighbouring lanes store neighbouring bytes.  Products of code and scale have 6 bits and are exact in fp16.
 template <typename T, bool VEC>

@@ -32,8 +32,7 @@ __device__ __forceinline__ float f4_scaled(float sum, uint32_t rho_x, uint32_t r
 // Whether a scale is within 2^-60 .. 2^60, where a sum may be multiplied by one after the other.
 __device__ __forceinline__ bool f4_plain(uint32_t rho) { return rho - (67u << 23) <= (120u << 23); }
 
-// Bounded waits, of about two seconds: false when they run out.  By the SM's clock: one read of the global timer costs
-// as much as the products of half a stage.
+// Bounded waits, of about two seconds by the SM's clock: false when they run out.
 template <typename F>
 __device__ __forceinline__ bool f4_wait_for(F ready) {
   long long start = 0;
@@ -103,7 +102,9 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr, uint32_t rank) {
 
 // ------------------------------------------------------------------ up to 128 rows
 //
-// A tile is 128 weight rows (the matrix rows, so that few x rows are few columns) by all x rows, up to BN.
+// A tile is 128 weight rows (the matrix rows, so that few x rows are few columns) by all x rows, up to BN.  The bytes of
+// the weights bound it, in time the latency of 16 stages a CTA: 96 rows x 22016 x 4096 take 16.4 us with the packing of
+// x (floor 9.0, two CTAs an SM; with one, in two turns, 23.6), 1 row x 4096 x 4096 6.6 us, of which the weights are 1.4.
 template <int BN>
 struct F4Tile {
   static constexpr int kStages = BN > 64 ? 3 : 4;  // two CTAs an SM
@@ -322,8 +323,13 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
 //
 // Pairs of CTAs, two SMs each, go over tiles of 256 weight rows by 256 x rows, x rows fastest, so that the pairs at work
 // share few weight rows and weights are read from memory once.  A product of the pair takes 128 weight rows and half of the
-// x rows from either CTA's shared memory.  Warp 0 copies, warp 1 of the first CTA issues the products, warps 10..13 move
+// x rows from either CTA's shared memory, half the reading that 128 x 256 tiles need.  Warp 0 copies, warp 1 of the first CTA issues the products, warps 10..13 move
 // the scales, warps 2..9 take a tile's sums into registers and give the tensor memory back before they store them.
+//
+// What bounds it is the matrix pipe (59 % busy) with the barriers around each stage: 5003 x 27648 x 5120 take 277 us with
+// the packing of x (22), 5.1 PFLOP/s (a library bf16 product of that size at its best rate: 730).  Scales copied
+// by tcgen05.cp: 386 (one CTA a tile of 128 x 256, sums read by eight warps; 507 with four, before).  640 x 4096 x 11008,
+// 48 tiles for 76 pairs: 28 us, 51 before.
 
 __device__ __forceinline__ uint32_t cluster_map(const void* p, uint32_t rank) {
   uint32_t a;

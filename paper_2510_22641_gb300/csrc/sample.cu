@@ -1,4 +1,4 @@
-// Sampling: temperature, top-k, top-p, min-p and the draw by a given random number, one pass of rules per row.
+// Sampling: temperature, top-k, top-p, min-p and the draw by a given random number.
 #include <float.h>
 
 #include "lowbit.cuh"
@@ -105,6 +105,12 @@ struct SampleParams {
 };
 
 // ------------------------------------------------------------------ the kernel
+//
+// What bounds it: instructions (28 an element where every token's mass is needed) and the barriers between the steps.
+// 256 rows of 150001 bf16 logits: 33 us for the largest alone (floor 11.4), 50 with top_k 50, 88 when every mass is added
+// up once, 205 with top_p 0.95 (twice, and the border's search); mixed rows 107 (bit by bit over a row that is read
+// again for every bit: 5095).  One row of 32000: 12.9 us, of which clusters' barriers and the first fetch of the code
+// are most.
 //
 // A cluster of CTAs holds a row in shared memory, read from global memory once, with the largest logit found on the way.
 // A rule's border is found by counting: tokens (or their masses) are added up in 704 bins of a sixteenth of an octave of
