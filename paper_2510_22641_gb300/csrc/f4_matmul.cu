@@ -48,13 +48,19 @@ __device__ __forceinline__ bool f4_wait(uint64_t* bar, uint32_t parity) {
   return f4_wait_for([&] { return mbar_try_wait(bar, parity); });
 }
 
-// N sums times their rows' scales (rho: of the x rows, in shared memory); NaN where the sums are not valid.
+// N sums times their rows' scales (rho: of the x rows, in shared memory, 16-byte aligned); NaN where the sums are not
+// valid.
 template <int N>
 __device__ __forceinline__ void f4_scale(float* v, const uint32_t* rho, uint32_t rho_w, bool plain, bool valid) {
-  const float fw = __uint_as_float(rho_w);
   if (plain && valid) {
+    const Float2x fw(__uint_as_float(rho_w));
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = v[j] * __uint_as_float(rho[j]) * fw;
+    for (int j = 0; j < N; j += 4) {
+      const float4 r = *reinterpret_cast<const float4*>(rho + j);
+      const float2 a = (Float2x(v[j], v[j + 1]) * Float2x(r.x, r.y) * fw).get();
+      const float2 b = (Float2x(v[j + 2], v[j + 3]) * Float2x(r.z, r.w) * fw).get();
+      v[j] = a.x, v[j + 1] = a.y, v[j + 2] = b.x, v[j + 3] = b.y;
+    }
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = valid ? f4_scaled(v[j], rho[j], rho_w) : __uint_as_float(0x7fc00000u);
