@@ -329,11 +329,12 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
 //
 // Pairs of CTAs, two SMs each, go over tiles of 256 weight rows by 256 x rows, x rows fastest, so that the pairs at work
 // share few weight rows and weights are read from memory once.  A product of the pair takes 128 weight rows and half of the
-// x rows from either CTA's shared memory, half the reading that 128 x 256 tiles need.  Warp 0 copies, warp 1 of the first CTA issues the products, warps 10..13 move
-// the scales, warps 2..9 take a tile's sums into registers and give the tensor memory back before they store them.
+// x rows from either CTA's shared memory, half the reading that 128 x 256 tiles need.  Warp 0 copies, warp 1 of the first
+// CTA issues the products, warps 10..13 move the scales, warps 2..9 take a tile's sums into registers and give the tensor
+// memory back before they store them.
 //
-// What bounds it is the matrix pipe (59 % busy) with the barriers around each stage: 5003 x 27648 x 5120 take 277 us with
-// the packing of x (22), 5.1 PFLOP/s (a library bf16 product of that size at its best rate: 730).  Scales copied
+// What bounds it is the matrix pipe (59 % busy) with the barriers around each stage: 5003 x 27648 x 5120 take 274 us with
+// the packing of x (22), 5.2 PFLOP/s (a library bf16 product of that size at its best rate: 730).  Scales copied
 // by tcgen05.cp: 386 (one CTA a tile of 128 x 256, sums read by eight warps; 507 with four, before).  640 x 4096 x 11008,
 // 48 tiles for 76 pairs: 28 us, 51 before.
 
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(kF4PairThreads, 1) ssd_f4_matmul_pair_kernel(c
   uint64_t* empty = full + S::kStages;
   uint64_t* scaled = empty + S::kStages;  // a stage's scales are in both CTAs' tensor memory (the first one's barrier)
   uint64_t* done = scaled + S::kStages;   // a tile's sums are complete
-  uint64_t* taken = done + 1;           // and in registers, of both CTAs (the first one's barrier)
+  uint64_t* taken = done + 1;             // and in registers, of both CTAs (the first one's barrier)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(taken + 1);
   volatile int* stop = reinterpret_cast<volatile int*>(tmem_slot + 1);
   uint32_t* rho = reinterpret_cast<uint32_t*>(full) + 64;  // [2][256]: of this tile and of the next
@@ -519,33 +520,53 @@ __global__ void __launch_bounds__(kF4PairThreads, 1) ssd_f4_matmul_pair_kernel(c
           : "=r"(plain)
           : "r"(static_cast<int>(f4_plain(mine) && f4_plain(rho_w)))
           : "memory");
+      // 128 columns a warp
+      const int left = cols - half * (BN / 2);
+      const bool store = n < p.n;
+      [[maybe_unused]] uint32_t h[sizeof(T) == 2 ? BN / 4 : 1];  // pairs of bf16: the residual's, then the results
+      if constexpr (sizeof(T) == 2) {
+        if (p.residual) {
+          const uint16_t* r = static_cast<const uint16_t*>(p.residual) + (m0 + half * (BN / 2)) * p.r_row + n;
+#pragma unroll
+          for (int j = 0; j < BN / 2; j += 2, r += 2 * p.r_row) {
+            const uint32_t a = store && j < left ? *r : 0u, b = store && j + 1 < left ? r[p.r_row] : 0u;
+            h[j / 2] = a | b << 16;
+          }
+        }
+      }
+      // of fp32 residuals 16 are under way ahead of the 16 that are added
+      [[maybe_unused]] float ahead[sizeof(T) == 4 ? 16 : 1];
+      [[maybe_unused]] const T* res = static_cast<const T*>(p.residual) + (m0 + half * (BN / 2)) * p.r_row + n;
+      auto fetch = [&](int from) {
+#pragma unroll
+        for (int j = 0; j < static_cast<int>(sizeof(ahead) / sizeof(float)); ++j)
+          ahead[j] = store && from + j < left ? to_f32(res[(from + j) * p.r_row]) : 0.0f;
+      };
+      if (sizeof(T) == 4 && p.residual) fetch(0);
       const bool ok = !*stop && f4_wait(done, it & 1);  // after a failure the rest is NaN
       tmem_fence_after();
-      // 128 columns a warp, 32 at a time.  bf16 results are scaled and packed as they are read, fp32 ones take two turns
-      // of 64: the registers of 14 warps hold no more.  The tensor memory is given back after the last read.
+      // bf16 results are scaled and packed as they are read, 32 at a time, fp32 ones take two turns of 64: the registers of
+      // 14 warps hold no more.  The tensor memory is given back after the last read.
       const uint32_t from = tmem + (static_cast<uint32_t>(q * 32) << 16) + half * (BN / 2);
-      const int left = cols - half * (BN / 2);
       auto release = [&] {
         tmem_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(taken_bar);
       };
       if (!ok) *stop = 1;
-      const bool store = n < p.n;
       rx += half * (BN / 2);
       if constexpr (sizeof(T) == 2) {
-        uint32_t h[BN / 4];
 #pragma unroll
         for (int c = 0; c < BN / 2; c += 32) {
           float v[32];
           tmem_ld32(from + c, v);
           f4_scale<32>(v, rx + c, rho_w, plain, ok);
-          // residuals are added before the rounding
-          if (p.residual && store)
-            for (int j = 0; j < 32; ++j)
-              if (c + j < left) v[j] += to_f32(static_cast<const T*>(p.residual)[(m0 + half * (BN / 2) + c + j) * p.r_row + n]);
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
+            if (p.residual) {
+              const float2 r = bf16x2_to_float2(h[(c + j) / 2]);
+              v[j] += r.x, v[j + 1] += r.y;
+            }
             const __nv_bfloat162 b = __floats2bfloat162_rn(v[j], v[j + 1]);
             h[(c + j) / 2] = *reinterpret_cast<const uint32_t*>(&b);
           }
@@ -570,12 +591,18 @@ __global__ void __launch_bounds__(kF4PairThreads, 1) ssd_f4_matmul_pair_kernel(c
           tmem_ld32(from + c + 32, v + 32);
           if (c + 64 == BN / 2) release();
           f4_scale<64>(v, rx + c, rho_w, plain, ok);
-          if (!store) continue;
           T* y = static_cast<T*>(p.y) + (m0 + half * (BN / 2) + c) * p.y_row + n;
-          const T* r = static_cast<const T*>(p.residual) + (m0 + half * (BN / 2) + c) * p.r_row + n;
 #pragma unroll
-          for (int j = 0; j < 64; ++j, y += p.y_row)
-            if (c + j < left) *y = p.residual ? v[j] + r[j * p.r_row] : v[j];
+          for (int b = 0; b < 64; b += 16) {
+            if (p.residual) {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) v[b + j] += ahead[j];
+              if (c + b + 16 < BN / 2) fetch(c + b + 16);
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j, y += p.y_row)
+              if (store && c + b + j < left) *y = v[b + j];
+          }
         }
       }
     }
