@@ -67,27 +67,41 @@ __device__ __forceinline__ void f4_scale(float* v, const uint32_t* rho, uint32_t
   }
 }
 
-// Stores N sums of weight row n and x rows m .. m + count - 1.  rho: of the x rows, in shared memory.  plain: both
-// rows' scales are f4_plain.
+// Stores N sums of weight row n and x rows m .. m + count - 1, res (0 where there is none) added.  rho: of the x rows, in
+// shared memory.  plain: both rows' scales are f4_plain.
 template <typename T, int N>
-__device__ __forceinline__ void f4_store(const F4MatmulParams& p, int m, int n, int count, const float* v,
+__device__ __forceinline__ void f4_store(const F4MatmulParams& p, int m, int n, int count, const float* v, const float* res,
                                          const uint32_t* rho, uint32_t rho_w, bool plain) {
   T* y = static_cast<T*>(p.y) + m * p.y_row + n;
   const float fw = __uint_as_float(rho_w);
-  if (plain && count >= N && !p.residual) {
+  if (plain && count >= N) {
+    T out[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j, y += p.y_row) *y = from_f32<T>(v[j] * __uint_as_float(rho[j]) * fw);
-  } else {
-    const T* r = static_cast<const T*>(p.residual);
-    if (r) r += m * p.r_row + n;
-#pragma unroll
-    for (int j = 0; j < N; ++j, y += p.y_row) {
-      if (j >= count) break;
-      const float s = f4_scaled(v[j], rho[j], rho_w);
-      *y = from_f32<T>(r ? s + to_f32(*r) : s);
-      r += r ? p.r_row : 0;
+    for (int j = 0; j < N; ++j) {
+      const float s = v[j] * __uint_as_float(rho[j]) * fw;
+      out[j] = from_f32<T>(p.residual ? s + res[j] : s);
     }
+#pragma unroll
+    for (int j = 0; j < N; ++j, y += p.y_row) *y = out[j];
+    return;
   }
+#pragma unroll
+  for (int j = 0; j < N; ++j, y += p.y_row) {
+    if (j >= count) break;
+    const float s = plain ? v[j] * __uint_as_float(rho[j]) * fw : f4_scaled(v[j], rho[j], rho_w);
+    *y = from_f32<T>(p.residual ? s + res[j] : s);
+  }
+}
+// Its residuals, all under way at once.
+template <typename T, int N>
+__device__ __forceinline__ void f4_residual(const F4MatmulParams& p, int m, int n, int count, float* res) {
+  const T* r = static_cast<const T*>(p.residual) + m * p.r_row + n;
+  T in[N] = {};
+#pragma unroll
+  for (int j = 0; j < N; ++j, r += p.r_row)
+    if (j < count) in[j] = *r;
+#pragma unroll
+  for (int j = 0; j < N; ++j) res[j] = to_f32(in[j]);
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -269,6 +283,9 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
     bool plain = f4_plain(rho_w);
     for (int i = 0; i < cols; ++i) plain &= f4_plain(rho[i]);
     plain = __all_sync(~0u, plain || n >= p.n);
+    float res[16] = {};
+    const bool add = p.residual && split == 1 && n < p.n;
+    if (add) f4_residual<T, 16>(p, 0, n, cols, res);
     ok = ok && f4_wait(done, 0);
     tmem_fence_after();
     for (int c = 0; c < nn; c += 16) {
@@ -280,7 +297,8 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
 #pragma unroll
         for (int j = 0; j < 16; ++j) part[(c + j) * kF4Rows + q * 32 + lane] = v[j];
       } else if (n < p.n) {
-        f4_store<T, 16>(p, c, n, cols - c, v, rho + c, rho_w, plain);
+        f4_store<T, 16>(p, c, n, cols - c, v, res, rho + c, rho_w, plain);
+        if (add) f4_residual<T, 16>(p, c + 16, n, cols - c - 16, res);
       }
     }
   }
@@ -298,6 +316,13 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
     constexpr int kAhead = 4;
     for (int i = i0 + warp; i < i1; i += kAhead * 6) {
       float4 v[kAhead] = {};
+      float res[kAhead][4] = {};
+      if (p.residual)
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (i + 6 * k < i1 && n + j < p.n) f4_residual<T, 1>(p, i + 6 * k, n + j, 1, &res[k][j]);
       for (int r = 0; r < split; ++r) {
         float4 t[kAhead];
 #pragma unroll
@@ -313,7 +338,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
         const float s[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (n + j < p.n) f4_store<T, 1>(p, i + 6 * k, n + j, 1, s + j, rho + i + 6 * k, rho_w[j], false);
+          if (n + j < p.n) f4_store<T, 1>(p, i + 6 * k, n + j, 1, s + j, &res[k][j], rho + i + 6 * k, rho_w[j], false);
       }
     }
     __syncwarp();

@@ -42,7 +42,7 @@ __device__ __forceinline__ void turn_of(int pos, uint64_t step, float& c, float&
   if (quarter & 2) s = -s;
 }
 
-// One product rounded, the other not, in every kernel alike: a call's bits do not depend on its alignment.
+// One product rounded, the other not, in every kernel alike: without norms a call's bits do not depend on its alignment.
 __device__ __forceinline__ void turn_pair(float u, float v, float c, float s, float& a, float& b) {
   a = __fmaf_rn(u, c, -__fmul_rn(v, s));
   b = __fmaf_rn(v, c, __fmul_rn(u, s));
