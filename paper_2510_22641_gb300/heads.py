@@ -7,6 +7,7 @@ asynchronously, keep nothing between calls and may be captured into a CUDA graph
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Sequence
 
 import torch
@@ -15,7 +16,9 @@ from . import _binding as B
 from .lowbit import _call, _fail, _rows2, _rows3, _type
 
 
-_Heads = B.SSDHeads * 2
+# Fields of ssd_heads and ssd_sampling as bytes: filling a ctypes structure takes longer than the call it is for.
+_HEADS = "PPi4xqqqqPi4x"
+_one, _two, _sampling = (struct.Struct(f).pack for f in (_HEADS, 2 * _HEADS, "fffiPPPP"))
 
 
 class Rotary:
@@ -74,10 +77,10 @@ class Rotary:
         if k is None:
             if k_out is not None or k_gain is not None:
                 _fail("k: missing")
-            both = _Heads(first)
+            both = _one(*first)
         else:
             k_out, second = self._operand(k, k_out, k_gain, rows, i, q.dtype, "k")
-            both = _Heads(first, second)
+            both = _two(*first, *second)
         _call(i, self.lib.ssd_rotary_apply, self._ref, both, 1 if k is None else 2, code, rows, pos.data_ptr(), pst[0],
               pst[1] if len(pst) > 1 else 0)
         return q_out, k_out
@@ -96,7 +99,7 @@ class Rotary:
             y_row, y_head, _ = _rows3(y, (rows, heads, d), index, what + "_out")
             if y.dtype is not dtype:
                 _fail(f"{what}_out: {dtype} expected, got {y.dtype}")
-        g, g_type = None, 0
+        g = g_type = 0
         if gain is not None:
             if gain.shape != (d,) or gain.get_device() != index or not gain.is_contiguous():
                 _fail(f"{what}_gain: contiguous [{d}] on {x.device} expected, got {tuple(gain.shape)} on {gain.device}")
@@ -122,7 +125,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: float | torch.Ten
         return t.data_ptr()
 
     tensor, f32, i32 = torch.Tensor, torch.float32, torch.int32
-    t_rows = p_rows = m_rows = k_rows = None
+    t_rows = p_rows = m_rows = k_rows = 0
     if isinstance(temperature, tensor):
         temperature, t_rows = 0.0, per_row(temperature, f32, "temperature")
     if isinstance(top_p, tensor):
@@ -131,11 +134,11 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: float | torch.Ten
         min_p, m_rows = 0.0, per_row(min_p, f32, "min_p")
     if isinstance(top_k, tensor):
         top_k, k_rows = 0, per_row(top_k, i32, "top_k")
-    how = B.SSDSampling(temperature, top_p, min_p, top_k, t_rows, p_rows, m_rows, k_rows)
+    how = _sampling(temperature, top_p, min_p, top_k, t_rows, p_rows, m_rows, k_rows)
     if out is None:
         out = torch.empty(one, dtype=i32, device=device)
     prob = torch.empty(one, dtype=f32, device=device) if with_prob else None
     _call(i, lib.ssd_sample, logits.data_ptr(), _type(logits.dtype, "logits"), rows, vocab,
-          _rows2(logits, (rows, vocab), i, "logits"), per_row(u, f32, "u"), ctypes.byref(how), per_row(out, i32, "out"),
+          _rows2(logits, (rows, vocab), i, "logits"), per_row(u, f32, "u"), how, per_row(out, i32, "out"),
           None if prob is None else prob.data_ptr())
     return (out, prob) if with_prob else out

@@ -30,6 +30,18 @@ def test_structs_match_the_header(tmp_path):
             assert c[(n, f)] == getattr(t, f).offset, (n, f)
 
 
+def test_fields_as_bytes_match_the_structs():
+    from paper_2510_22641_gb300 import heads
+    v = (11, 12, 13, -14, 15, -16, 17, 18, 1)
+    two = (B.SSDHeads * 2).from_buffer_copy(heads._two(*v, *v))
+    assert heads._one(*v) == bytes(two)[:ctypes.sizeof(B.SSDHeads)]
+    for h in two:
+        assert tuple(getattr(h, f) for f, _ in B.SSDHeads._fields_) == v
+    s = B.SSDSampling.from_buffer_copy(heads._sampling(0.5, 0.25, 0.125, -7, 21, 22, 23, 24))
+    assert [getattr(s, f) for f, _ in B.SSDSampling._fields_] == [0.5, 0.25, 0.125, -7, 21, 22, 23, 24]
+    assert len(heads._sampling(0, 0, 0, 0, 0, 0, 0, 0)) == ctypes.sizeof(B.SSDSampling)
+
+
 def test_packed_sizes(l):
     record = 128 * 256 // 2 + 128 * 256 // 16
     assert l.ssd_f4_bytes(1, 1) == record + 128 * 4
