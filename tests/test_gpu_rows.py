@@ -423,3 +423,55 @@ def test_streams_and_graphs_of_sampling():
     g.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+# ----------------------------------------------------------------------------------------- large operands
+
+def test_offsets_past_32_bits():
+    """More than 2^31 elements in every operand that can have them; the last rows are looked at."""
+    some = normal((40, 16384), 1).to(torch.bfloat16)
+    x = torch.zeros(132000, 16384, dtype=torch.bfloat16, device="cuda")
+    x[-40:] = some
+    p = lib.F4Rows(x)
+    w = lib.F4Weight(normal((32, 16384), 2))
+    want = lib.F4Rows(some).dequantize()
+    y = w.matmul(p)
+    check_product(y[-40:], want, w.dequantize())
+    assert not y[:-40].any()
+    assert torch.equal(p.dequantize(torch.bfloat16)[-40:].float(), want)
+    del x, p, y
+    xs, wide = normal((8200, 64), 3), lib.F4Weight(normal((263000, 64), 4))
+    y = wide.matmul(xs)
+    check_product(y[-2:], lib.F4Rows(xs).dequantize()[-2:], wide.dequantize())
+    del y, wide
+    torch.cuda.empty_cache()
+    heads = torch.zeros(300000, 64, 128, dtype=torch.bfloat16, device="cuda")
+    heads[-3:] = normal((3, 64, 128), 5)
+    pos = torch.arange(300000, dtype=torch.int32, device="cuda")
+    last = lib.Rotary(128).rotate(heads[-3:].contiguous(), None, pos[-3:])[0]
+    assert torch.equal(lib.Rotary(128).rotate(heads, None, pos, q_out=heads)[0][-3:], last)
+    del heads
+    torch.cuda.empty_cache()
+    z = torch.zeros(8200, 262144, device="cuda")
+    z[-5:] = logits_of(5, 262144, 6)
+    u = torch.rand(8200, generator=torch.Generator().manual_seed(7)).cuda()
+    token, prob = lib.sample(z, u, 1.0, 0, 0.9, 0.0, with_prob=True)
+    check_tokens(z[-5:], u[-5:], (1.0, 0, 0.9, 0.0), (token[-5:], prob[-5:]))
+    flat = token[:-5].cpu().numpy()
+    kept = math.ceil(float(np.float32(0.9)) * 262144)   # equal logits: the first of them by index
+    assert np.array_equal(flat, np.minimum(np.floor(u[:-5].cpu().double().numpy() * kept), kept - 1).astype(np.int32))
+
+
+def test_two_large_products_at_once():
+    w = [lib.F4Weight(normal((3000, 2048), s, 0.02)) for s in (1, 2)]
+    x = [normal((m, 2048), m) for m in (900, 700)]
+    want = [a.matmul(b) for a, b in zip(w, x)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in w]
+    for _ in range(10):
+        got = []
+        for s, a, b in zip(streams, w, x):
+            with torch.cuda.stream(s):
+                got.append(a.matmul(b))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
