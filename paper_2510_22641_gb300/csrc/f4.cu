@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(256) ssd_f4_pack_long_kernel(const F4PackParam
 //
 // A CTA per record: a warp takes four rows at a time, of each 4 columns a lane and the 4 that are 128 further, so that
 // neighbouring lanes store neighbouring bytes.  Products of code and scale have 6 bits and are exact in fp16.
-template <typename T, bool VEC>
+template <typename T>
 __global__ void __launch_bounds__(256) ssd_f4_unpack_kernel(const uint8_t* packed, int rows, int k, int chunks,
                                                             const float* rho, T* out) {
   pdl_wait();
@@ -126,18 +126,62 @@ __global__ void __launch_bounds__(256) ssd_f4_unpack_kernel(const uint8_t* packe
         }
         T* y = out + static_cast<int64_t>(r) * k + 128 * h;
         const int left = k - col - 128 * h;
-        if (VEC && left >= 4) {
-          if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
-          } else {
-            const __nv_bfloat162 b[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
-            *reinterpret_cast<uint2*>(y) = *reinterpret_cast<const uint2*>(b);
-          }
+        if (left <= 0) continue;  // k is a multiple of four
+        if constexpr (sizeof(T) == 4) {
+          *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
         } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (j < left) y[j] = from_f32<T>(v[j]);
+          const __nv_bfloat162 b[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
+          *reinterpret_cast<uint2*>(y) = *reinterpret_cast<const uint2*>(b);
         }
+      }
+    }
+  }
+}
+
+// Rows that are not aligned to four elements: a lane decodes 8 columns, and the warp stores 32 neighbouring ones at a time,
+// by way of shared memory.
+template <typename T>
+__global__ void __launch_bounds__(256) ssd_f4_unpack_odd_kernel(const uint8_t* packed, int rows, int k, int chunks,
+                                                                const float* rho, T* out) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ float turn[8][kF4Cols];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x, tile = blockIdx.y;
+  const int left = k - chunk * kF4Cols, end = min(rows - tile * kF4Rows, kF4Rows);
+  const uint8_t* at = packed + (static_cast<int64_t>(tile) * chunks + chunk) * kF4Record;
+  rho += static_cast<int64_t>(tile) * kF4Rows;
+  out += static_cast<int64_t>(tile) * kF4Rows * k + chunk * kF4Cols;
+  for (int r0 = warp; r0 < end; r0 += 32) {
+    uint32_t codes[4], scale[4];
+    float f[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = min(r0 + 8 * j, end - 1);
+      codes[j] = *reinterpret_cast<const uint32_t*>(at + f4_code_byte(r, lane * 8));
+      scale[j] = at[f4_scale_byte(r, lane * 8)];
+      f[j] = rho[r];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (r0 + 8 * j >= end) break;
+      const __half2 s = __half2half2(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(scale[j]), __NV_E4M3)));
+      float2 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __half2 c(__nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(codes[j] >> (8 * i)), __NV_E2M1));
+        v[i] = __half22float2(__hmul2(c, s));
+      }
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        reinterpret_cast<float4*>(turn[warp])[lane * 2 + i] =
+            make_float4(v[2 * i].x * f[j], v[2 * i].y * f[j], v[2 * i + 1].x * f[j], v[2 * i + 1].y * f[j]);
+      __syncwarp();
+      T* y = out + static_cast<int64_t>(r0 + 8 * j) * k + lane;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (32 * i >= left) break;
+        if (32 * i + lane < left) y[32 * i] = from_f32<T>(turn[warp][32 * i + lane]);
       }
     }
   }
@@ -169,8 +213,8 @@ ssd_status f4_unpack_dispatch(const uint8_t* in, int rows, int k, T* out, cudaSt
     const uint8_t* at = in + static_cast<int64_t>(first / kF4Rows) * chunks * kF4Record;
     T* y = out + static_cast<int64_t>(first) * k;
     const ssd_status e =
-        vec ? op_launch("ssd_f4_unpack", ssd_f4_unpack_kernel<T, true>, grid, 256, 0, s, at, n, k, chunks, rho + first, y)
-            : op_launch("ssd_f4_unpack", ssd_f4_unpack_kernel<T, false>, grid, 256, 0, s, at, n, k, chunks, rho + first, y);
+        vec ? op_launch("ssd_f4_unpack", ssd_f4_unpack_kernel<T>, grid, 256, 0, s, at, n, k, chunks, rho + first, y)
+            : op_launch("ssd_f4_unpack", ssd_f4_unpack_odd_kernel<T>, grid, 256, 0, s, at, n, k, chunks, rho + first, y);
     if (e) return e;
   }
   return SSD_OK;

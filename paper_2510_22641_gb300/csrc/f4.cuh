@@ -34,13 +34,32 @@ template <typename T>
 struct Raw8 {
   uint32_t w[2 * sizeof(T)];
 
-  // From `col` on, zeros past k.  VEC: 16-byte aligned.
+  // From `col` on, zeros past k.  VEC: 16-byte aligned.  Else the 16-byte pieces that hold the columns are read, where
+  // they lie within the row, and moved into place (a row's lanes are all off by as much); the columns at a row's ends
+  // and those of short rows, which are mostly ends, are read one by one (9000 x 14335, packed and read back: 310 us with
+  // all of them so, and with lanes' own stores, 242 now).
   template <bool VEC>
   __device__ __forceinline__ void load(const T* p, int col, int k) {
     if (VEC && col + 8 <= k) {
 #pragma unroll
       for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i)
         reinterpret_cast<uint4*>(w)[i] = reinterpret_cast<const uint4*>(p + col)[i];
+      return;
+    }
+    constexpr int kWords = 2 * sizeof(T);
+    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(p + col) & 15), at = col * static_cast<int>(sizeof(T)) - off;
+    if (!VEC && k >= 512 && at >= 0 && at + 4 * kWords + 16 <= k * static_cast<int>(sizeof(T))) {
+      const uint4* in = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) + at);
+      uint4 v[kWords / 4 + 1];
+#pragma unroll
+      for (int i = 0; i <= kWords / 4; ++i) v[i] = in[i];
+      uint32_t* u = reinterpret_cast<uint32_t*>(v);
+#pragma unroll
+      for (int i = 0; i < kWords + 3; ++i) u[i] = off & 4 ? u[i + 1] : u[i];
+#pragma unroll
+      for (int i = 0; i < kWords + 1; ++i) u[i] = off & 8 ? u[i + 2] : u[i];
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = sizeof(T) == 4 ? u[i] : __funnelshift_r(u[i], u[i + 1], 8 * (off & 2));
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {

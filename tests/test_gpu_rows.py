@@ -37,7 +37,7 @@ def check_packed(x):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("rows,k", [(1, 1), (1, 16), (3, 17), (16, 256), (7, 257), (130, 512), (129, 1000), (5, 2055),
-                                    (300, 48), (2, 14336), (1, 40000)])
+                                    (300, 48), (2, 14336), (1, 40000), (33, 1001), (17, 3001), (9, 513), (300, 2)])
 def test_pack_equals_the_reference(rows, k, dtype):
     check_packed(uneven(rows, k, rows + k, DT[dtype]))
 
