@@ -9,16 +9,18 @@ namespace {
 // ------------------------------------------------------------------ masses
 //
 // The mass of a token is exp((l - top) / T) up to a factor that is the same for the whole row, as an integer with 44 bits
-// after the point, so that sums are exact in any order.  With c = 1024 log2(e) / T as a pair of floats, n = l c rounded to
-// an integer, f = l c - n (by fused multiply-adds, to 2^-25) and a token's place n(top) - n(l),
+// after the point, so that sums are exact in any order.  With c = 1024 log2(e) / T as a pair of floats, n = l c_hi rounded
+// to an integer, f = l c - n (by fused multiply-adds, to 2^-25) and a token's place n(top) - n(l),
 //   exp(l / T) 2^(-n(top) / 1024) = 2^-(place >> 10) * 2^(-(place & 1023) / 1024) * 2^(f / 1024):
-// a table of 1024 values, a polynomial, one multiplication, one shift.
+// a table of 1024 values, a polynomial, one multiplication, one shift.  |f| is at most 1/2 + |l c_lo|, and c_lo at most
+// 1.22 * 2^-24 c, so with |l c| below 2^20 + 44 * 1024 it stays below 0.58.  (Up to 2^21 it reached 0.65, past the 0.6 that
+// the polynomial is moved by, where a mass was off by 2^-9.)
 
 constexpr int kExpBits = 10, kExpSize = 1 << kExpBits;
 struct ExpTable {
   uint32_t v[kExpSize];
 };
-// 2^(-j / 1024) * 2^32, less so that a value times 2^(1.11 / 1024) still fits 32 bits (the common factor cancels).  The
+// 2^(-j / 1024) * 2^32, less so that a value times 2^((0.6 + f) / 1024), at most 2^(1.18 / 1024), fits 32 bits (the common factor cancels).  The
 // Taylor series of e^x, 0 <= x < ln 2, in 64 bits when this is compiled.
 constexpr ExpTable make_exp_table() {
   ExpTable t = {};
@@ -39,8 +41,8 @@ __device__ constexpr ExpTable kExpTable = make_exp_table();
 constexpr uint32_t kMassPlaces = 44u << kExpBits;
 
 struct MassOf {
-  float origin;      // 0; the largest logit where c times it leaves the integers below 2^22 (then l - origin is exact
-                     // wherever there is mass)
+  float origin;      // 0; the largest logit where c times it is 2^20 or more (then l - origin is exact wherever there is
+                     // mass)
   float c_hi, c_lo;  // 1024 log2(e) / T
   uint32_t top;      // bits of the largest logit's `number`
 
@@ -273,7 +275,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     const float t = one ? 1.0f : temp;
     mass.c_hi = kHigh / t;
     mass.c_lo = (fmaf(-mass.c_hi, t, kHigh) + kLow) / t;
-    mass.origin = fabsf(top * mass.c_hi) < 2097152.0f || isinf(top) ? 0.0f : top;
+    mass.origin = fabsf(top * mass.c_hi) < 1048576.0f || isinf(top) ? 0.0f : top;
     mass.top = __float_as_uint(mass.number(top));
   }
   // kept: logits above `cut`, and of those equal to it the tokens up to `last`
