@@ -272,7 +272,8 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     // 1024 log2(e) / T by the remainder of the rounded quotient
     constexpr double kScale = 1024.0 * 1.4426950408889634074;
     constexpr float kHigh = static_cast<float>(kScale), kLow = static_cast<float>(kScale - static_cast<double>(kHigh));
-    const float t = one ? 1.0f : temp;
+    // Beside an infinite logit no finite one has mass, at any temperature: the largest keeps them all from infinity.
+    const float t = one ? 1.0f : isinf(top) ? FLT_MAX : temp;
     mass.c_hi = kHigh / t;
     mass.c_lo = (fmaf(-mass.c_hi, t, kHigh) + kLow) / t;
     mass.origin = fabsf(top * mass.c_hi) < 1048576.0f || isinf(top) ? 0.0f : top;

@@ -19,3 +19,17 @@ def test_rows_far_from_zero(temperature, dtype):
     u = torch.rand(rows, generator=torch.Generator().manual_seed(2)).cuda()
     for how in ((temperature, 0, 1.0, 0.0), (temperature, 0, 0.6, 0.0), (temperature, 40, 0.9, 0.2)):
         check_tokens(z, u, how, lib.sample(z, u, *how, with_prob=True))
+
+
+def test_infinities_beside_the_largest_values():
+    """Infinite logits share the mass however large the finite ones are and whatever the temperature; a temperature of
+    infinity leaves finite logits equal."""
+    inf, nan, most = float("inf"), float("nan"), 3.4e38
+    rows = [[inf, most, inf, -most], [most, inf, 1e36, nan], [-inf, nan, inf, most], [1.0, most, inf, inf],
+            [1.0, -most, nan, 2.0], [-inf, 5.0, -5.0, most]]
+    z = torch.tensor(rows, device="cuda")
+    for v in (0.0, 0.3, 0.6, 0.99):
+        u = torch.full((len(rows),), v, device="cuda")
+        for t in (1.0, 1e-25, 1e25, inf):
+            for how in ((t, 0, 1.0, 0.0), (t, 0, 0.45, 0.0), (t, 3, 0.8, 0.1)):
+                check_tokens(z, u, how, lib.sample(z, u, *how, with_prob=True))
