@@ -72,6 +72,13 @@ struct MassOf {
     w[0] = t + __umulhi(t, __float_as_uint(qs.x) & 0x7fffffu);
     w[1] = u + __umulhi(u, __float_as_uint(qs.y) & 0x7fffffu);
   }
+  // A mass in whole units of 2^-44 from its 12th octave on, where they fit 32 bits, and before that in digits, which are
+  // exact: sums of these are sums of values, in any order and grouping.  (Digits added up and then shifted keep the bits
+  // below 2^-44, as many as their sums are cut into: borders could move by a token with the number of CTAs.)
+  static __device__ __forceinline__ uint32_t units(uint32_t w, uint32_t place) {
+    return __funnelshift_rc(w, 0u, max(static_cast<int>(place >> kExpBits) - 12, 0));
+  }
+  static __device__ __forceinline__ int unit_bits(int bin) { return max(12 - (bin >> 4), 0); }  // of a bin's units
   static __device__ __forceinline__ uint64_t value(uint32_t w, uint32_t place) {
     const uint64_t v = static_cast<uint64_t>(w) << 12 >> (place >> kExpBits & 63);
     return place < kMassPlaces ? v : 0ull;
@@ -382,11 +389,12 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   }
 
   // Adds up the cluster's bins of this step, finds the one in which the running measure reaches goal_of(all of it) (1 or
-  // more; 0: none) and returns the goal.  masses: bin b holds digits, which belong 12 - (b >> 4) places to the left.  Every CTA gets the others' sums over groups of bins, and reads one group.
+  // more; 0: none) and returns the goal.  masses: the bins hold MassOf::units.  Every CTA gets the others' sums over groups
+  // of bins, and reads one group.
   int step = 0;
   auto find_bin = [&](bool masses, auto goal_of) -> uint64_t {
     const int b = step & 1;
-    auto value_of = [&](uint64_t v, int bin) { return masses ? v << 12 >> (bin >> 4) : v; };
+    auto value_of = [&](uint64_t v, int bin) { return masses ? v << MassOf::unit_bits(bin) : v; };
     __syncthreads();
     {
       uint64_t v = lane < kGroup ? value_of(sh.bin[b][warp * kGroup + lane], warp * kGroup + lane) : 0;
@@ -506,7 +514,8 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
         mass.two(l, m, sh.table, place + e, v + e);
         on[e] = place[e] < kMassPlaces && (!limited || kept(l, first_index + u * E + e));
         on[e + 1] = place[e + 1] < kMassPlaces && (!limited || kept(m, first_index + u * E + e + 1));
-        if (counting) v[e] = v[e + 1] = 1;
+        v[e] = counting ? 1 : MassOf::units(v[e], place[e]);
+        v[e + 1] = counting ? 1 : MassOf::units(v[e + 1], place[e + 1]);
       }
       // low halves, and then what they carry: a 64-bit atomic on shared memory is a loop
 #pragma unroll
@@ -519,9 +528,13 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     if (goal == 0) return;
     goal -= sh.before;
     const int bin = sh.border;
-    // within the bin masses are their digits, which all belong equally far to the left
-    if (!counting) goal = ((goal << (bin >> 4)) + 4095) >> 12;
-    auto measure = [&](float l) -> uint64_t { return counting ? 1u : mass.digits(l, mass.place(l), sh.table); };
+    // within the bin masses are in its units
+    const int bits = counting ? 0 : MassOf::unit_bits(bin);
+    goal = (goal + (1u << bits) - 1) >> bits;
+    auto measure = [&](float l) -> uint64_t {
+      const uint32_t at = mass.place(l);
+      return counting ? 1u : MassOf::units(mass.digits(l, at, sh.table), at);
+    };
     const float low = low_of(bin), high = high_of(bin);
     auto in_bin = [&](float l, int index) { return mass.place(l) >> 6 == static_cast<uint32_t>(bin) && kept(l, index); };
     limited = true;
