@@ -13,7 +13,7 @@ from typing import Sequence
 import torch
 
 from . import _binding as B
-from .lowbit import _call, _fail, _rows2, _rows3, _type
+from .lowbit import _INT, _call, _fail, _ints, _rows2, _rows3, _type
 
 
 # Fields of ssd_heads and ssd_sampling as bytes: filling a ctypes structure takes longer than the call it is for.
@@ -36,6 +36,7 @@ class Rotary:
         if sections is not None and axes is not None:
             _fail("sections or axes expected, not both")
         n = 1 if sections is None else len(sections)
+        _ints(head_dim=head_dim, rotary_dim=turn, **{f"sections[{a}]": v for a, v in enumerate(sections or ())})
         section = None if sections is None else (ctypes.c_int * n)(*sections)
         self._c = B.SSDRotary()
         if self.lib.ssd_rotary_init(ctypes.byref(self._c), head_dim, turn, int(interleaved), n, section, theta, eps):
@@ -69,6 +70,8 @@ class Rotary:
         rows = q.shape[0] if q.dim() else 0
         if i < 0:
             _fail(f"q: a CUDA tensor expected, got {q.device}")
+        if rows > _INT:
+            _fail(f"q: {rows} rows")
         ps, pst = pos.shape, pos.stride()
         if pos.dtype is not torch.int32 or pos.get_device() != i or \
                 (ps != (rows, self.axes) and (self.axes != 1 or ps != (rows,))):
@@ -91,6 +94,8 @@ class Rotary:
         if len(shape) != 3 or x.dtype is not dtype:
             _fail(f"{what}: {dtype} [rows][heads][{d}] expected, got {x.dtype} {tuple(shape)}")
         heads = shape[1]
+        if heads > _INT:
+            _fail(f"{what}: {heads} heads")
         xs = _rows3(x, (rows, heads, d), index, what)
         if y is None:
             y = torch.empty(shape, dtype=dtype, device=x.device)
@@ -117,6 +122,8 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: float | torch.Ten
     if i < 0 or logits.dim() != 2:
         _fail(f"logits: [rows][vocab] on a GPU expected, got {tuple(logits.shape)} on {logits.device}")
     rows, vocab = logits.shape
+    if rows > _INT or vocab > _INT:
+        _fail(f"logits: {rows} rows of {vocab}")
     one, device = (rows,), logits.device
 
     def per_row(t: torch.Tensor, dtype: torch.dtype, what: str) -> int:

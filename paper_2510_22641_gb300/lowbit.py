@@ -35,6 +35,15 @@ def _call(index: int, entry, *args):
         raise B.SSDError(status, B.load().ssd_op_last_error().decode())
 
 
+_INT = 0x7fffffff   # the library's sizes are C ints, into which ctypes cuts larger numbers without a word
+
+
+def _ints(**sizes: int) -> None:
+    for what, v in sizes.items():
+        if not -_INT - 1 <= v <= _INT:
+            _fail(f"{what}: {v} is out of range")
+
+
 # The checks below run on every call of a decode loop: they compare whole shapes and device indices.
 
 def _rows3(t: torch.Tensor, shape: tuple, index: int, what: str) -> tuple:
@@ -70,6 +79,7 @@ class KV8Step:
     KV8Cache.plan fills."""
 
     def __init__(self, cache: KV8Cache, batch: int, rows: int, rows_per_request: int | None = None, row_tile: int = 0):
+        _ints(batch=batch, rows=rows)
         n = B.load().ssd_kv8_step_ints(batch, rows)
         if n < 0 or batch > cache.max_batch:
             _fail(f"step of {rows} rows of {batch} requests (the cache has {cache.max_batch} seats)")
@@ -107,6 +117,8 @@ class KV8Cache:
     def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, block_tokens: int, n_blocks: int,
                  max_batch: int, max_blocks: int, device: torch.device | str = "cuda"):
         self.lib = B.load()
+        _ints(n_layers=n_layers, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, block_tokens=block_tokens,
+              n_blocks=n_blocks, max_batch=max_batch, max_blocks=max_blocks)
         self.n_layers, self.n_heads, self.n_kv_heads, self.head_dim = n_layers, n_heads, n_kv_heads, head_dim
         self.block_tokens, self.n_blocks, self.max_batch, self.max_blocks = block_tokens, n_blocks, max_batch, max_blocks
         self._c = B.SSDKv8(n_layers=n_layers, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
@@ -133,6 +145,11 @@ class KV8Cache:
         c.data, c.scales, c.table = self.data.data_ptr(), self.scales.data_ptr(), self.table.data_ptr()
         c.pool, c.work = self.pool.data_ptr(), self.work.data_ptr()
         self._index, self._state, self._scale = device.index, (1 + max_batch,), 1.0 / math.sqrt(head_dim)
+
+    def _layer(self, layer: int) -> int:
+        if not 0 <= layer < self.n_layers:
+            _fail(f"layer {layer} of {self.n_layers}")
+        return layer
 
     def new_step(self, batch: int, rows: int, rows_per_request: int | None = None, row_tile: int = 0) -> KV8Step:
         """A plan's buffer for `rows` new rows of `batch` requests.  row_tile: query rows of a kv head the
@@ -163,12 +180,13 @@ class KV8Cache:
         dtype = k.dtype
         if v.dtype is not dtype:
             _fail(f"k and v: one type expected, got {dtype} and {v.dtype}")
-        _call(i, self.lib.ssd_kv8_append, self._ref, layer, k.data_ptr(), v.data_ptr(), _type(dtype, "k"), step.rows,
-              ks[0], ks[1], vs[0], vs[1], step._slot)
+        _call(i, self.lib.ssd_kv8_append, self._ref, self._layer(layer), k.data_ptr(), v.data_ptr(), _type(dtype, "k"),
+              step.rows, ks[0], ks[1], vs[0], vs[1], step._slot)
 
     def read(self, layer: int, slots: torch.Tensor, dtype: torch.dtype = torch.float32):
         """ssd_kv8_read: the (k, v) values held at int32 `slots`, each [n][n_kv_heads][head_dim]."""
         i, n = self._index, slots.numel()
+        self._layer(layer), _ints(slots=n)
         at, code = _int32(slots, (n,), i, "slots"), _type(dtype, "dtype")
         shape = (n, self.n_kv_heads, self.head_dim)
         k = torch.empty(shape, dtype=dtype, device=self.device)
@@ -185,6 +203,7 @@ class KV8Cache:
         if step.cache is not self:
             _fail("the step was made for another cache")
         qs, dtype = _rows3(q, step._q, i, "q"), q.dtype
+        self._layer(layer)
         if out is None:
             out = torch.empty(step._q, dtype=dtype, device=self.device)
             os = out.stride()
@@ -210,6 +229,7 @@ class W4Weight:
         if weight.dim() != 2 or not weight.is_cuda or (weight.stride(1) != 1 and weight.numel()):
             _fail("weight: a 2-D CUDA tensor with contiguous rows expected")
         self.n, self.k = weight.shape
+        _ints(n=self.n, k=self.k, group=group)
         self.group, self.device = group, weight.device
         size = self.lib.ssd_w4_bytes(self.n, self.k, group)
         if size < 0:
@@ -242,6 +262,8 @@ class W4Weight:
         if x.dim() != 2:
             _fail(f"x: [rows][{self.k}] expected, got {tuple(x.shape)}")
         rows, dtype, i = x.shape[0], x.dtype, self._index
+        if rows > _INT:
+            _fail(f"x: {rows} rows")
         xs, code = self._rows(x, (rows, self.k), dtype, "x"), _type(dtype, "x")
         if out is None:
             out = torch.empty((rows, self.n), dtype=dtype, device=self.device)
@@ -285,7 +307,9 @@ class F4Rows:
         if x.dim() != 2 or not x.is_cuda:
             _fail(f"a 2-D CUDA tensor expected, got {tuple(x.shape)} on {x.device}")
         self.lib, self.shape, self.device, self._index = B.load(), x.shape, x.device, x.get_device()
-        self.packed = _f4_buffer(self.lib, self.lib.ssd_f4_bytes(*x.shape), x.device)
+        rows, k = x.shape
+        _ints(rows=rows, k=k)
+        self.packed = _f4_buffer(self.lib, self.lib.ssd_f4_bytes(rows, k), x.device)
         self._packed = self.packed.data_ptr()
         self.pack(x)
 
@@ -321,6 +345,8 @@ class F4Weight(F4Rows):
         if len(shape) != 2 or shape[1] != k:
             _fail(f"x: [rows][{k}] expected, got {tuple(shape)}")
         rows = shape[0]
+        if rows > _INT:
+            _fail(f"x: {rows} rows")
         if isinstance(x, F4Rows):
             if x._index != i:
                 _fail(f"x: on cuda:{i} expected, got {x.device}")
