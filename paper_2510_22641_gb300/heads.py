@@ -141,7 +141,11 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: float | torch.Ten
         min_p, m_rows = 0.0, per_row(min_p, f32, "min_p")
     if isinstance(top_k, tensor):
         top_k, k_rows = 0, per_row(top_k, i32, "top_k")
-    how = _sampling(temperature, top_p, min_p, top_k, t_rows, p_rows, m_rows, k_rows)
+    try:
+        how = _sampling(temperature, top_p, min_p, top_k, t_rows, p_rows, m_rows, k_rows)
+    except (struct.error, OverflowError, TypeError):
+        _fail(f"temperature, top_p and min_p: fp32 numbers expected, top_k: a 32-bit integer, got {temperature}, {top_p}, {min_p}, "
+              f"{top_k}")
     if out is None:
         out = torch.empty(one, dtype=i32, device=device)
     prob = torch.empty(one, dtype=f32, device=device) if with_prob else None

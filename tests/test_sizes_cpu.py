@@ -102,6 +102,12 @@ def test_logits(rows, vocab):
     refused(lambda: lib.sample(Tensor(rows, vocab), Tensor(rows)))
 
 
+@pytest.mark.parametrize("how", [{"top_k": 1 << 31}, {"top_k": 1 << 40}, {"top_k": -(1 << 31) - 1}, {"top_k": 50.0}, {"top_k": None},
+                                 {"temperature": 1e39}, {"temperature": None}, {"top_p": "0.9"}, {"min_p": -1e300}], ids=str)
+def test_settings_of_a_draw(how):
+    refused(lambda: lib.sample(Tensor(3, 100), Tensor(3), **how))
+
+
 def cache():
     return made(lib.KV8Cache, n_layers=2, n_heads=4, n_kv_heads=4, head_dim=64, block_tokens=16, n_blocks=8, max_batch=2, max_blocks=4,
                 _ref=None, _scale=0.125)
