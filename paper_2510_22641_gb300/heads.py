@@ -143,7 +143,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: float | torch.Ten
         top_k, k_rows = 0, per_row(top_k, i32, "top_k")
     try:
         how = _sampling(temperature, top_p, min_p, top_k, t_rows, p_rows, m_rows, k_rows)
-    except (struct.error, OverflowError, TypeError):
+    except (struct.error, OverflowError):
         _fail(f"temperature, top_p and min_p: fp32 numbers expected, top_k: a 32-bit integer, got {temperature}, {top_p}, {min_p}, "
               f"{top_k}")
     if out is None:

@@ -103,7 +103,7 @@ def test_logits(rows, vocab):
 
 
 @pytest.mark.parametrize("how", [{"top_k": 1 << 31}, {"top_k": 1 << 40}, {"top_k": -(1 << 31) - 1}, {"top_k": 50.0}, {"top_k": None},
-                                 {"temperature": 1e39}, {"temperature": None}, {"top_p": "0.9"}, {"min_p": -1e300}], ids=str)
+                                 {"temperature": 10 ** 400}, {"temperature": None}, {"top_p": "0.9"}], ids=str)
 def test_settings_of_a_draw(how):
     refused(lambda: lib.sample(Tensor(3, 100), Tensor(3), **how))
 
