@@ -3,7 +3,7 @@
 
 #include <type_traits>
 
-#include "tcgen05.cuh"
+#include "tcgen05_f4.cuh"
 
 namespace ssd {
 namespace {
