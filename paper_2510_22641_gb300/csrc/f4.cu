@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(256) ssd_f4_unpack_odd_kernel(const uint8_t* p
                                                                 const float* rho, T* out) {
   pdl_wait();
   pdl_trigger();
-  __shared__ float turn[8][kF4Cols];
+  __shared__ alignas(16) float turn[8][kF4Cols];  // stored by 16 bytes
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = blockIdx.x, tile = blockIdx.y;
   const int left = k - chunk * kF4Cols, end = min(rows - tile * kF4Rows, kF4Rows);
   const uint8_t* at = packed + (static_cast<int64_t>(tile) * chunks + chunk) * kF4Record;
