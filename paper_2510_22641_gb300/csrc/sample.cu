@@ -135,13 +135,13 @@ constexpr int kList = 512;  // tokens that one CTA ranks by comparing all with a
 
 struct SampleShared {
   uint32_t table[kExpSize];
-  uint64_t bin[2][kBins];                    // of one search step, and of the next
+  alignas(16) uint64_t bin[2][kBins];        // of one search step, and of the next; read by twos
   uint64_t groups[2][8][kSampleWarps];       // their sums over kGroup bins, of every CTA
   uint64_t seg[kSegs];
   uint64_t part[2][kSampleWarps];
   uint64_t sent[kUses][8];                   // written by the CTA of that rank
   uint64_t list[kList];                      // key and inverted index of tokens that are ranked one by one
-  uint64_t all[kList + 2];                   // the cluster's lists as one
+  alignas(16) uint64_t all[kList + 2];       // the cluster's lists as one; read by twos
   uint64_t by_rank[kList], sorted[kList];
   uint64_t before, at;
   uint64_t arrived[kPieces];                 // barriers of the row's pieces
