@@ -649,8 +649,10 @@ SSD_API ssd_status ssd_f4_matmul(const void* w, int n, int k, const void* x, int
 #define SSD_ROTARY_MAX_DIM 256
 
 /* How heads turn: of the first `turn` elements pair i (elements i and i + turn / 2, or 2 i and 2 i + 1 with
- * interleaved != 0) is rotated by position[axis[i]] * step[i] turns, step a 64-bit fraction of a turn per position, so
- * that angles are exact to pos * 2^-54 of a radian at any position.  The other elements pass through.
+ * interleaved != 0) is rotated by position[axis[i]] * step[i] turns, step a 64-bit fraction of a turn per position, whose
+ * product's overflow is the reduction: at any int32 position an angle is what the step says, cut to 32 bits of a turn
+ * (2^-29 of a radian).  ssd_rotary_init's steps are computed in doubles, to 2^-52 of a radian, so its angles are within
+ * |pos| * 2^-52 + 2^-29.  The other elements pass through.
  * ssd_rotary_init fills it; callers with other frequencies may write step and axis themselves. */
 typedef struct {
   int head_dim;     /* elements of a head, even, 2 .. SSD_ROTARY_MAX_DIM */

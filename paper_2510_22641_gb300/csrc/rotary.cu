@@ -26,7 +26,8 @@ struct RotaryParams {
 };
 
 // Cosine and sine of pos * step turns.  step is a 64-bit fraction of a turn, so the product's low 64 bits are the
-// angle's fraction, with no rounding to grow with the position; the nearest quarter turn is taken off as an integer.
+// angle's fraction, with no rounding but the step's own to grow with the position.  Its upper 32 bits are taken, 2^-29 of a
+// radian; the nearest quarter turn goes off as an integer.
 __device__ __forceinline__ void turn_of(int pos, uint64_t step, float& c, float& s) {
   const int32_t t = static_cast<int32_t>((static_cast<uint64_t>(static_cast<int64_t>(pos)) * step) >> 32);
   const int32_t quarter = static_cast<int32_t>((static_cast<uint32_t>(t) + (1u << 29)) >> 30);
