@@ -287,6 +287,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
     const bool add = p.residual && split == 1 && n < p.n;
     if (add) f4_residual<T, 16>(p, 0, n, cols, res);
     ok = ok && f4_wait(done, 0);
+    if (!ok) drain_ring(full, S::kStages, c1 - c0);  // the copies under way land before their place is used or given up
     tmem_fence_after();
     for (int c = 0; c < nn; c += 16) {
       float v[16];
@@ -467,10 +468,9 @@ __global__ void __launch_bounds__(kF4PairThreads, 1) ssd_f4_matmul_pair_kernel(c
         if (++s == S::kStages) s = 0, phase ^= 1;
       }
     }
-    if (!ok) {
-      *stop = 1;  // the copies under way land before the CTA leaves
-      for (int i = 0; i < S::kStages; ++i) mbar_wait_for(&full[i], i < s ? phase ^ 1 : phase, 100000000ull);
-    }
+    if (!ok) *stop = 1;
+    // The copies under way land before the CTA leaves, whoever gave up waiting for them.
+    for (int i = 0; i < S::kStages; ++i) mbar_wait_for(&full[i], i < s ? phase ^ 1 : phase, 100000000ull);
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       int s = 0, phase = 0, it = 0;
