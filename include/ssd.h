@@ -437,9 +437,12 @@ SSD_API ssd_status ssd_profile_projection(ssd_ctx* ctx, int which, int layer, in
  * (kind SSD_FAULT_ALLOC: reported as SSD_ERR_OOM) or the countdown-th kernel launch
  * through the library's launch wrappers (kind SSD_FAULT_LAUNCH: reported as
  * SSD_ERR_CUDA, the kernel is not launched) of any ctx fails once, without
- * reaching the GPU.  kind SSD_FAULT_NONE or countdown <= 0 disarms.  Process-wide;
- * not thread-safe against concurrent ssd_* calls. */
-enum { SSD_FAULT_NONE = 0, SSD_FAULT_ALLOC = 1, SSD_FAULT_LAUNCH = 2 };
+ * reaching the GPU.  SSD_FAULT_COPY: the countdown-th product of ssd_f4_matmul or
+ * launch of ssd_sample leaves out the first copy of its first tile or row, and its
+ * bounded waits last a quarter of a millisecond, so that they run out; SSD_FAULT_WAIT:
+ * they last that long, with every copy made.  kind SSD_FAULT_NONE or countdown <= 0
+ * disarms.  Process-wide; not thread-safe against concurrent ssd_* calls. */
+enum { SSD_FAULT_NONE = 0, SSD_FAULT_ALLOC = 1, SSD_FAULT_LAUNCH = 2, SSD_FAULT_COPY = 3, SSD_FAULT_WAIT = 4 };
 SSD_API void ssd_set_fault_injection(int kind, int countdown);
 
 /* Runs out one bounded device wait on purpose: a kernel waits, with the same

@@ -26,6 +26,8 @@ SSD_DLEN_GENERATED = 1
 SSD_FAULT_NONE = 0
 SSD_FAULT_ALLOC = 1
 SSD_FAULT_LAUNCH = 2
+SSD_FAULT_COPY = 3
+SSD_FAULT_WAIT = 4
 SSD_TYPE_BF16 = 0
 SSD_TYPE_FP32 = 1
 SSD_TYPE_F4 = 2

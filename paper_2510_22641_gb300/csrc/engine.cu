@@ -24,6 +24,7 @@
 #include "attention.cuh"
 #include "control.cuh"
 #include "gemv.cuh"
+#include "lowbit.cuh"
 #include "prefill_params.cuh"
 
 namespace ssd {
@@ -103,6 +104,12 @@ bool injected_fault(int kind) {
 }
 
 }  // namespace
+
+// Of the next launch of a product of 4-bit floats or of sampling.
+ssd::OpWait ssd::op_wait() {
+  const bool hold = injected_fault(SSD_FAULT_COPY), brief = hold || injected_fault(SSD_FAULT_WAIT);
+  return {brief ? 250000 : 2000000000, hold};
+}
 
 struct ssd_ctx {
   ssd_config cfg{};
@@ -2550,7 +2557,7 @@ ssd_status ssd_get_batch_step_log(ssd_ctx* c, int b, int32_t* accepted, int32_t*
 void ssd_set_fault_injection(int kind, int countdown) {
   g_fault_kind.store(0);
   g_fault_countdown.store(countdown > 0 ? countdown : 0);
-  if (countdown > 0 && (kind == SSD_FAULT_ALLOC || kind == SSD_FAULT_LAUNCH)) g_fault_kind.store(kind);
+  if (countdown > 0 && kind > SSD_FAULT_NONE && kind <= SSD_FAULT_WAIT) g_fault_kind.store(kind);
 }
 
 ssd_status ssd_probe_bounded_wait(ssd_ctx* c, int64_t limit_ns) {

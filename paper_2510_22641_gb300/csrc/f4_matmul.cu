@@ -19,6 +19,8 @@ struct F4MatmulParams {
   void* y;
   const void* residual;
   int64_t y_row, r_row;
+  long long limit;  // of a wait, in cycles of the SM's clock
+  int hold;         // the first tile's first copy of w is left out
 };
 
 // sum * rho_x * rho_w by two powers of two with the same sign of exponent, so that neither step leaves the range
@@ -32,20 +34,20 @@ __device__ __forceinline__ float f4_scaled(float sum, uint32_t rho_x, uint32_t r
 // Whether a scale is within 2^-60 .. 2^60, where a sum may be multiplied by one after the other.
 __device__ __forceinline__ bool f4_plain(uint32_t rho) { return rho - (67u << 23) <= (120u << 23); }
 
-// Bounded waits, of about two seconds by the SM's clock: false when they run out.
+// Bounded waits, of about two seconds: false when they run out.
 template <typename F>
-__device__ __forceinline__ bool f4_wait_for(F ready) {
+__device__ __forceinline__ bool f4_wait_for(F ready, long long limit) {
   long long start = 0;
   for (uint32_t i = 1;; ++i) {
     if (ready()) return true;
     if ((i & 1023u) != 0) continue;
     const long long now = clock64();
     if (start == 0) start = now;
-    if (now - start > 4000000000ll) return false;
+    if (now - start > limit) return false;
   }
 }
-__device__ __forceinline__ bool f4_wait(uint64_t* bar, uint32_t parity) {
-  return f4_wait_for([&] { return mbar_try_wait(bar, parity); });
+__device__ __forceinline__ bool f4_wait(uint64_t* bar, uint32_t parity, long long limit) {
+  return f4_wait_for([&] { return mbar_try_wait(bar, parity); }, limit);
 }
 
 // N sums times their rows' scales (rho: of the x rows, in shared memory, 16-byte aligned); NaN where the sums are not
@@ -184,7 +186,8 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
       auto load_w = [&](int c) {
         const int s = (c - c0) % S::kStages;
         mbar_arrive_expect_tx(&full[s], kF4Record + (kPack ? 0 : nn * 128 + S::kScales));
-        bulk_load(smem + s * S::kStage, w + static_cast<int64_t>(c) * kF4Record, kF4Record, &full[s]);
+        if (!p.hold || blockIdx.x + c > 0)
+          bulk_load(smem + s * S::kStage, w + static_cast<int64_t>(c) * kF4Record, kF4Record, &full[s]);
       };
       auto load_x = [&](int c) {
         if (kPack) return;
@@ -202,7 +205,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
       int c = ahead;
       for (; c < c1; ++c) {
         const int i = c - c0;
-        if (!f4_wait(&empty[i % S::kStages], (i / S::kStages - 1) & 1)) break;
+        if (!f4_wait(&empty[i % S::kStages], (i / S::kStages - 1) & 1, p.limit)) break;
         load_w(c);
         load_x(c);
       }
@@ -213,7 +216,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
       const uint32_t idesc = umma_idesc_f4(kF4Rows, nn);
       for (int c = c0; c < c1; ++c) {
         const int i = c - c0, s = i % S::kStages;
-        if (!f4_wait(&full[s], (i / S::kStages) & 1)) {
+        if (!f4_wait(&full[s], (i / S::kStages) & 1, p.limit)) {
           ok = false;
           break;
         }
@@ -263,7 +266,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
         uint8_t* const at = smem + s * S::kStage + kF4Record;
         for (int r = 0; r < cols; ++r, ++turn) {
           if ((turn & 3) != warp - 2) continue;
-          ok = __all_sync(~0u, i < S::kStages || f4_wait(&empty[s], (i / S::kStages - 1) & 1));
+          ok = __all_sync(~0u, i < S::kStages || f4_wait(&empty[s], (i / S::kStages - 1) & 1, p.limit));
           if (!ok) break;
           const F4Row f(max(max(part[4 * r], part[4 * r + 1]), max(part[4 * r + 2], part[4 * r + 3])));
           if (lane == 0) rho[r] = __float_as_uint(f.rho());
@@ -286,7 +289,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
     float res[16] = {};
     const bool add = p.residual && split == 1 && n < p.n;
     if (add) f4_residual<T, 16>(p, 0, n, cols, res);
-    ok = ok && f4_wait(done, 0);
+    ok = ok && f4_wait(done, 0, p.limit);
     if (!ok) drain_ring(full, S::kStages, c1 - c0);  // the copies under way land before their place is used or given up
     tmem_fence_after();
     for (int c = 0; c < nn; c += 16) {
@@ -460,11 +463,12 @@ __global__ void __launch_bounds__(kF4PairThreads, 1) ssd_f4_matmul_pair_kernel(c
       }
       const uint32_t bytes = kF4Record + half * 128 + records * S::kScales;
       for (int c = 0; c < p.chunks; ++c, src += kF4Record) {
-        ok = __all_sync(~0u, !*stop && f4_wait(&empty[s], phase));
+        ok = __all_sync(~0u, !*stop && f4_wait(&empty[s], phase, p.limit));
         if (!ok) break;
         if (lane == 0) mbar_arrive_expect_tx(&full[s], bytes);
         __syncwarp();
-        if (size) bulk_load(smem + s * S::kStage + to, src, size, &full[s]);
+        if (size && (!p.hold || blockIdx.x + t + c + lane > 0))
+          bulk_load(smem + s * S::kStage + to, src, size, &full[s]);
         if (++s == S::kStages) s = 0, phase ^= 1;
       }
     }
@@ -478,11 +482,11 @@ __global__ void __launch_bounds__(kF4PairThreads, 1) ssd_f4_matmul_pair_kernel(c
       const uint64_t a0 = umma_desc_sw128(smem_u32(smem)), b0 = umma_desc_sw128(smem_u32(smem) + kF4Record);
       for (int t = first; t < tiles && ok; t += step, ++it) {
         const uint32_t idesc = umma_idesc_f4(2 * kF4Rows, tile_cols(t % tiles_m * BN));
-        if (*stop || !f4_wait(taken, (it & 1) ^ 1)) break;
+        if (*stop || !f4_wait(taken, (it & 1) ^ 1, p.limit)) break;
         tmem_fence_after();
         uint32_t more = 0;
         for (int c = 0; c < p.chunks; ++c) {
-          ok = f4_wait(&full[s], phase) && f4_wait(&scaled[s], phase);
+          ok = f4_wait(&full[s], phase, p.limit) && f4_wait(&scaled[s], phase, p.limit);
           if (!ok) break;
           tmem_fence_after();
           const uint32_t sa = tmem + S::kSums + s * S::kScaleCols, sb = sa + 16;
@@ -507,7 +511,7 @@ __global__ void __launch_bounds__(kF4PairThreads, 1) ssd_f4_matmul_pair_kernel(c
     const uint32_t arrive0 = cluster_map(scaled, 0);
     for (int t = first; t < tiles && ok; t += step)
       for (int c = 0; c < p.chunks; ++c) {
-        ok = __all_sync(~0u, !*stop && f4_wait(&full[s], phase));
+        ok = __all_sync(~0u, !*stop && f4_wait(&full[s], phase, p.limit));
         if (!ok) break;
         const uint8_t* at = smem + s * S::kStage + kF4CodeBytes + lane * 16;
         const uint32_t to = tmem + quarter + S::kSums + s * S::kScaleCols;
@@ -568,7 +572,7 @@ __global__ void __launch_bounds__(kF4PairThreads, 1) ssd_f4_matmul_pair_kernel(c
           ahead[j] = store && from + j < left ? to_f32(res[(from + j) * p.r_row]) : 0.0f;
       };
       if (sizeof(T) == 4 && p.residual) fetch(0);
-      const bool ok = !*stop && f4_wait(done, it & 1);  // after a failure the rest is NaN
+      const bool ok = !*stop && f4_wait(done, it & 1, p.limit);  // after a failure the rest is NaN
       tmem_fence_after();
       // bf16 results are scaled and packed as they are read, 32 at a time, fp32 ones take two turns of 64: the registers of
       // 14 warps hold no more.  The tensor memory is given back after the last read.
@@ -730,6 +734,8 @@ ssd_status ssd_f4_matmul(const void* w, int n, int k, const void* x, int x_type,
     p.vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (rows == 1 || x_row_stride % (16 / xsize) == 0);
   }
   p.y = y, p.residual = residual, p.y_row = y_row_stride, p.r_row = res_row_stride;
+  const OpWait wait = op_wait();
+  p.limit = 2 * wait.ns, p.hold = wait.hold;
   return type == SSD_TYPE_FP32 ? f4_dispatch<float>(p, x_type, s) : f4_dispatch<__nv_bfloat16>(p, x_type, s);
 }
 

@@ -51,6 +51,12 @@ template <typename... P, typename... A>
 ssd_status op_launch(const char* what, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t s, A... args) {
   return op_launch_cluster(what, kernel, grid, threads, smem, dim3(1), s, args...);
 }
+// How long a launch's bounded waits last, in nanoseconds, and whether its first copy is left out (ssd_set_fault_injection).
+struct OpWait {
+  int64_t ns;
+  bool hold;
+};
+OpWait op_wait();
 // The status of a launch that has just been made.
 ssd_status op_launched(const char* what);
 

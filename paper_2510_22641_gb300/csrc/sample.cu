@@ -111,6 +111,8 @@ struct SampleParams {
   ssd_sampling how;
   int32_t* token;
   float* prob;
+  uint64_t limit;  // of a wait, in nanoseconds
+  int hold;        // the first row's first copy is left out
 };
 
 // ------------------------------------------------------------------ the kernel
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
     for (int i = 0; i < kPieces; ++i) {
       const int u0 = max(i * piece, 1), u1 = min((i + 1) * piece, units - 1);
       mbar_arrive_expect_tx(&sh.arrived[i], u0 < u1 ? (u1 - u0) * 16 : 0);
-      if (u0 < u1) bulk_load(data + u0, in + u0, (u1 - u0) * 16, &sh.arrived[i]);
+      if (u0 < u1 && (!p.hold || rank + row + i > 0)) bulk_load(data + u0, in + u0, (u1 - u0) * 16, &sh.arrived[i]);
     }
   }
   if (warp == 1 && lane < 2 * E) {  // the first and the last unit
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(kSampleThreads) ssd_sample_kernel(const Sample
   __syncthreads();
   float most = -INFINITY;
   for (int i = 0; i < kPieces; ++i) {
-    if (!mbar_wait(&sh.arrived[i], 0)) sh.failed = 1;
+    if (!mbar_wait_for(&sh.arrived[i], 0, p.limit)) sh.failed = 1;
 #pragma unroll 2
     for (int u = i * piece + tid; u < min((i + 1) * piece, units); u += kSampleThreads) {
       const Logits16<T> x = data[u];
@@ -716,7 +718,8 @@ extern "C" ssd_status ssd_sample(const void* logits, int type, int rows, int voc
       shared |= x && op_overlap(row_words(y), row_words(x), 1);
     if (shared) return op_fail(SSD_ERR_INVALID_ARG, "ssd_sample: an output overlaps another buffer");
   }
-  const SampleParams p{logits, row_stride, vocab, u, *how, token, prob};
+  const OpWait wait = op_wait();
+  const SampleParams p{logits, row_stride, vocab, u, *how, token, prob, static_cast<uint64_t>(wait.ns), wait.hold};
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   return type == SSD_TYPE_FP32 ? sample_launch<float>(p, rows, s) : sample_launch<__nv_bfloat16>(p, rows, s);
 }
