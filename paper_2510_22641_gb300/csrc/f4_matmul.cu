@@ -213,6 +213,7 @@ __global__ void __launch_bounds__(192) ssd_f4_matmul_kernel(const F4MatmulParams
     }
   } else if (warp == 1) {
     if (lane == 0) {
+      pdl_wait();  // what the launch before still takes is not time that the waits below may run out in
       const uint32_t idesc = umma_idesc_f4(kF4Rows, nn);
       for (int c = c0; c < c1; ++c) {
         const int i = c - c0, s = i % S::kStages;

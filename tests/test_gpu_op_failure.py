@@ -70,3 +70,25 @@ def test_short_waits_are_long_enough():
     with injected(lib.SSD_FAULT_WAIT):
         t = lib.sample(z, u)
     assert torch.equal(t, want)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_waits_begin_after_the_launch_before(rows):
+    """A product may take its place on the GPU while the launch before it still runs; that time is not its own.  Here that
+    launch takes more than a millisecond on two SMs, and the waits behind it last a quarter of one."""
+    k = 1 << 20
+    big, wide = lib.F4Weight(normal((200, k), 1, 0.02)), lib.F4Rows(normal((200, k), 2))
+    w, x = lib.F4Weight(normal((300, 2560), 3, 0.02)), lib.F4Rows(uneven(rows, 2560, 4))
+    want = w.matmul(x)
+    for _ in range(3):
+        torch.cuda.synchronize()
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        big.matmul(wide)
+        b.record()
+        torch.cuda.synchronize()
+        assert a.elapsed_time(b) > 0.5, "the launch before is too short for this test"
+        big.matmul(wide)
+        with injected(lib.SSD_FAULT_WAIT):
+            y = w.matmul(x)
+        assert torch.equal(y, want)
