@@ -714,8 +714,8 @@ typedef struct {
  * temperature 0, top_p 1, min_p 0, u 0.
  *   logits: device, type SSD_TYPE_*, [rows][row_stride];  u: device fp32 [rows], in [0, 1)
  *   token: device int32 [rows];  prob: device fp32 [rows], the token's share of the kept mass, or NULL
- * Masses are exp(z - max z) to about 2^-30 of themselves or 2^-44, held as integers, so the result does not depend on
- * the order of any sum.  vocab at most SSD_SAMPLE_MAX_VOCAB.  token and prob must not overlap each other or an input.
+ * Masses are exp(z - max z) to about 2^-30 of themselves or 2^-44, held as integers, so a row's result does not depend
+ * on the order of any sum or on the rows that come with it.  vocab at most SSD_SAMPLE_MAX_VOCAB.  token and prob must not overlap each other or an input.
  * Should a wait inside the kernel run out (two seconds), the row's token is -1 and its prob NaN. */
 SSD_API ssd_status ssd_sample(const void* logits, int type, int rows, int vocab, int64_t row_stride, const float* u,
                               const ssd_sampling* how, int32_t* token, float* prob, void* cuda_stream);

@@ -12,8 +12,9 @@ struct F4PackParams {
   float* rho;
 };
 
-// Packing reads x and writes 0.56 bytes an element; what bounds it is instructions (16 an element, 74 % of the issue
-// slots): 22016 x 4096 bf16 in 50 us (floor 34).  Read twice, eight warps a row, correctly rounded reciprocals: 77.
+// Packing reads x and writes 0.56 bytes an element: 22016 x 4096 bf16 in 50 us (floor 34), fp32 in 64 (floor 61).  At bf16
+// neither bytes (0.68 of the copy rate) nor instructions (16 an element, 74 % of the issue slots) bound it alone: warps
+// wait for loads, 57 % of the places taken.  Read twice, eight warps a row, correctly rounded reciprocals: 77.
 //
 // A row is held in registers between its maximum and its codes, by `warps` warps (1, 2, 4 or 8) of up to J chunks of
 // 256 columns each, 8 columns a lane; the CTA has 8 warps.  The row is read once.
@@ -80,7 +81,8 @@ __global__ void __launch_bounds__(256) ssd_f4_pack_long_kernel(const F4PackParam
   }
 }
 
-// Reading back writes 4 bytes an element (to fp32) for 0.56 read: 22016 x 4096 in 65 us, 0.94 of the copy rate; eight
+// Reading back writes 4 bytes an element (to fp32) for 0.56 read: 22016 x 4096 in 66 us, 0.92 of the copy rate (to bf16 40,
+// 0.86); eight
 // neighbouring columns a lane, whose stores leave every second 16 bytes to the next instruction, took 81, a column a
 // thread 357.
 //

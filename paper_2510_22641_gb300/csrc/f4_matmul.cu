@@ -127,9 +127,10 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr, uint32_t rank) {
 // A tile is 128 weight rows (the matrix rows, so that few x rows are few columns) by all x rows, up to BN.  The bytes of
 // the weights bound it, in time the latency of 16 stages a CTA: 96 rows x 22016 x 4096 take 16.4 us with the packing of
 // x (floor 9.0, two CTAs an SM; with one, in two turns, 23.6), 1 row x 4096 x 4096 6.6 us, of which the weights are 1.4.
+// 33 to 64 rows have one CTA an SM, as two lack 1152 bytes of shared memory: 64 x 22016 x 4096 22.8 us, 32 rows 14.3.
 template <int BN>
 struct F4Tile {
-  static constexpr int kStages = BN > 64 ? 3 : 4;  // two CTAs an SM
+  static constexpr int kStages = BN > 64 ? 3 : 4;  // two CTAs an SM, of 64 columns one
   static constexpr int kCodes = BN * kF4Cols / 2, kScales = kF4Record - kF4CodeBytes;
   static constexpr int kStage = kF4Record + kCodes + kScales;
   // tensor memory columns: the sums, then each stage's scales (16 of w, 16 of x)
@@ -671,7 +672,8 @@ ssd_status f4_dispatch(const F4MatmulParams& p, int x_type, cudaStream_t s) {
   const int bn = p.rows <= 16 ? 16 : p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
   const int tiles = (p.n + kF4Rows - 1) / kF4Rows;
   // A cluster shares a tile's columns as long as that leaves a CTA an SM (1 x 4096 x 4096: one CTA a tile 11.2 us, four
-  // 7.1; with more CTAs than SMs the clusters wait for each other's places: 64 x 11008 x 4096 one 12.8, two 20.5).
+  // 7.1; with more CTAs than places the clusters wait for each other: 64 x 11008 x 4096, where an SM takes one CTA, one a
+  // tile 12.4, two 20.5.  Between one and two CTAs an SM the sizes that have room for two were not measured).
   int split = 1;
   while (split < 8 && tiles * split * 2 <= 152 && split * 2 <= p.chunks) split *= 2;
   if (p.rows_in)

@@ -20,8 +20,8 @@ constexpr int kExpBits = 10, kExpSize = 1 << kExpBits;
 struct ExpTable {
   uint32_t v[kExpSize];
 };
-// 2^(-j / 1024) * 2^32, less so that a value times 2^((0.6 + f) / 1024), at most 2^(1.18 / 1024), fits 32 bits (the common factor cancels).  The
-// Taylor series of e^x, 0 <= x < ln 2, in 64 bits when this is compiled.
+// 2^(-j / 1024) * 2^32, less so that a value times 2^((0.6 + f) / 1024), at most 2^(1.18 / 1024), fits 32 bits (the common
+// factor cancels).  The Taylor series of e^x, 0 <= x < ln 2, in 64 bits when this is compiled.
 constexpr ExpTable make_exp_table() {
   ExpTable t = {};
   for (int j = 0; j < kExpSize; ++j) {
@@ -117,16 +117,17 @@ struct SampleParams {
 
 // ------------------------------------------------------------------ the kernel
 //
-// What bounds it: instructions (28 an element where every token's mass is needed) and the barriers between the steps.
-// 256 rows of 150001 bf16 logits: 33 us for the largest alone (floor 11.4), 50 with top_k 50, 88 when every mass is added
-// up once, 205 with top_p 0.95 (twice, and the border's search); mixed rows 107 (bit by bit over a row that is read
-// again for every bit: 5095).  One row of 32000: 12.9 us, of which clusters' barriers and the first fetch of the code
-// are most.
+// What bounds it: instructions (42 an element over mixed rows) and the barriers between the steps.
+// 256 rows of 150001 bf16 logits: 33 us for the largest alone (floor 11.4), 50 with top_k 50, 83 when every mass is added
+// up once, 197 with top_p 0.95 (twice, and the border's search); mixed rows 108 to 111 (bit by bit over a row that is
+// read again for every bit: 5095).  One row of 32000: 12.3 to 12.9 us, of which clusters' barriers and the first fetch of
+// the code are most.
 //
 // A cluster of CTAs holds a row in shared memory, read from global memory once, with the largest logit found on the way.
 // A rule's border is found by counting: tokens (or their masses) are added up in 704 bins of a sixteenth of an octave of
 // mass each; the bin in which the rule's count or mass is reached is split by the logits' bits into up to 704 again until
-// one value is left.  All sums are of integers, so neither the atomics' order nor the cut into CTAs matters.
+// one value is left.  All sums are of the masses as integers, exact, so neither the atomics' order nor the cut into CTAs
+// matters, nor which of the searches a row takes.
 
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kBins = static_cast<int>(kMassPlaces >> 6), kGroup = kBins / kSampleWarps,
               kSegUnits = 64, kSegs = 256;
